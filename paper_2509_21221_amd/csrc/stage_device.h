@@ -1,0 +1,135 @@
+// Device helpers of the microbatch operators: rows of any alignment in steps
+// of eight columns, and reductions over a wave.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gwtf {
+
+using f16_t = _Float16;
+using bf16_t = __bf16;
+
+// Eight adjacent columns.  Loads and stores of whole eights are one 16-byte
+// access (two for 32-bit types) that needs no more alignment than the element.
+constexpr int kVec = 8;
+
+template <class T>
+struct Vec8 {
+    typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+};
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+// Columns [0, n) of p, the rest `fill`.  n >= 8 is the common case.
+template <class T>
+__device__ __forceinline__ void load8(const T *p, int64_t n, float v[8], float fill = 0.f)
+{
+    if (n >= kVec) {
+        const f32x8 f = __builtin_convertvector(*reinterpret_cast<const typename Vec8<T>::type *>(p), f32x8);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = f[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = i < n ? float(p[i]) : fill;
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void store8(T *p, int64_t n, const float v[8])
+{
+    if (n >= kVec) {
+        f32x8 f;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) f[i] = v[i];
+        *reinterpret_cast<typename Vec8<T>::type *>(p) = __builtin_convertvector(f, typename Vec8<T>::type);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (i < n) p[i] = T(v[i]);
+    }
+}
+
+__device__ __forceinline__ int64_t load_token(const void *t, int is64, int64_t i)
+{
+    return is64 ? static_cast<const int64_t *>(t)[i] : int64_t(static_cast<const int32_t *>(t)[i]);
+}
+
+// Division of u < 2^32 by a fixed d >= 1 (Granlund and Montgomery): a high
+// product and two shifts.
+struct FastDiv {
+    uint32_t d, m, s1, s2;
+    static FastDiv make(uint32_t d)
+    {
+        uint32_t l = 0;
+        while (l < 32 && (uint64_t(1) << l) < d) ++l;
+        FastDiv f;
+        f.d = d;
+        f.m = uint32_t(((uint64_t(1) << 32) * ((uint64_t(1) << l) - d)) / d + 1);
+        f.s1 = l < 1 ? l : 1;
+        f.s2 = l > 1 ? l - 1 : 0;
+        return f;
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t u) const
+    {
+        const uint32_t t = __umulhi(m, u);
+        return (t + ((u - t) >> s1)) >> s2;
+    }
+};
+
+// Lane exchanges within rows of 16 lanes (rotation by n).
+template <int n>
+__device__ __forceinline__ int row_ror(int v)
+{
+    return __builtin_amdgcn_update_dpp(v, v, 0x120 + n, 0xf, 0xf, false);
+}
+template <int n>
+__device__ __forceinline__ float row_ror(float v)
+{
+    return __int_as_float(row_ror<n>(__float_as_int(v)));
+}
+
+__device__ __forceinline__ float lane_value(float v, int lane)
+{
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
+// Sum over 16 lanes, in every one of them; over the wave, uniform.
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += row_ror<8>(v);
+    v += row_ror<4>(v);
+    v += row_ror<2>(v);
+    v += row_ror<1>(v);
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v = row_sum(v);
+    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+}
+
+// The largest of unsigned words likewise (float magnitudes compare as their
+// bits do, with infinities and NaN above all numbers).
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint32_t row_umax(uint32_t v)
+{
+    v = umax(v, uint32_t(row_ror<8>(int(v))));
+    v = umax(v, uint32_t(row_ror<4>(int(v))));
+    v = umax(v, uint32_t(row_ror<2>(int(v))));
+    v = umax(v, uint32_t(row_ror<1>(int(v))));
+    return v;
+}
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v)
+{
+    v = row_umax(v);
+    const uint32_t a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16);
+    const uint32_t c = __builtin_amdgcn_readlane(v, 32), d = __builtin_amdgcn_readlane(v, 48);
+    return umax(umax(a, b), umax(c, d));
+}
+
+// 2^x and ln 2 / log2 e; the hardware's exponential and logarithm have base 2.
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+} // namespace gwtf

@@ -1,0 +1,109 @@
+// Dropout whose mask is a function of the seed, the site and the row's
+// identity (gwtf_stage_dropout).
+//
+//   out = residual + (u >= t ? x * 65536 / (65536 - t) : 0)
+//
+// One call of Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random
+// numbers: as easy as 1, 2, 3", 2011) gives the 16-bit u of eight columns: ten
+// rounds of two 32 x 32 -> 64 bit products for 16 bytes of a 16-bit type.
+// With 32 bits a value the products, which take four times as long to issue
+// as other operations, would cost more than the memory.
+#include "stage_device.h"
+#include "stage_internal.h"
+
+namespace gwtf {
+namespace {
+
+struct DropoutParams {
+    const void *x, *res;
+    void *out;
+    const int64_t *rows;
+    int64_t xs, rs, os, row0;
+    int32_t H;
+    uint32_t units; // (rows of this launch) * (steps of eight columns in a row)
+    FastDiv steps;
+    uint32_t k0, k1, site, limit;
+    float keep_scale;
+};
+
+__device__ __forceinline__ void philox4x32(uint32_t k0, uint32_t k1, uint32_t c[4])
+{
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = uint64_t(0xD2511F53u) * c[0], b = uint64_t(0xCD9E8D57u) * c[2];
+        const uint32_t n0 = uint32_t(b >> 32) ^ c[1] ^ k0, n2 = uint32_t(a >> 32) ^ c[3] ^ k1;
+        c[1] = uint32_t(b);
+        c[3] = uint32_t(a);
+        c[0] = n0;
+        c[2] = n2;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void dropout_kernel(DropoutParams p)
+{
+    const uint32_t u = blockIdx.x * 256u + threadIdx.x;
+    if (u >= p.units) return;
+    const uint32_t r = p.steps.div(u), step = u - r * p.steps.d;
+    const int64_t row = p.row0 + r, col = int64_t(step) * kVec, n = p.H - col;
+    float v[8], res[8];
+    load8(static_cast<const T *>(p.x) + row * p.xs + col, n, v);
+    if (p.res) load8(static_cast<const T *>(p.res) + row * p.rs + col, n, res);
+    const uint64_t id = p.rows ? uint64_t(p.rows[row]) : uint64_t(row);
+    uint32_t c[4] = {step, p.site, uint32_t(id), uint32_t(id >> 32)};
+    philox4x32(p.k0, p.k1, c);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        const uint32_t bits = (i & 1) ? c[i / 2] >> 16 : c[i / 2] & 0xffffu;
+        v[i] = bits >= p.limit ? v[i] * p.keep_scale : 0.f;
+        if (p.res) v[i] += res[i];
+    }
+    store8(static_cast<T *>(p.out) + row * p.os + col, n, v);
+}
+
+template <class T>
+hipError_t run(const gwtf_stage_dropout_t &a, uint32_t limit, hipStream_t s)
+{
+    const int64_t steps = (a.hidden + kVec - 1) / kVec;
+    // units of one launch stay below 2^30
+    const int64_t slab = (int64_t(1) << 30) / steps;
+    DropoutParams p;
+    p.x = a.x;
+    p.res = a.residual;
+    p.out = a.out;
+    p.rows = a.rows;
+    p.xs = a.x_stride;
+    p.rs = a.residual_stride;
+    p.os = a.out_stride;
+    p.H = int32_t(a.hidden);
+    p.steps = FastDiv::make(uint32_t(steps));
+    p.k0 = uint32_t(a.seed);
+    p.k1 = uint32_t(a.seed >> 32);
+    p.site = a.site;
+    p.limit = limit;
+    p.keep_scale = 65536.f / float(65536 - limit);
+    for (int64_t r = 0; r < a.num_tokens; r += slab) {
+        const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
+        p.row0 = r;
+        p.units = uint32_t(n * steps);
+        dropout_kernel<T><<<dim3((p.units + 255) / 256), dim3(256), 0, s>>>(p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+} // namespace
+
+hipError_t launch_dropout(const gwtf_stage_dropout_t &a, uint32_t limit, hipStream_t s)
+{
+    switch (a.type) {
+    case GWTF_TYPE_F32: return run<float>(a, limit, s);
+    case GWTF_TYPE_F16: return run<f16_t>(a, limit, s);
+    default: return run<bf16_t>(a, limit, s);
+    }
+}
+
+} // namespace gwtf

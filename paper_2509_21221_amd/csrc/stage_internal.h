@@ -1,0 +1,45 @@
+// Internal interface between the host API of the microbatch operators
+// (stage_api.hip) and their kernels.  Not part of the public C ABI.
+#pragma once
+
+#include "gwtf_stage.h"
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace gwtf {
+
+// Device workspace of a handle, used in the order of its stream.
+struct StageWorkspace {
+    uint64_t *sort_a = nullptr, *sort_b = nullptr; // [max_tokens] each: token << 32 | position
+    float *partial = nullptr;                      // embedding gradient: sums of runs that cross chunks
+    float *dweight = nullptr;                      // norm gradient: [kNormGradGroups][max_hidden]
+    unsigned char *logprob = nullptr;              // kLogprobItems records, then kLogprobRows counters (0 between calls)
+    int cus = 0;
+};
+
+// Embedding gradient: the sorted tokens are dealt out in chunks, one wave per
+// chunk and slab of columns, about kEmbedItems of them.
+constexpr int64_t kEmbedItems = 8192;
+constexpr int kEmbedMinChunk = 4;
+int64_t embed_partial_bytes(int64_t max_tokens, int64_t max_hidden);
+
+// Norm gradient: most workgroups that sum dweight over their rows.
+constexpr int kNormGradGroups = 1024;
+
+// Log probabilities: most rows that are split over workgroups, most
+// workgroups that then share them, and bytes of one's record.
+constexpr int kLogprobRows = 512;
+constexpr int kLogprobItems = 2048;
+constexpr int kLogprobRecord = 16 + 8 * GWTF_STAGE_MAX_TOP;
+
+hipError_t launch_embed(const gwtf_stage_embed_t &a, hipStream_t s);
+hipError_t launch_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace &w, hipStream_t s);
+hipError_t launch_dropout(const gwtf_stage_dropout_t &a, uint32_t limit, hipStream_t s);
+hipError_t launch_norm(const gwtf_stage_norm_t &a, const StageWorkspace &w, hipStream_t s);
+hipError_t launch_norm_grad(const gwtf_stage_norm_grad_t &a, const StageWorkspace &w, hipStream_t s);
+hipError_t launch_logprob(const gwtf_stage_logprob_t &a, const StageWorkspace &w, hipStream_t s);
+hipError_t launch_logprob_grad(const gwtf_stage_logprob_grad_t &a, const StageWorkspace &w, hipStream_t s);
+
+} // namespace gwtf

@@ -1,0 +1,327 @@
+// Hand-off between stages: residual added, RMS norm, optional 8-bit values
+// (gwtf_stage_norm), and the gradient (gwtf_stage_norm_grad).
+//
+//   h = x + residual, rstd = 1 / sqrt(mean(h^2) + eps), y = h * rstd * weight
+//   dx = dh + rstd * (dy * weight - xhat * mean(dy * weight * xhat)), xhat = h * rstd
+//   dweight = sum over rows of dy * xhat
+//
+// A row stays in registers between its reduction and its use, eight columns a
+// lane, so that every value is read once: one wave a row up to 1024 columns,
+// WAVES waves a row above.
+#include "stage_device.h"
+#include "stage_internal.h"
+
+namespace gwtf {
+namespace {
+
+constexpr float kF8Max = 448.f;
+constexpr float kScaleMin = 0x1p-126f;
+
+// Sum over the waves of a row (one wave: itself), in every lane.
+template <int WAVES>
+__device__ __forceinline__ float group_sum(float v, float *red, int wave)
+{
+    v = wave_sum(v);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) red[wave] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) v += red[i];
+    }
+    return v;
+}
+
+__device__ __forceinline__ void store_f8(uint8_t *p, int64_t n, const float v[8])
+{
+    int lo = 0, hi = 0;
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], lo, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], hi, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], hi, true);
+    if (n >= kVec) {
+        typedef int i32x2 __attribute__((ext_vector_type(2), aligned(1)));
+        i32x2 w;
+        w[0] = lo;
+        w[1] = hi;
+        *reinterpret_cast<i32x2 *>(p) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (i < n) p[i] = uint8_t((i < 4 ? lo : hi) >> (8 * (i & 3)));
+    }
+}
+
+// y / s of one scale's values; `bits`: the largest magnitude's.
+__device__ __forceinline__ float scale_of(uint32_t bits)
+{
+    return bits >= 0x7f800000u ? __builtin_nanf("") : fmaxf(__uint_as_float(bits) / kF8Max, kScaleMin);
+}
+__device__ __forceinline__ void quantise(float y[8], float s)
+{
+    const float inv = 1.f / s;
+    const bool bad = !(s == s);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        const float v = fminf(fmaxf(y[i] * inv, -kF8Max), kF8Max); // the product may round past 448
+        y[i] = bad ? s : v;
+    }
+}
+
+template <class T, int K, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwtf_stage_norm_t p)
+{
+    __shared__ float red[WAVES];
+    __shared__ uint32_t redmax[WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = WAVES == 1 ? int64_t(blockIdx.x) * 4 + wave : int64_t(blockIdx.x);
+    if (row >= p.num_tokens) return; // WAVES == 1 only: no barrier follows
+    const int part = WAVES == 1 ? 0 : wave;
+    const T *x = static_cast<const T *>(p.x) + row * p.x_stride;
+    const T *res = static_cast<const T *>(p.residual) + row * p.residual_stride;
+    const T *weight = static_cast<const T *>(p.weight);
+    const int H = int(p.hidden);
+
+    float h[K][8], sq = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int col = ((k * WAVES + part) * 64 + lane) * kVec;
+        load8(x + col, H - col, h[k]);
+        if (p.residual) {
+            float r[8];
+            load8(res + col, H - col, r);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) h[k][i] += r[i];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sq += h[k][i] * h[k][i];
+    }
+    sq = group_sum<WAVES>(sq, red, part);
+    const float rstd = 1.f / sqrtf(sq / float(H) + p.eps);
+    if (p.rstd && part == 0 && lane == 0) p.rstd[row] = rstd;
+
+    uint32_t most = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int col = ((k * WAVES + part) * 64 + lane) * kVec, n = H - col;
+        if (p.h_out) store8(static_cast<T *>(p.h_out) + row * p.h_stride + col, n, h[k]);
+        float w[8];
+        load8(weight + col, n, w);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) h[k][i] = h[k][i] * rstd * w[i];
+        if (p.form == GWTF_NORM_PLAIN) {
+            store8(static_cast<T *>(p.y) + row * p.y_stride + col, n, h[k]);
+            continue;
+        }
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (i < n) m = umax(m, __float_as_uint(h[k][i]) & 0x7fffffffu);
+        if (p.form == GWTF_NORM_F8_BLOCK) { // 128 columns are 16 lanes
+            const float s = scale_of(row_umax(m));
+            quantise(h[k], s);
+            store_f8(static_cast<uint8_t *>(p.y) + row * p.y_stride + col, n, h[k]);
+            const int blocks = (H + GWTF_NORM_BLOCK - 1) / GWTF_NORM_BLOCK;
+            if ((lane & 15) == 0 && n > 0) p.scales[row * blocks + col / GWTF_NORM_BLOCK] = s;
+        } else {
+            most = umax(most, m);
+        }
+    }
+    if (p.form != GWTF_NORM_F8_ROW) return;
+    most = wave_umax(most);
+    if constexpr (WAVES > 1) {
+        if (lane == 0) redmax[wave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) most = umax(most, redmax[i]);
+    }
+    const float s = scale_of(most);
+    if (part == 0 && lane == 0) p.scales[row] = s;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int col = ((k * WAVES + part) * 64 + lane) * kVec;
+        quantise(h[k], s);
+        store_f8(static_cast<uint8_t *>(p.y) + row * p.y_stride + col, H - col, h[k]);
+    }
+}
+
+// Every workgroup takes the rows blockIdx.x, blockIdx.x + gridDim.x, .. (four
+// at a time with one wave a row) and keeps its sum of dweight in registers.
+template <class T, int K, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_grad_kernel(gwtf_stage_norm_grad_t p, float *partial)
+{
+    __shared__ float red[2][WAVES];
+    __shared__ float sums[WAVES == 1 ? 4 * K * 512 : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int part = WAVES == 1 ? 0 : wave, mine = WAVES == 1 ? wave : 0;
+    const int64_t rows_at_once = WAVES == 1 ? 4 : 1;
+    const int H = int(p.hidden);
+    const T *weight = static_cast<const T *>(p.weight);
+    float w[K][8], dw[K][8];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int col = ((k * WAVES + part) * 64 + lane) * kVec;
+        load8(weight + col, H - col, w[k]);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) dw[k][i] = 0.f;
+    }
+    int turn = 0;
+    for (int64_t row = blockIdx.x * rows_at_once + mine; row < p.num_tokens;
+         row += gridDim.x * rows_at_once, turn ^= 1) {
+        const T *dy = static_cast<const T *>(p.dy) + row * p.dy_stride;
+        const T *hp = static_cast<const T *>(p.h) + row * p.h_stride;
+        const float rstd = p.rstd[row];
+        float g[K][8], xh[K][8], d[K][8], c = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int col = ((k * WAVES + part) * 64 + lane) * kVec;
+            load8(dy + col, H - col, g[k]);
+            load8(hp + col, H - col, xh[k]);
+            if (p.dh) {
+                load8(static_cast<const T *>(p.dh) + row * p.dh_stride + col, H - col, d[k]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) d[k][i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                xh[k][i] *= rstd;
+                dw[k][i] += g[k][i] * xh[k][i];
+                g[k][i] *= w[k][i];
+                c += g[k][i] * xh[k][i];
+            }
+        }
+        // two buffers in turn: a wave may be one row ahead of the slowest reader
+        c = group_sum<WAVES>(c, red[turn], part) / float(H);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int col = ((k * WAVES + part) * 64 + lane) * kVec;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) d[k][i] += rstd * (g[k][i] - xh[k][i] * c);
+            store8(static_cast<T *>(p.dx) + row * p.dx_stride + col, H - col, d[k]);
+        }
+    }
+    if (!partial) return;
+    float *out = partial + int64_t(blockIdx.x) * H;
+    if constexpr (WAVES == 1) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) sums[(wave * K + k) * 512 + lane * kVec + i] = dw[k][i];
+        }
+        __syncthreads();
+        for (int col = threadIdx.x; col < H; col += 256)
+            out[col] = (sums[col] + sums[K * 512 + col]) + (sums[2 * K * 512 + col] + sums[3 * K * 512 + col]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int col = ((k * WAVES + part) * 64 + lane) * kVec;
+            store8(out + col, H - col, dw[k]);
+        }
+    }
+}
+
+// dweight from the workgroups' sums: 16 columns a workgroup, 64 threads a
+// column, each over adjacent sums in order.
+__global__ __launch_bounds__(1024) void dweight_kernel(const float *partial, int groups, int H, float *dweight)
+{
+    __shared__ float red[64][17];
+    const int c = threadIdx.x & 15, g = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+    const int each = (groups + 63) / 64, g0 = g * each, g1 = g0 + each < groups ? g0 + each : groups;
+    float v = 0.f;
+    if (col < H)
+        for (int i = g0; i < g1; ++i) v += partial[int64_t(i) * H + col];
+    red[g][c] = v;
+    __syncthreads();
+    for (int half = 32; half > 0; half >>= 1) {
+        if (g < half) red[g][c] += red[g + half][c];
+        __syncthreads();
+    }
+    if (g == 0 && col < H) dweight[col] = red[0][c];
+}
+
+__global__ void zero_kernel(float *p, int64_t n)
+{
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i < n) p[i] = 0.f;
+}
+
+template <class T, int K, int WAVES>
+hipError_t run_norm(const gwtf_stage_norm_t &a, hipStream_t s)
+{
+    const int64_t rows = WAVES == 1 ? 4 : 1;
+    norm_kernel<T, K, WAVES><<<dim3(uint32_t((a.num_tokens + rows - 1) / rows)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <class T, int K, int WAVES>
+hipError_t run_norm_grad(const gwtf_stage_norm_grad_t &a, const StageWorkspace &w, hipStream_t s)
+{
+    const int64_t rows = WAVES == 1 ? 4 : 1;
+    int64_t groups = (a.num_tokens + rows - 1) / rows;
+    if (groups > kNormGradGroups) groups = kNormGradGroups;
+    norm_grad_kernel<T, K, WAVES>
+        <<<dim3(uint32_t(groups)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a, a.dweight ? w.dweight : nullptr);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.dweight) return e;
+    dweight_kernel<<<dim3(uint32_t((a.hidden + 15) / 16)), dim3(1024), 0, s>>>(w.dweight, int(groups), int(a.hidden), a.dweight);
+    return hipGetLastError();
+}
+
+// Waves and steps of a row by its width: 512 columns a wave and step.
+template <class T, class Fn>
+hipError_t by_width(int64_t H, Fn f)
+{
+    if (H <= 512) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+    if (H <= 1024) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
+    if (H <= 2048) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+    if (H <= 4096) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
+    if (H <= 8192) return f(std::integral_constant<int, 2>(), std::integral_constant<int, 8>());
+    return f(std::integral_constant<int, 2>(), std::integral_constant<int, 16>());
+}
+
+template <class T>
+hipError_t norm_typed(const gwtf_stage_norm_t &a, hipStream_t s)
+{
+    return by_width<T>(a.hidden, [&](auto k, auto w) { return run_norm<T, decltype(k)::value, decltype(w)::value>(a, s); });
+}
+template <class T>
+hipError_t norm_grad_typed(const gwtf_stage_norm_grad_t &a, const StageWorkspace &ws, hipStream_t s)
+{
+    return by_width<T>(a.hidden,
+                       [&](auto k, auto w) { return run_norm_grad<T, decltype(k)::value, decltype(w)::value>(a, ws, s); });
+}
+
+} // namespace
+
+hipError_t launch_norm(const gwtf_stage_norm_t &a, const StageWorkspace &, hipStream_t s)
+{
+    if (a.num_tokens == 0) return hipSuccess;
+    switch (a.type) {
+    case GWTF_TYPE_F32: return norm_typed<float>(a, s);
+    case GWTF_TYPE_F16: return norm_typed<f16_t>(a, s);
+    default: return norm_typed<bf16_t>(a, s);
+    }
+}
+
+hipError_t launch_norm_grad(const gwtf_stage_norm_grad_t &a, const StageWorkspace &w, hipStream_t s)
+{
+    if (a.num_tokens == 0) {
+        if (!a.dweight) return hipSuccess;
+        zero_kernel<<<dim3(uint32_t((a.hidden + 255) / 256)), dim3(256), 0, s>>>(a.dweight, a.hidden);
+        return hipGetLastError();
+    }
+    switch (a.type) {
+    case GWTF_TYPE_F32: return norm_grad_typed<float>(a, w, s);
+    case GWTF_TYPE_F16: return norm_grad_typed<f16_t>(a, w, s);
+    default: return norm_grad_typed<bf16_t>(a, w, s);
+    }
+}
+
+} // namespace gwtf
