@@ -2,10 +2,12 @@
 // (gwtf_stage_logprob), and the gradient (gwtf_stage_logprob_grad).
 //
 // One pass over a row with the running maximum m of each lane,
-//   s = sum e^(x - m)   and   t = sum e^(x - m) (x - m),
+//   s = sum e^(x - m)   and   t = sum e^(x - m) (x - m) / ln 2,
 // both rescaled when m grows; parts with different m join the same way.  Then
-//   lse = m + ln s,   entropy = ln s - t / s,
-// where every term of t has one sign, so nothing cancels.
+//   lse = m + ln s,   entropy = ln s - ln 2 * t / s,
+// where every term of t has one sign, so nothing cancels.  (x - m) log2 e as
+// one fused operation with m log2 e at hand would overflow for masks of the
+// type's lowest value.
 //
 // Alternatives: each wave keeps its largest entries as keys (order of the
 // value, then lower index) sorted over its lanes, and looks closer at a step
@@ -19,7 +21,7 @@ namespace {
 constexpr float kLowest = -200.f; // 2^-200 is 0: keeps 0 * -infinity out of t
 
 struct Softmax {
-    float m, s, t; // t in units of ln 2
+    float m, s, t;
 };
 
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -__builtin_inff() ? 0.f : m; }
@@ -67,32 +69,58 @@ __device__ __forceinline__ uint64_t key_of(int order, uint32_t index)
     return (uint64_t(uint32_t(order) ^ 0x80000000u) << 32) | (0xffffffffu - index);
 }
 
-// The wave's `top` largest keys, the j-th in lane j.
+__device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane)
+{
+    const uint32_t hi = __builtin_amdgcn_readlane(int(k >> 32), lane), lo = __builtin_amdgcn_readlane(int(uint32_t(k)), lane);
+    return (uint64_t(hi) << 32) | lo;
+}
+
+// The wave's `top` largest keys, the j-th in lane j, 0 in the other lanes.
+// Keys join by rank: every new key is compared with the others and with the
+// list in independent steps, where inserting them one after another is a
+// chain of some 400 cycles for each (seven rows of 131,072 with eight
+// alternatives: 96 us inserting, see the kernel for the present time).
 struct TopList {
-    uint64_t key;  // this lane's
-    int last;      // order of the last of them; lower than any value's while there are fewer
+    uint64_t key, last; // this lane's; the smallest that counts (uniform)
+    uint64_t *slots;    // `top` of this wave's, in LDS
     int top;
-    __device__ __forceinline__ void start(int k)
+    __device__ __forceinline__ void start(int k, uint64_t *lds)
     {
-        key = 0;
+        key = last = 0;
+        slots = lds;
         top = k;
-        last = -0x7fffffff - 1;
     }
-    __device__ __forceinline__ uint64_t key_at(int lane) const
+    __device__ __forceinline__ bool list_empty() const { return lane_key(key, 0) == 0; }
+    __device__ __forceinline__ int last_order() const { return int(uint32_t(last >> 32) ^ 0x80000000u); }
+    // Takes the keys of the lanes with key > last (`some`, not empty).
+    __device__ __forceinline__ void merge(uint64_t k, uint64_t some)
     {
-        const uint32_t hi = __builtin_amdgcn_readlane(int(key >> 32), lane);
-        const uint32_t lo = __builtin_amdgcn_readlane(int(uint32_t(key)), lane);
-        return (uint64_t(hi) << 32) | lo;
+        const int lane = __lane_id();
+        int rank = 0, mine = lane;
+        if (list_empty()) {
+            for (uint64_t m = some; m; m &= m - 1) rank += lane_key(k, __builtin_ctzll(m)) > k;
+            mine += __popcll(some);
+        } else {
+            for (uint64_t m = some; m; m &= m - 1) {
+                const uint64_t other = lane_key(k, __builtin_ctzll(m));
+                rank += other > k;
+                mine += other > key;
+            }
+            for (int j = 0; j < top; ++j) rank += lane_key(key, j) > k;
+        }
+        if ((some >> lane & 1) && rank < top) slots[rank] = k;
+        if (lane < top && mine < top) slots[mine] = key;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        key = lane < top ? slots[lane] : 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        last = lane_key(key, top - 1);
     }
-    __device__ __forceinline__ void insert(uint64_t k) // k is uniform
+    __device__ __forceinline__ void offer(uint64_t k)
     {
-        const int lane = __lane_id(), place = __popcll(__ballot(key > k));
-        const int hi = __builtin_amdgcn_update_dpp(0, int(key >> 32), 0x138, 0xf, 0xf, false); // from the lane below
-        const int lo = __builtin_amdgcn_update_dpp(0, int(uint32_t(key)), 0x138, 0xf, 0xf, false);
-        if (lane == place) key = k;
-        else if (lane > place) key = (uint64_t(uint32_t(hi)) << 32) | uint32_t(lo);
-        const uint64_t l = key_at(top - 1);
-        last = int(uint32_t(l >> 32) ^ 0x80000000u);
+        const uint64_t some = __ballot(k > last);
+        if (some) merge(k, some);
     }
 };
 
@@ -137,6 +165,20 @@ __device__ __forceinline__ void finish_row(const gwtf_stage_logprob_t &a, int64_
     }
 }
 
+// Words of a record that a workgroup of another XCD reads in the same launch:
+// written through to and read from memory, past the caches that the XCDs do
+// not share.
+__device__ __forceinline__ void put(uint32_t *p, uint32_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void put(uint64_t *p, uint64_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float get_float(const uint32_t *p)
+{
+    return __uint_as_float(__hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+__device__ __forceinline__ uint64_t get_key(const uint64_t *p)
+{
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
 template <class T, bool TOP>
 __global__ __launch_bounds__(kLpWaves * 64) void logprob_kernel(LogprobParams p)
 {
@@ -150,16 +192,16 @@ __global__ __launch_bounds__(kLpWaves * 64) void logprob_kernel(LogprobParams p)
     const T *x = static_cast<const T *>(a.logits) + row * a.logits_stride;
     Softmax r = {-__builtin_inff(), 0.f, 0.f};
     TopList list;
-    list.start(a.top);
+    list.start(a.top, keys + (TOP ? wave * GWTF_STAGE_MAX_TOP : 0));
     for (int64_t base = c0; base < c1; base += kStep) {
         const int64_t col = base + (wave * 64 + lane) * kVec;
         float v[16];
         load8(x + col, c1 - col, v, -__builtin_inff());
         load8(x + col + kStep / 2, c1 - col - kStep / 2, v + 8, -__builtin_inff());
-        float top = v[0];
+        float most = v[0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, v[i]);
-        const float m = fmaxf(r.m, top), ms = finite_or_zero(m);
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, v[i]);
+        const float m = fmaxf(r.m, most), ms = finite_or_zero(m);
         const float d0 = (r.m - ms) * kLog2e, e0 = exp2_(d0);
         r.t = e0 * (r.t + fmaxf(d0, kLowest) * r.s);
         r.s *= e0;
@@ -171,22 +213,29 @@ __global__ __launch_bounds__(kLpWaves * 64) void logprob_kernel(LogprobParams p)
             r.t += e * fmaxf(d, kLowest);
         }
         if constexpr (TOP) {
-            if (__ballot(order_of(top) > list.last)) {
+            // A wave goes up through its columns, so what only equals the
+            // last of the list in a later step has the higher index.
+            if (!__ballot(list.last == 0 || order_of(most) > list.last_order())) continue;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int64_t at = col + (i < 8 ? 0 : kStep / 2) + (i & 7);
-                    const int o = order_of(v[i]);
-                    const bool real = at < c1 && v[i] == v[i];
-                    uint64_t some = __ballot(real && o >= list.last);
-                    while (some) {
-                        const int l = __builtin_ctzll(some);
-                        some &= some - 1;
-                        const int ol = __builtin_amdgcn_readlane(o, l);
-                        // ties within a step come in any order: the whole key decides
-                        const uint64_t k = key_of(ol, uint32_t(__builtin_amdgcn_readlane(int(at), l)));
-                        if (k > list.key_at(a.top - 1)) list.insert(k);
-                    }
-                }
+            for (int i = 0; i < 16; ++i)
+                if (col + (i < 8 ? 0 : kStep / 2) + (i & 7) >= c1) v[i] = __builtin_nanf("");
+            // Each lane offers its largest entry that is left, the lowest
+            // index of equal ones, until none is above the list's last.
+            for (;;) {
+                float best = v[0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) best = fmaxf(best, v[i]); // the other one of a NaN
+                int slot = -1;
+#pragma unroll
+                for (int i = 15; i >= 0; --i) slot = v[i] == best ? i : slot;
+                const uint32_t at = uint32_t(col) + (slot < 8 ? 0 : kStep / 2) + (slot & 7);
+                const uint64_t k = slot < 0 ? 0 : key_of(order_of(best), at);
+                const uint64_t some = __ballot(k > list.last);
+                if (!some) break;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (slot == i) v[i] = __builtin_nanf("");
+                list.merge(k, some);
             }
         }
     }
@@ -199,50 +248,56 @@ __global__ __launch_bounds__(kLpWaves * 64) void logprob_kernel(LogprobParams p)
     if (wave == 0) {
         r = join(join(parts[0], parts[1]), join(parts[2], parts[3]));
         if constexpr (TOP) {
-            for (int w = 1; w < kLpWaves; ++w)
-                for (int j = 0; j < a.top; ++j) {
-                    const uint64_t k = keys[w * GWTF_STAGE_MAX_TOP + j];
-                    if (k <= list.key_at(a.top - 1)) break; // a wave's keys fall
-                    list.insert(k);
-                }
+            for (int w = 1; w < kLpWaves; ++w) list.offer(lane < a.top ? keys[w * GWTF_STAGE_MAX_TOP + lane] : 0);
         }
     }
     if (p.segments == 1) {
         if (wave == 0) finish_row<T>(a, row, r, list);
         return;
     }
-    // The workgroup that arrives last joins the row's records.
+    // The workgroup that arrives last joins the row's records.  Records and
+    // counter are words of agent scope; the wait puts a record in memory before
+    // its arrival is counted.  (A fence of agent scope would write back and
+    // drop the whole L2 of the XCD: 8 us on seven rows of 131,072.)
     unsigned char *record = p.records + int64_t(blockIdx.x) * kLogprobRecord;
     if (wave == 0) {
-        if (lane == 0) *reinterpret_cast<Softmax *>(record) = r;
-        if constexpr (TOP) {
-            if (lane < a.top) reinterpret_cast<uint64_t *>(record + 16)[lane] = list.key;
+        if (lane == 0) {
+            uint32_t *w = reinterpret_cast<uint32_t *>(record);
+            put(w, __float_as_uint(r.m));
+            put(w + 1, __float_as_uint(r.s));
+            put(w + 2, __float_as_uint(r.t));
         }
-        __threadfence();
-        if (lane == 0) last_one = atomicAdd(p.arrived + row, 1u) == uint32_t(p.segments - 1);
+        if constexpr (TOP) {
+            if (lane < a.top) put(reinterpret_cast<uint64_t *>(record + 16) + lane, list.key);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (lane == 0)
+            last_one = __hip_atomic_fetch_add(p.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                       uint32_t(p.segments - 1);
     }
     __syncthreads();
-    if (!last_one || wave != 0) return;
-    __threadfence();
+    if (!last_one) return;
     const unsigned char *first = p.records + row * p.segments * kLogprobRecord;
+    if constexpr (TOP) {
+        // all waves take parts of the keys, then the first one theirs
+        list.start(a.top, keys + wave * GWTF_STAGE_MAX_TOP);
+        const int all = p.segments * a.top;
+        for (int i0 = wave * 64; i0 < all; i0 += kLpWaves * 64) {
+            const int i = i0 + lane, seg = i / a.top;
+            list.offer(i < all ? get_key(reinterpret_cast<const uint64_t *>(first + seg * kLogprobRecord + 16) + (i - seg * a.top)) : 0);
+        }
+        if (lane < a.top) keys[wave * GWTF_STAGE_MAX_TOP + lane] = list.key;
+        __syncthreads();
+    }
+    if (wave != 0) return;
     r = {-__builtin_inff(), 0.f, 0.f};
-    for (int i = lane; i < p.segments; i += 64) r = join(r, *reinterpret_cast<const Softmax *>(first + i * kLogprobRecord));
+    for (int i = lane; i < p.segments; i += 64) {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(first + i * kLogprobRecord);
+        r = join(r, Softmax{get_float(w), get_float(w + 1), get_float(w + 2)});
+    }
     r = wave_join(r);
     if constexpr (TOP) {
-        list.start(a.top);
-        const int all = p.segments * a.top;
-        for (int i0 = 0; i0 < all; i0 += 64) {
-            const int i = i0 + lane, seg = i / a.top;
-            const uint64_t k = i < all ? reinterpret_cast<const uint64_t *>(first + seg * kLogprobRecord + 16)[i - seg * a.top] : 0;
-            uint64_t some = __ballot(k > list.key_at(a.top - 1));
-            while (some) {
-                const int l = __builtin_ctzll(some);
-                some &= some - 1;
-                const uint64_t kl = (uint64_t(uint32_t(__builtin_amdgcn_readlane(int(k >> 32), l))) << 32) |
-                                    uint32_t(__builtin_amdgcn_readlane(int(uint32_t(k)), l));
-                if (kl > list.key_at(a.top - 1)) list.insert(kl);
-            }
-        }
+        for (int w = 1; w < kLpWaves; ++w) list.offer(lane < a.top ? keys[w * GWTF_STAGE_MAX_TOP + lane] : 0);
     }
     finish_row<T>(a, row, r, list);
     if (lane == 0) p.arrived[row] = 0;
