@@ -180,6 +180,12 @@ class StageOps:
         self._tokens = {torch.int32: GWTF_TOKEN_I32, torch.int64: GWTF_TOKEN_I64}
         self._forms = {"none": GWTF_NORM_PLAIN, "row": GWTF_NORM_F8_ROW, "block": GWTF_NORM_F8_BLOCK}
         self._current = torch._C._cuda_getCurrentRawStream  # the current stream without an object for it
+        # a small call is bound by its host work: new tensors come from one at
+        # hand (1.4 us each, torch.empty with a device 1.6) and calls go to the
+        # library's functions directly
+        self._f32 = torch.empty(0, dtype=torch.float32, device=self._dev)
+        lib = _library()
+        self._calls = {name: getattr(lib, "gwtf_stage_" + name) for name in _CALLS}
         self.handle = gwtf_stage_create(max_tokens, max_hidden, max_vocab, device, self._raw)
 
     # ---- arguments ----
@@ -214,18 +220,17 @@ class StageOps:
             raise ValueError(f"{name}: need a contiguous vector on cuda:{self.device}")
         return t.data_ptr(), kind
 
-    def _new(self, shape, dtype):
-        return self.torch.empty(shape, dtype=dtype, device=self._dev)
-
-    def _run(self, call, args, tensors):
+    def _run(self, name, args, tensors):
         if self.handle is None:
             raise RuntimeError("StageOps: closed")
         if self._current(self.device) == self._raw:
-            call(self.handle, args)
+            code = self._calls[name](self.handle, args)
+            if code:
+                _check(code, self.handle)
             return
         here = self.torch.cuda.current_stream(self.device)
         self.stream.wait_stream(here)
-        call(self.handle, args)
+        _check(self._calls[name](self.handle, args), self.handle)
         here.wait_stream(self.stream)
         for t in tensors:
             if t is not None:
@@ -239,10 +244,10 @@ class StageOps:
         ids, idk = self._ids(tokens, "tokens")
         n, (v, h) = tokens.shape[0], table.shape
         if out is None:
-            out = self._new((n, h), table.dtype)
+            out = table.new_empty((n, h))
         a = gwtf_stage_embed_t(n, h, v, kind, idk, scale, ids, *self._mat(table, table.shape, table.dtype, "table"),
                                *self._mat(out, (n, h), table.dtype, "out"))
-        self._run(gwtf_stage_embed, a, (tokens, table, out))
+        self._run("embed", a, (tokens, table, out))
         return out
 
     def embed_grad(self, tokens, dout, vocab: int, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False):
@@ -255,13 +260,13 @@ class StageOps:
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs an existing out tensor")
-            out = self._new((vocab, h), dout.dtype if dtype is None else dtype)
+            out = dout.new_empty((vocab, h), dtype=dtype)
         elif dtype is not None and out.dtype != dtype:
             raise ValueError(f"out: {out.dtype} is not the dtype asked for, {dtype}")
         a = gwtf_stage_embed_grad_t(n, h, vocab, kind, self._type(out, "out"), idk, bool(accumulate), scale, ids,
                                     *self._mat(dout, (n, h), dout.dtype, "dout"),
                                     *self._mat(out, (vocab, h), out.dtype, "out"))
-        self._run(gwtf_stage_embed_grad, a, (tokens, dout, out))
+        self._run("embed_grad", a, (tokens, dout, out))
         return out
 
     # ---- dropout ----
@@ -275,13 +280,13 @@ class StageOps:
             raise ValueError("seed must fit in 64 bits and site in 32, both >= 0")
         shape, dt = x.shape, x.dtype
         if out is None:
-            out = self._new(shape, dt)
+            out = x.new_empty(shape)
         a = gwtf_stage_dropout_t(shape[0], shape[1], kind, site, seed, p,
                                  None if rows is None else self._vec(rows, shape[0], self.torch.int64, "rows"),
                                  *self._mat(x, shape, dt, "x"),
                                  *((None, 0) if residual is None else self._mat(residual, shape, dt, "residual")),
                                  *self._mat(out, shape, dt, "out"))
-        self._run(gwtf_stage_dropout, a, (x, rows, residual, out))
+        self._run("dropout", a, (x, rows, residual, out))
         return out
 
     # ---- hand-off ----
@@ -299,18 +304,21 @@ class StageOps:
         groups = (n, 1 if form == GWTF_NORM_F8_ROW else -(-h // GWTF_NORM_BLOCK))
         f32, ydt = torch.float32, torch.float8_e4m3fn if form else dt
         if out is None:
-            out = (self._new(shape, ydt), self._new(groups, f32) if form else None,
-                   None if residual is None else self._new(shape, dt), self._new((n,), f32))
+            new = self._f32.new_empty
+            out = (new(shape, dtype=ydt), new(groups) if form else None,
+                   None if residual is None else x.new_empty(shape), new((n,)))
         y, scales, hout, rstd = out
-        if form and (self._mat(scales, groups, f32, "scales") and not scales.is_contiguous()):
-            raise ValueError("scales: must be contiguous")
+        if form:
+            sc = self._mat(scales, groups, f32, "scales")[0]
+            if not scales.is_contiguous():
+                raise ValueError("scales: must be contiguous")
         a = gwtf_stage_norm_t(n, h, kind, form, eps, *self._mat(x, shape, dt, "x"),
                               *((None, 0) if residual is None else self._mat(residual, shape, dt, "residual")),
                               self._vec(weight, h, dt, "weight"), *self._mat(y, shape, ydt, "y"),
                               *((None, 0) if hout is None else self._mat(hout, shape, dt, "h")),
-                              scales.data_ptr() if form else None,
+                              sc if form else None,
                               None if rstd is None else self._vec(rstd, n, f32, "rstd"))
-        self._run(gwtf_stage_norm, a, (x, residual, weight, y, scales, hout, rstd))
+        self._run("norm", a, (x, residual, weight, y, scales, hout, rstd))
         return out
 
     def norm_grad(self, dy, h, weight, rstd, dh=None, out=None):
@@ -320,7 +328,7 @@ class StageOps:
         kind = self._type(h, "h")
         shape, dt, f32 = h.shape, h.dtype, self.torch.float32
         if out is None:
-            out = (self._new(shape, dt), self._new((shape[1],), f32))
+            out = (h.new_empty(shape), self._f32.new_empty((shape[1],)))
         dx, dw = out
         a = gwtf_stage_norm_grad_t(shape[0], shape[1], kind, *self._mat(dy, shape, dt, "dy"),
                                    *self._mat(h, shape, dt, "h"),
@@ -328,7 +336,7 @@ class StageOps:
                                    self._vec(weight, shape[1], dt, "weight"), self._vec(rstd, shape[0], f32, "rstd"),
                                    *self._mat(dx, shape, dt, "dx"),
                                    None if dw is None else self._vec(dw, shape[1], f32, "dweight"))
-        self._run(gwtf_stage_norm_grad, a, (dy, h, dh, weight, rstd, dx, dw))
+        self._run("norm_grad", a, (dy, h, dh, weight, rstd, dx, dw))
         return out
 
     # ---- the data node's last stage ----
@@ -339,22 +347,22 @@ class StageOps:
         logarithm of its sum of exponentials, and the ``top`` most likely
         tokens, equal ones by ascending index (None with top == 0)."""
         torch, kind = self.torch, self._type(logits, "logits")
-        shape, f32 = logits.shape, torch.float32
+        shape, new = logits.shape, self._f32.new_empty
         n, v = shape
         ids, idk, logp = None, 0, None
         if targets is not None:
             ids, idk = self._ids(targets, "targets")
             if targets.shape[0] != n:
                 raise ValueError(f"targets: need {n} of them")
-            logp = self._new((n,), f32)
-        entropy, lse = self._new((n,), f32), self._new((n,), f32)
+            logp = new((n,))
+        entropy, lse = new((n,)), new((n,))
         top_logp = top_ids = None
         if top:
-            top_logp, top_ids = self._new((n, top), f32), self._new((n, top), torch.int32)
+            top_logp, top_ids = new((n, top)), new((n, top), dtype=torch.int32)
         a = gwtf_stage_logprob_t(n, v, kind, idk, top, *self._mat(logits, shape, logits.dtype, "logits"), ids,
                                  logp.data_ptr() if logp is not None else None, entropy.data_ptr(), lse.data_ptr(),
                                  top_logp.data_ptr() if top else None, top_ids.data_ptr() if top else None)
-        self._run(gwtf_stage_logprob, a, (logits, targets, logp, entropy, lse, top_logp, top_ids))
+        self._run("logprob", a, (logits, targets, logp, entropy, lse, top_logp, top_ids))
         return logp, entropy, lse, top_logp, top_ids
 
     def logprob_grad(self, logits, targets, lse, entropy=None, dlogp=None, dentropy=None, out=None):
@@ -374,14 +382,14 @@ class StageOps:
         if dentropy is not None and entropy is None:
             raise ValueError("dentropy needs entropy")
         if out is None:
-            out = self._new(shape, dt)
+            out = logits.new_empty(shape)
         a = gwtf_stage_logprob_grad_t(n, v, kind, idk, *self._mat(logits, shape, dt, "logits"), ids,
                                       self._vec(lse, n, f32, "lse"),
                                       None if dentropy is None else self._vec(entropy, n, f32, "entropy"),
                                       None if dlogp is None else self._vec(dlogp, n, f32, "dlogp"),
                                       None if dentropy is None else self._vec(dentropy, n, f32, "dentropy"),
                                       *self._mat(out, shape, dt, "out"))
-        self._run(gwtf_stage_logprob_grad, a, (logits, targets, lse, entropy, dlogp, dentropy, out))
+        self._run("logprob_grad", a, (logits, targets, lse, entropy, dlogp, dentropy, out))
         return out
 
     def close(self):
