@@ -34,6 +34,22 @@ __device__ __forceinline__ void load8(const T *p, int64_t n, float v[8], float f
     }
 }
 
+// The same as they lie in memory, for reads that are to be in flight for long;
+// columns from n on are 0.
+template <class T>
+__device__ __forceinline__ typename Vec8<T>::type load8_raw(const T *p, int64_t n)
+{
+    typename Vec8<T>::type v = {};
+    if (n >= kVec) {
+        v = *reinterpret_cast<const typename Vec8<T>::type *>(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (i < n) v[i] = p[i];
+    }
+    return v;
+}
+
 template <class T>
 __device__ __forceinline__ void store8(T *p, int64_t n, const float v[8])
 {

@@ -45,66 +45,221 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p)
     store8(static_cast<T *>(p.a.out) + row * p.a.out_stride + col, n, v);
 }
 
+// ---- zeros for the rows of absent tokens ----
+//
+// Most of the gradient's bytes are zeros that depend on nothing but which
+// tokens are there, so they are written beside the sorting, whose few
+// workgroups leave the memory idle: each of kFillGroups workgroups looks
+// through all tokens for those of its own rows.
+
+constexpr int kFillGroups = 512;
+constexpr int kFillRows = 4096;           // most rows of one workgroup
+constexpr int64_t kFillTokens = 32768;    // with more tokens a look through them costs more than the sort hides:
+                                          // then embed_grad_kernel writes the zeros
+
+struct FillParams {
+    void *grad;
+    int64_t stride, hidden;
+    const void *tokens;
+    int64_t N, v0, v1; // rows [v0, v1)
+    int32_t token_type, wide; // wide: 32-bit gradient
+    int32_t rows;      // of one workgroup
+};
+
+__device__ __forceinline__ void zero_row(char *g, int64_t bytes)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+    const u32x4 z = {0, 0, 0, 0};
+    for (int64_t at = (threadIdx.x & 63) * 16; at < bytes; at += 64 * 16) {
+        if (at + 16 <= bytes) {
+            *reinterpret_cast<u32x4 *>(g + at) = z;
+        } else {
+            for (int64_t i = at; i < bytes; i += 2) *reinterpret_cast<uint16_t *>(g + i) = 0;
+        }
+    }
+}
+
+template <int THREADS>
+__device__ void fill_absent(const FillParams &p, int group, uint32_t *there /* [kFillRows / 32] */)
+{
+    const int64_t first = p.v0 + int64_t(group) * p.rows;
+    const int rows = int(p.v1 - first < p.rows ? p.v1 - first : p.rows);
+    for (int i = threadIdx.x; i < (p.rows + 31) / 32; i += THREADS) there[i] = 0;
+    __syncthreads();
+    for (int64_t i = threadIdx.x; i < p.N; i += 8 * THREADS) {
+        int64_t t[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) t[q] = i + q * THREADS < p.N ? load_token(p.tokens, p.token_type, i + q * THREADS) : -1;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const uint64_t r = uint64_t(t[q] - first);
+            if (t[q] >= 0 && r < uint64_t(rows)) atomicOr(&there[r >> 5], 1u << (r & 31));
+        }
+    }
+    __syncthreads();
+    const int64_t size = p.wide ? 4 : 2;
+    for (int r = threadIdx.x >> 6; r < rows; r += THREADS / 64)
+        if (!(there[r >> 5] >> (r & 31) & 1))
+            zero_row(static_cast<char *>(p.grad) + (first + r) * p.stride * size, p.hidden * size);
+}
+
 // ---- sorting tokens ----
 //
 // Keys token << 32 | position are all different, so any sort is stable.  One
-// workgroup sorts kSortBlock of them in LDS (bitonic); up to kMergeWays sorted
-// blocks are merged in one launch, where each key finds its place by a binary
-// search in every other block.
+// workgroup sorts kSortBlock of them (bitonic), two adjacent keys a thread:
+// exchanges over up to 64 keys stay within a thread or a wave, only those over
+// more, 10 of 66, go through LDS with a barrier (5 us a block; 15 us with all
+// in LDS).  Up to kMergeWays sorted blocks are merged in one launch, where each
+// key finds its place by a binary search in every other block.  Workgroups
+// after the sorting ones write zeros.
 
 constexpr int kSortBlock = 2048;
 constexpr int kMergeWays = 32;
 
-__global__ __launch_bounds__(1024) void sort_block_kernel(const void *tokens, int token_type, int64_t vocab, int64_t N,
-                                                          uint64_t *out)
+// The value of lane ^ x.
+template <int x>
+__device__ __forceinline__ int lane_xor(int v)
 {
-    __shared__ uint64_t key[kSortBlock];
-    const int64_t base = int64_t(blockIdx.x) * kSortBlock;
-    for (int i = threadIdx.x; i < kSortBlock; i += 1024) {
-        const int64_t pos = base + i;
-        uint64_t k = ~uint64_t(0);
-        if (pos < N) {
-            const int64_t t = load_token(tokens, token_type, pos);
-            k = (uint64_t(t >= 0 && t < vocab ? uint32_t(t) : 0xffffffffu) << 32) | uint32_t(pos);
-        }
-        key[i] = k;
-    }
-    __syncthreads();
-    for (int size = 2; size <= kSortBlock; size <<= 1) {
-        for (int j = size >> 1; j > 0; j >>= 1) {
-            const int t = threadIdx.x, i = 2 * t - (t & (j - 1)), l = i + j;
-            const uint64_t a = key[i], b = key[l];
-            if ((a > b) == ((i & size) == 0)) {
-                key[i] = b;
-                key[l] = a;
-            }
-            __syncthreads();
-        }
-    }
-    for (int i = threadIdx.x; i < kSortBlock; i += 1024)
-        if (base + i < N) out[base + i] = key[i];
+    if constexpr (x == 1) return __builtin_amdgcn_update_dpp(v, v, 0xB1, 0xf, 0xf, false);      // quad 1 0 3 2
+    else if constexpr (x == 2) return __builtin_amdgcn_update_dpp(v, v, 0x4E, 0xf, 0xf, false); // quad 2 3 0 1
+    else if constexpr (x == 8) return row_ror<8>(v);
+    else return __shfl_xor(v, x);
+}
+template <int x>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) { return uint32_t(lane_xor<x>(int(v))); }
+template <int x>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v)
+{
+    return (uint64_t(uint32_t(lane_xor<x>(int(v >> 32)))) << 32) | uint32_t(lane_xor<x>(int(uint32_t(v))));
+}
+template <class K>
+__device__ __forceinline__ K lower(K a, K b) { return a < b ? a : b; }
+template <class K>
+__device__ __forceinline__ K higher(K a, K b) { return a < b ? b : a; }
+
+// Exchange of keys i and i ^ (2 x) between lanes; `up`: the run is ascending.
+template <int x, class K>
+__device__ __forceinline__ void exchange(K &a, K &b, int lane, bool up)
+{
+    const K pa = lane_xor<x>(a), pb = lane_xor<x>(b);
+    const bool low = ((lane & x) == 0) == up;
+    a = low ? lower(pa, a) : higher(pa, a);
+    b = low ? lower(pb, b) : higher(pb, b);
 }
 
-// Merges groups of kMergeWays sorted blocks of `len` keys.
-__global__ __launch_bounds__(256) void merge_kernel(const uint64_t *in, int64_t N, int64_t len, uint64_t *out)
+// K: 32 bits, token << 11 | index in the block, where tokens have at most 21
+// bits (the sort is bound by its vector instructions, a third of those for 64
+// bits), else 64.
+template <class K>
+__global__ __launch_bounds__(1024) void sort_block_kernel(const void *tokens, int token_type, int64_t vocab, int64_t N,
+                                                          uint64_t *out, uint32_t blocks, FillParams f)
 {
-    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= N) return;
-    const uint64_t k = in[i];
-    const int64_t own = i / len, group0 = own / kMergeWays * kMergeWays;
-    int64_t place = group0 * len + (i - own * len);
-    for (int64_t b = group0; b < group0 + kMergeWays && b * len < N; ++b) {
-        if (b == own) continue;
-        int64_t lo = b * len, hi = lo + len < N ? lo + len : N;
-        const int64_t first = lo;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (in[mid] < k) lo = mid + 1;
-            else hi = mid;
-        }
-        place += lo - first;
+    __shared__ K key[2][kSortBlock];
+    if (blockIdx.x >= blocks) {
+        fill_absent<1024>(f, int(blockIdx.x - blocks), reinterpret_cast<uint32_t *>(key));
+        return;
     }
-    out[place] = k;
+    constexpr int kShift = sizeof(K) == 4 ? 11 : 32;
+    const int64_t base = int64_t(blockIdx.x) * kSortBlock;
+    const int t = threadIdx.x, lane = t & 63;
+    K k[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int64_t pos = base + 2 * t + i;
+        const int64_t tok = pos < N ? load_token(tokens, token_type, pos) : -1;
+        // absent and padding come after all tokens, in order of their position
+        k[i] = (K(tok >= 0 && tok < vocab ? tok : vocab) << kShift) | K(2 * t + i);
+    }
+    int turn = 0;
+#pragma unroll
+    for (int size = 2; size <= kSortBlock; size <<= 1) {
+        const bool up = ((2 * t) & size) == 0;
+        // over more than a wave: partner thread t ^ (j / 2); two buffers, so
+        // that one barrier is enough
+        for (int j = size >> 1; j >= 128; j >>= 1, turn ^= 1) {
+            key[turn][2 * t] = k[0];
+            key[turn][2 * t + 1] = k[1];
+            __syncthreads();
+            const int other = 2 * (t ^ (j >> 1));
+            const K pa = key[turn][other], pb = key[turn][other + 1];
+            const bool low = ((2 * t & j) == 0) == up;
+            k[0] = low ? lower(pa, k[0]) : higher(pa, k[0]);
+            k[1] = low ? lower(pb, k[1]) : higher(pb, k[1]);
+        }
+        if (size >= 128) exchange<32>(k[0], k[1], lane, up);
+        if (size >= 64) exchange<16>(k[0], k[1], lane, up);
+        if (size >= 32) exchange<8>(k[0], k[1], lane, up);
+        if (size >= 16) exchange<4>(k[0], k[1], lane, up);
+        if (size >= 8) exchange<2>(k[0], k[1], lane, up);
+        if (size >= 4) exchange<1>(k[0], k[1], lane, up);
+        const K lo = lower(k[0], k[1]), hi = higher(k[0], k[1]);
+        k[0] = up ? lo : hi;
+        k[1] = up ? hi : lo;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (base + 2 * t + i >= N) continue;
+        const int64_t tok = int64_t(k[i] >> kShift);
+        out[base + 2 * t + i] = (uint64_t(tok < vocab ? uint32_t(tok) : 0xffffffffu) << 32) |
+                                uint32_t(base + int64_t(k[i] & K(kSortBlock - 1)));
+    }
+}
+
+// Merges groups of kMergeWays sorted blocks of `len` (a power of two) keys.  A
+// search is a chain of dependent reads, so every `1 << shift`-th key of the
+// group is put into LDS first and only its last steps go to memory (16,384
+// tokens: one cache line).  Four lanes share a key, each with up to eight
+// searches side by side.
+constexpr int kSamples = 4096;
+constexpr int kMergeThreads = 1024;
+constexpr int kMergeKeys = kMergeThreads / 4;
+constexpr int kSearches = kMergeWays / 4;
+
+__global__ __launch_bounds__(kMergeThreads) void merge_kernel(const uint64_t *in, uint32_t N, uint32_t len, int shift,
+                                                              uint64_t *out, uint32_t blocks, FillParams f)
+{
+    __shared__ uint64_t sample[kSamples];
+    if (blockIdx.x >= blocks) {
+        fill_absent<kMergeThreads>(f, int(blockIdx.x - blocks), reinterpret_cast<uint32_t *>(sample));
+        return;
+    }
+    // a workgroup's adjacent keys lie within one block, as len is a multiple of
+    // their number; offsets below are within the group of blocks
+    const uint32_t i0 = blockIdx.x * uint32_t(kMergeKeys), own = i0 / len, group0 = own / kMergeWays * kMergeWays;
+    const int64_t start = int64_t(group0) * len;
+    const uint64_t *const g = in + start;
+    const uint32_t total = uint32_t(N - start < int64_t(len) * kMergeWays ? N - start : int64_t(len) * kMergeWays);
+    for (uint32_t q = threadIdx.x; q < total >> shift; q += kMergeThreads) sample[q] = g[((q + 1) << shift) - 1];
+    const uint32_t i = uint32_t(i0 + threadIdx.x / 4 - start), part = threadIdx.x & 3;
+    const uint64_t k = i < total ? g[i] : 0;
+    __syncthreads();
+    uint32_t lo[kSearches], end[kSearches];
+#pragma unroll
+    for (int q = 0; q < kSearches; ++q) {
+        const uint32_t b = part + 4 * q, first = b * len;
+        lo[q] = first;
+        end[q] = b == own - group0 || first >= total ? first : (first + len < total ? first + len : total);
+    }
+    uint32_t step = len;
+    for (; step >= 1u << shift; step >>= 1) {
+#pragma unroll
+        for (int q = 0; q < kSearches; ++q)
+            if (lo[q] + step <= end[q] && sample[((lo[q] + step) >> shift) - 1] < k) lo[q] += step;
+    }
+    for (; step > 0; step >>= 1) {
+        uint64_t v[kSearches];
+#pragma unroll
+        for (int q = 0; q < kSearches; ++q) v[q] = lo[q] + step <= end[q] ? g[lo[q] + step - 1] : ~uint64_t(0);
+#pragma unroll
+        for (int q = 0; q < kSearches; ++q)
+            if (v[q] < k) lo[q] += step;
+    }
+    int place = 0;
+#pragma unroll
+    for (int q = 0; q < kSearches; ++q) place += int(lo[q] - (part + 4 * q) * len);
+    place += lane_xor<1>(place);
+    place += lane_xor<2>(place);
+    if (part == 0 && i < total) out[start + place + (i - (own - group0) * len)] = k;
 }
 
 // ---- sums ----
@@ -118,7 +273,9 @@ struct EmbedGradParams {
     int64_t fill_block;       // first workgroup that writes zeros
 };
 
-constexpr int kFillRows = 16; // rows of the table a wave looks at for zeros
+constexpr int kSearchRows = 16; // rows of the table a wave looks up for zeros
+constexpr int kRowsInFlight = 8;
+constexpr int kPartsInFlight = 16; // a run of one token over all chunks: 512 sums, one after another
 
 __device__ __forceinline__ uint32_t key_token(uint64_t k) { return uint32_t(k >> 32); }
 
@@ -137,18 +294,79 @@ __device__ __forceinline__ void write_grad(const gwtf_stage_embed_grad_t &a, int
     store8(g, n, v);
 }
 
+// One chunk and slab.  FULL: the slab has all of its 512 columns, so that
+// reads stand side by side with no branch between them.  Lane l holds the key
+// of entry l of 64; two batches of rows are in flight.
+template <class T, class G, bool FULL>
+__device__ __forceinline__ void sum_chunk(const EmbedGradParams &p, int64_t c, int64_t slab_col, int lane)
+{
+    const gwtf_stage_embed_grad_t &a = p.a;
+    constexpr int U = kRowsInFlight * 2 / int(sizeof(T));
+    const int64_t N = a.num_tokens, col = slab_col + lane * kVec, n = FULL ? kVec : a.hidden - col;
+    const int64_t e0 = c * p.chunk, e1 = e0 + p.chunk < N ? e0 + p.chunk : N;
+    const T *dout = static_cast<const T *>(a.dout) + col;
+    // tokens just outside the chunk, with the keys of its first entries
+    const uint64_t before_key = e0 > 0 ? p.sorted[e0 - 1] : ~uint64_t(0), after_key = e1 < N ? p.sorted[e1] : ~uint64_t(0);
+    uint64_t mine = p.sorted[e0 + lane < e1 ? e0 + lane : e1 - 1];
+    uint32_t token = __builtin_amdgcn_readfirstlane(key_token(mine));
+    if (token == 0xffffffffu) return;
+    bool before = __builtin_amdgcn_readfirstlane(key_token(before_key)) == token; // the run began in an earlier chunk
+    const uint32_t after_token = __builtin_amdgcn_readfirstlane(key_token(after_key));
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    typename Vec8<T>::type v[U], vn[U];
+    for (int64_t eb = e0; eb < e1; eb += 64) {
+        if (eb > e0) mine = p.sorted[eb + lane < e1 ? eb + lane : e1 - 1];
+        const int count = int(e1 - eb < 64 ? e1 - eb : 64);
+        auto fetch = [&](int at, typename Vec8<T>::type (&row)[U]) {
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                const uint32_t pos = __builtin_amdgcn_readlane(int(uint32_t(mine)), (at + q) & 63); // entries past the end read the last row
+                const T *r = dout + int64_t(pos) * a.dout_stride;
+                if constexpr (FULL) row[q] = *reinterpret_cast<const typename Vec8<T>::type *>(r);
+                else row[q] = load8_raw(r, n);
+            }
+        };
+        fetch(0, v);
+        for (int at = 0; at < count; at += U) {
+            if (at + U < count) fetch(at + U, vn); // the next rows, in flight while these are added
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                if (at + q >= count) break;
+                const uint32_t t = __builtin_amdgcn_readlane(int(key_token(mine)), at + q);
+                if (t != token) {
+                    if (before) store8(p.partial + (c * 2) * a.hidden + col, n, acc);
+                    else write_grad<G>(a, token, col, n, acc);
+                    if (t == 0xffffffffu) return;
+                    before = false;
+                    token = t;
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) acc[i] = 0.f;
+                }
+                const f32x8 f = __builtin_convertvector(v[q], f32x8);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) acc[i] += f[i];
+            }
+#pragma unroll
+            for (int q = 0; q < U; ++q) v[q] = vn[q];
+        }
+    }
+    if (before) store8(p.partial + (c * 2) * a.hidden + col, n, acc);
+    else if (after_token == token) store8(p.partial + (c * 2 + 1) * a.hidden + col, n, acc);
+    else write_grad<G>(a, token, col, n, acc);
+}
+
 template <class T, class G>
 __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradParams p)
 {
     const gwtf_stage_embed_grad_t &a = p.a;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t N = a.num_tokens;
     if (blockIdx.x >= p.fill_block) {
         // zeros for the rows whose token is absent
-        const int64_t v0 = ((blockIdx.x - p.fill_block) * 4 + (threadIdx.x >> 6)) * int64_t(kFillRows);
+        const int64_t v0 = ((blockIdx.x - p.fill_block) * 4 + wave) * int64_t(kSearchRows);
         if (v0 >= a.vocab) return;
         bool absent = false;
-        if (lane < kFillRows && v0 + lane < a.vocab) {
+        if (lane < kSearchRows && v0 + lane < a.vocab) {
             const uint64_t k = uint64_t(v0 + lane) << 32;
             int64_t lo = 0, hi = N;
             while (lo < hi) {
@@ -159,46 +377,17 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradParams p)
             absent = lo == N || key_token(p.sorted[lo]) != uint32_t(v0 + lane);
         }
         uint64_t rows = __ballot(absent);
-        const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         while (rows) {
             const int r = __builtin_ctzll(rows);
             rows &= rows - 1;
-            G *g = static_cast<G *>(a.grad) + (v0 + r) * a.grad_stride;
-            for (int64_t col = lane * kVec; col < a.hidden; col += 64 * kVec) store8(g + col, a.hidden - col, zero);
+            zero_row(static_cast<char *>(a.grad) + (v0 + r) * a.grad_stride * int64_t(sizeof(G)), a.hidden * int64_t(sizeof(G)));
         }
         return;
     }
-    const int64_t item = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    const int64_t c = item / p.slabs;
+    const int64_t item = int64_t(blockIdx.x) * 4 + wave, c = item / p.slabs, slab_col = (item - c * p.slabs) * 512;
     if (c >= p.chunks) return;
-    const int64_t col = (item - c * p.slabs) * 512 + lane * kVec, n = a.hidden - col;
-    const int64_t e0 = c * p.chunk, e1 = e0 + p.chunk < N ? e0 + p.chunk : N;
-    const T *dout = static_cast<const T *>(a.dout) + col;
-    uint32_t token = key_token(p.sorted[e0]);
-    if (token == 0xffffffffu) return;
-    bool before = e0 > 0 && key_token(p.sorted[e0 - 1]) == token; // the run began in an earlier chunk
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int64_t e = e0; e < e1; ++e) {
-        const uint64_t k = p.sorted[e];
-        const uint32_t t = key_token(k);
-        if (t != token) {
-            if (before) store8(p.partial + (c * 2) * a.hidden + col, n, acc);
-            else write_grad<G>(a, token, col, n, acc);
-            if (t == 0xffffffffu) return;
-            before = false;
-            token = t;
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) acc[i] = 0.f;
-        }
-        float v[8];
-        load8(dout + int64_t(uint32_t(k)) * a.dout_stride, n, v);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) acc[i] += v[i];
-    }
-    const bool after = e1 < N && key_token(p.sorted[e1]) == token;
-    if (before) store8(p.partial + (c * 2) * a.hidden + col, n, acc);
-    else if (after) store8(p.partial + (c * 2 + 1) * a.hidden + col, n, acc);
-    else write_grad<G>(a, token, col, n, acc);
+    if (slab_col + 512 <= a.hidden) sum_chunk<T, G, true>(p, c, slab_col, lane);
+    else sum_chunk<T, G, false>(p, c, slab_col, lane);
 }
 
 // Runs that cross chunks, each by the wave of the chunk in which it begins.
@@ -206,21 +395,48 @@ template <class G>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradParams p)
 {
     const gwtf_stage_embed_grad_t &a = p.a;
-    const int lane = threadIdx.x & 63;
-    const int64_t item = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item = int64_t(blockIdx.x) * 4 + wave;
     const int64_t c = item / p.slabs, N = a.num_tokens;
     const int64_t e0 = c * p.chunk, e1 = e0 + p.chunk;
     if (c >= p.chunks || e1 >= N) return;
-    const uint32_t token = key_token(p.sorted[e1 - 1]);
-    if (token == 0xffffffffu || key_token(p.sorted[e1]) != token) return; // no run goes on
-    if (key_token(p.sorted[e0]) == token && e0 > 0 && key_token(p.sorted[e0 - 1]) == token) return; // began earlier
-    const int64_t col = (item - c * p.slabs) * 512 + lane * kVec, n = a.hidden - col;
-    float acc[8], v[8];
+    const uint32_t first = key_token(p.sorted[e0]), token = key_token(p.sorted[e1 - 1]), next = key_token(p.sorted[e1]);
+    const uint32_t previous = e0 > 0 ? key_token(p.sorted[e0 - 1]) : 0xffffffffu;
+    if (token == 0xffffffffu || next != token) return; // no run goes on
+    if (first == token && previous == token) return;   // it began earlier
+    // chunks after this one that begin with the token, 64 looked at together
+    int64_t more = 0;
+    for (;;) {
+        const int64_t d = c + 1 + more + lane;
+        const uint64_t there = __ballot(d < p.chunks && key_token(p.sorted[d * p.chunk]) == token);
+        const int run = there == ~uint64_t(0) ? 64 : __builtin_ctzll(~there);
+        more += run;
+        if (run < 64) break;
+    }
+    const int64_t slab_col = (item - c * p.slabs) * 512, col = slab_col + lane * kVec, n = a.hidden - col;
+    if (n <= 0) return;
+    float acc[8];
     load8(p.partial + (c * 2 + 1) * a.hidden + col, n, acc);
-    for (int64_t d = c + 1; d < p.chunks && key_token(p.sorted[d * p.chunk]) == token; ++d) {
-        load8(p.partial + (d * 2) * a.hidden + col, n, v);
+    const float *next_part = p.partial + (c + 1) * 2 * a.hidden + col;
+    if (slab_col + 512 <= a.hidden) {
+        for (int64_t d = 0; d < more; d += kPartsInFlight) {
+            Vec8<float>::type v[kPartsInFlight];
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) acc[i] += v[i];
+            for (int q = 0; q < kPartsInFlight; ++q)
+                v[q] = *reinterpret_cast<const Vec8<float>::type *>(next_part + (d + q < more ? d + q : more - 1) * 2 * a.hidden);
+#pragma unroll
+            for (int q = 0; q < kPartsInFlight; ++q) {
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) acc[i] += d + q < more ? v[q][i] : 0.f;
+            }
+        }
+    } else {
+        for (int64_t d = 0; d < more; ++d) {
+            float v[8];
+            load8(next_part + d * 2 * a.hidden, n, v);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) acc[i] += v[i];
+        }
     }
     write_grad<G>(a, token, col, n, acc);
 }
@@ -263,13 +479,30 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
     p.chunk = chunk_of(N, a.hidden);
     p.chunks = (N + p.chunk - 1) / p.chunk;
     p.slabs = int(slabs_of(a.hidden));
+    // zeros beside the sort, half of them beside the merge where there is one
+    const bool beside = !a.accumulate && N > 0 && N <= kFillTokens;
+    FillParams f{a.grad, a.grad_stride, a.hidden, a.tokens, N, 0, 0, a.token_type, a.grad_type == GWTF_TYPE_F32, 1};
+    auto fill_groups = [&](int64_t v0, int64_t v1) -> uint32_t {
+        f.v0 = v0;
+        f.v1 = v1;
+        const int64_t rows = (v1 - v0 + kFillGroups - 1) / kFillGroups;
+        f.rows = int(rows < 1 ? 1 : rows > kFillRows ? kFillRows : rows);
+        return uint32_t((v1 - v0 + f.rows - 1) / f.rows);
+    };
     if (N > 0) {
-        sort_block_kernel<<<dim3(uint32_t((N + kSortBlock - 1) / kSortBlock)), dim3(1024), 0, s>>>(
-            a.tokens, a.token_type, a.vocab, N, w.sort_a);
+        uint32_t blocks = uint32_t((N + kSortBlock - 1) / kSortBlock);
+        const int64_t half = !beside ? 0 : N > kSortBlock ? a.vocab / 2 : a.vocab;
+        uint32_t fill = fill_groups(0, half);
+        auto sort = a.vocab < int64_t(1) << 21 ? sort_block_kernel<uint32_t> : sort_block_kernel<uint64_t>;
+        sort<<<dim3(blocks + fill), dim3(1024), 0, s>>>(a.tokens, a.token_type, a.vocab, N, w.sort_a, blocks, f);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         uint64_t *from = w.sort_a, *to = w.sort_b;
+        blocks = uint32_t((N + kMergeKeys - 1) / kMergeKeys);
+        fill = beside ? fill_groups(half, a.vocab) : 0; // one merge at most: N <= kSortBlock * kMergeWays
         for (int64_t len = kSortBlock; len < N; len *= kMergeWays) {
-            merge_kernel<<<dim3(uint32_t((N + 255) / 256)), dim3(256), 0, s>>>(from, N, len, to);
+            int shift = 4;
+            while ((len * kMergeWays) >> shift > kSamples) ++shift;
+            merge_kernel<<<dim3(blocks + fill), dim3(kMergeThreads), 0, s>>>(from, uint32_t(N), uint32_t(len), shift, to, blocks, f);
             if ((e = hipGetLastError()) != hipSuccess) return e;
             uint64_t *t = from;
             from = to;
@@ -278,7 +511,7 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
         p.sorted = from;
     }
     p.fill_block = (p.chunks * p.slabs + 3) / 4;
-    const int64_t fill = a.accumulate ? 0 : (a.vocab + 4 * kFillRows - 1) / (4 * kFillRows);
+    const int64_t fill = a.accumulate || beside ? 0 : (a.vocab + 4 * kSearchRows - 1) / (4 * kSearchRows);
     if (p.fill_block + fill == 0) return hipSuccess;
     embed_grad_kernel<T, G><<<dim3(uint32_t(p.fill_block + fill)), dim3(256), 0, s>>>(p);
     if ((e = hipGetLastError()) != hipSuccess) return e;

@@ -21,7 +21,7 @@ struct StageWorkspace {
 
 // Embedding gradient: the sorted tokens are dealt out in chunks, one wave per
 // chunk and slab of columns, about kEmbedItems of them.
-constexpr int64_t kEmbedItems = 8192;
+constexpr int64_t kEmbedItems = 4096;
 constexpr int kEmbedMinChunk = 4;
 int64_t embed_partial_bytes(int64_t max_tokens, int64_t max_hidden);
 

@@ -117,6 +117,26 @@ def test_embed_grad(dtype, n, h, v, pad):
             assert torch_().equal(start[ids(absent)], kept[ids(absent)])
 
 
+@pytest.mark.parametrize("n", [1, 700, 3000, 70000])
+def test_embed_grad_of_a_huge_vocabulary(n):
+    """Tokens of more than 21 bits: only some rows of the table are looked at."""
+    torch = torch_()
+    r = np.random.default_rng(n)
+    v = (1 << 21) + 9
+    dout, g = matrix(r, n, 4, "bfloat16")
+    pool = np.array([0, 1, v - 1, v - 2, (1 << 21) - 1, 1 << 21, (1 << 21) + 1, 77, -1, v, 1 << 40])
+    tok = pool[r.integers(0, len(pool), n)]
+    with ops(n, 4, v) as s:
+        out = s.embed_grad(ids(tok), dout, v, dtype=torch.float32)
+    rows, place = np.unique(np.where((tok >= 0) & (tok < v), tok, -1), return_inverse=True)
+    want = O.embed_grad(np.where(rows[place] < 0, -1, place), g, len(rows))
+    size = O.embed_grad(np.where(rows[place] < 0, -1, place), np.abs(g), len(rows))
+    some = rows >= 0
+    close(f64(out[ids(rows[some])]), want[some], (n + 2) * E * size[some] + TINY["float32"])
+    out[ids(rows[some])] = 0
+    assert int(out.count_nonzero()) == 0
+
+
 @pytest.mark.parametrize("n", [2048, 4096, 40000])
 def test_embed_grad_of_one_token(n):
     """One run over all chunks, and runs that end on every edge of a chunk."""
