@@ -85,7 +85,7 @@ typedef struct {
  * hipStream_t; NULL = the device's null stream) and allocates its workspace:
  * 16 bytes a token, max_tokens * max_hidden / 2 bytes for the embedding's
  * gradient (at most 256 MiB and at least 1 MiB), 4 bytes * max_hidden for each of
- * up to 1024 workgroups of the norm's gradient and about 1 MiB for
+ * up to 512 workgroups of the norm's gradient and about 1 MiB for
  * gwtf_stage_logprob.  *out receives the handle, or NULL on failure. */
 gwtf_status_t gwtf_stage_create(const gwtf_stage_shape_t *shape, void *hip_stream, gwtf_stage_t **out);
 

@@ -20,49 +20,78 @@ struct Vec8 {
 };
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
-// Columns [0, n) of p, the rest `fill`.  n >= 8 is the common case.
+template <class T, int w>
+struct VecN {
+    typedef T type __attribute__((ext_vector_type(w), aligned(sizeof(T))));
+};
+
+// Columns [0, n) of p, 0 < n < 8, as 4 + 2 + 1; the rest `fill`.
+template <class T>
+__device__ __forceinline__ typename Vec8<T>::type load_part(const T *p, int n, T fill)
+{
+    typename VecN<T, 4>::type f4 = {fill, fill, fill, fill};
+    typename VecN<T, 2>::type f2 = {fill, fill};
+    T f1 = fill;
+    if (n & 4) f4 = *reinterpret_cast<const typename VecN<T, 4>::type *>(p);
+    if (n & 2) f2 = *reinterpret_cast<const typename VecN<T, 2>::type *>(p + (n & 4));
+    if (n & 1) f1 = p[n & 6];
+    // the columns after the four: two and one, or one alone
+    const T r0 = n & 2 ? f2[0] : f1, r1 = f2[1], r2 = n & 2 ? f1 : fill;
+    typename Vec8<T>::type v = {f4[0], f4[1], f4[2], f4[3], r0, r1, r2, fill};
+    if (!(n & 4)) {
+        const typename Vec8<T>::type w = {r0, r1, r2, fill, fill, fill, fill, fill};
+        v = w;
+    }
+    return v;
+}
+template <class T>
+__device__ __forceinline__ void store_part(T *p, int n, const typename Vec8<T>::type &v)
+{
+    if (n & 4) {
+        const typename VecN<T, 4>::type f4 = {v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<typename VecN<T, 4>::type *>(p) = f4;
+    }
+    const T r0 = n & 4 ? v[4] : v[0], r1 = n & 4 ? v[5] : v[1], r2 = n & 4 ? v[6] : v[2];
+    if (n & 2) {
+        const typename VecN<T, 2>::type f2 = {r0, r1};
+        *reinterpret_cast<typename VecN<T, 2>::type *>(p + (n & 4)) = f2;
+    }
+    if (n & 1) p[n & 6] = n & 2 ? r2 : r0;
+}
+
+// Columns [0, n) of p as they lie in memory, the rest `fill`; n >= 8 is the
+// common case, n <= 0 reads nothing.
+template <class T>
+__device__ __forceinline__ typename Vec8<T>::type load8_raw(const T *p, int64_t n, T fill = T(0.f))
+{
+    if (n >= kVec) return *reinterpret_cast<const typename Vec8<T>::type *>(p);
+    return load_part(p, n > 0 ? int(n) : 0, fill);
+}
+
+template <class T>
+__device__ __forceinline__ void widen(const typename Vec8<T>::type &raw, float v[8])
+{
+    const f32x8 f = __builtin_convertvector(raw, f32x8);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = f[i];
+}
+
+// The same in 32 bits.
 template <class T>
 __device__ __forceinline__ void load8(const T *p, int64_t n, float v[8], float fill = 0.f)
 {
-    if (n >= kVec) {
-        const f32x8 f = __builtin_convertvector(*reinterpret_cast<const typename Vec8<T>::type *>(p), f32x8);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = f[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = i < n ? float(p[i]) : fill;
-    }
-}
-
-// The same as they lie in memory, for reads that are to be in flight for long;
-// columns from n on are 0.
-template <class T>
-__device__ __forceinline__ typename Vec8<T>::type load8_raw(const T *p, int64_t n)
-{
-    typename Vec8<T>::type v = {};
-    if (n >= kVec) {
-        v = *reinterpret_cast<const typename Vec8<T>::type *>(p);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (i < n) v[i] = p[i];
-    }
-    return v;
+    widen<T>(load8_raw(p, n, T(fill)), v);
 }
 
 template <class T>
 __device__ __forceinline__ void store8(T *p, int64_t n, const float v[8])
 {
-    if (n >= kVec) {
-        f32x8 f;
+    f32x8 f;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) f[i] = v[i];
-        *reinterpret_cast<typename Vec8<T>::type *>(p) = __builtin_convertvector(f, typename Vec8<T>::type);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (i < n) p[i] = T(v[i]);
-    }
+    for (int i = 0; i < kVec; ++i) f[i] = v[i];
+    const typename Vec8<T>::type r = __builtin_convertvector(f, typename Vec8<T>::type);
+    if (n >= kVec) *reinterpret_cast<typename Vec8<T>::type *>(p) = r;
+    else if (n > 0) store_part(p, int(n), r);
 }
 
 __device__ __forceinline__ int64_t load_token(const void *t, int is64, int64_t i)

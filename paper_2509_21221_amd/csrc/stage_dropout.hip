@@ -41,26 +41,43 @@ __device__ __forceinline__ void philox4x32(uint32_t k0, uint32_t k1, uint32_t c[
     }
 }
 
-template <class T>
+// Steps of eight columns a thread takes, with their reads side by side.
+constexpr uint32_t kUnits = 2;
+
+template <class T, bool RES>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutParams p)
 {
-    const uint32_t u = blockIdx.x * 256u + threadIdx.x;
-    if (u >= p.units) return;
-    const uint32_t r = p.steps.div(u), step = u - r * p.steps.d;
-    const int64_t row = p.row0 + r, col = int64_t(step) * kVec, n = p.H - col;
-    float v[8], res[8];
-    load8(static_cast<const T *>(p.x) + row * p.xs + col, n, v);
-    if (p.res) load8(static_cast<const T *>(p.res) + row * p.rs + col, n, res);
-    const uint64_t id = p.rows ? uint64_t(p.rows[row]) : uint64_t(row);
-    uint32_t c[4] = {step, p.site, uint32_t(id), uint32_t(id >> 32)};
-    philox4x32(p.k0, p.k1, c);
+    const uint32_t u0 = blockIdx.x * (256u * kUnits) + threadIdx.x;
+    typename Vec8<T>::type raw[kUnits], rraw[kUnits];
+    int64_t row[kUnits];
+    uint32_t step[kUnits];
+    uint64_t id[kUnits];
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        const uint32_t bits = (i & 1) ? c[i / 2] >> 16 : c[i / 2] & 0xffffu;
-        v[i] = bits >= p.limit ? v[i] * p.keep_scale : 0.f;
-        if (p.res) v[i] += res[i];
+    for (uint32_t q = 0; q < kUnits; ++q) {
+        const uint32_t u = u0 + q * 256u, r = p.steps.div(u < p.units ? u : 0);
+        step[q] = (u < p.units ? u : 0) - r * p.steps.d;
+        row[q] = p.row0 + r;
+        const int64_t col = int64_t(step[q]) * kVec, n = p.H - col;
+        raw[q] = load8_raw(static_cast<const T *>(p.x) + row[q] * p.xs + col, n);
+        if constexpr (RES) rraw[q] = load8_raw(static_cast<const T *>(p.res) + row[q] * p.rs + col, n);
+        id[q] = p.rows ? uint64_t(p.rows[row[q]]) : uint64_t(row[q]);
     }
-    store8(static_cast<T *>(p.out) + row * p.os + col, n, v);
+#pragma unroll
+    for (uint32_t q = 0; q < kUnits; ++q) {
+        uint32_t c[4] = {step[q], p.site, uint32_t(id[q]), uint32_t(id[q] >> 32)};
+        philox4x32(p.k0, p.k1, c);
+        float v[8], res[8];
+        widen<T>(raw[q], v);
+        if constexpr (RES) widen<T>(rraw[q], res);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const uint32_t bits = (i & 1) ? c[i / 2] >> 16 : c[i / 2] & 0xffffu;
+            v[i] = bits >= p.limit ? v[i] * p.keep_scale : 0.f;
+            if constexpr (RES) v[i] += res[i];
+        }
+        const int64_t col = int64_t(step[q]) * kVec;
+        if (u0 + q * 256u < p.units) store8(static_cast<T *>(p.out) + row[q] * p.os + col, p.H - col, v);
+    }
 }
 
 template <class T>
@@ -88,7 +105,9 @@ hipError_t run(const gwtf_stage_dropout_t &a, uint32_t limit, hipStream_t s)
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
         p.row0 = r;
         p.units = uint32_t(n * steps);
-        dropout_kernel<T><<<dim3((p.units + 255) / 256), dim3(256), 0, s>>>(p);
+        const dim3 grid((p.units + 256 * kUnits - 1) / (256 * kUnits));
+        if (p.res) dropout_kernel<T, true><<<grid, dim3(256), 0, s>>>(p);
+        else dropout_kernel<T, false><<<grid, dim3(256), 0, s>>>(p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

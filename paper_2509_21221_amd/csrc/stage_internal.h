@@ -26,7 +26,7 @@ constexpr int kEmbedMinChunk = 4;
 int64_t embed_partial_bytes(int64_t max_tokens, int64_t max_hidden);
 
 // Norm gradient: most workgroups that sum dweight over their rows.
-constexpr int kNormGradGroups = 1024;
+constexpr int kNormGradGroups = 512;
 
 // Log probabilities: most rows that are split over workgroups, most
 // workgroups that then share them, and bytes of one's record.

@@ -168,25 +168,40 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_grad_kerne
 #pragma unroll
         for (int i = 0; i < kVec; ++i) dw[k][i] = 0.f;
     }
-    int turn = 0;
-    for (int64_t row = blockIdx.x * rows_at_once + mine; row < p.num_tokens;
-         row += gridDim.x * rows_at_once, turn ^= 1) {
+    typename Vec8<T>::type rdy[K], rh[K], rd[K];
+    float rrstd = 0.f;
+    auto fetch = [&](int64_t row) {
         const T *dy = static_cast<const T *>(p.dy) + row * p.dy_stride;
         const T *hp = static_cast<const T *>(p.h) + row * p.h_stride;
-        const float rstd = p.rstd[row];
-        float g[K][8], xh[K][8], d[K][8], c = 0.f;
+        const T *dh = static_cast<const T *>(p.dh) + row * p.dh_stride;
+        rrstd = p.rstd[row];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int col = ((k * WAVES + part) * 64 + lane) * kVec;
-            load8(dy + col, H - col, g[k]);
-            load8(hp + col, H - col, xh[k]);
+            rdy[k] = load8_raw(dy + col, H - col);
+            rh[k] = load8_raw(hp + col, H - col);
+            if (p.dh) rd[k] = load8_raw(dh + col, H - col);
+        }
+    };
+    int turn = 0;
+    int64_t row = blockIdx.x * rows_at_once + mine;
+    if (row < p.num_tokens) fetch(row);
+    for (; row < p.num_tokens; row += gridDim.x * rows_at_once, turn ^= 1) {
+        const float rstd = rrstd;
+        float g[K][8], xh[K][8], d[K][8], c = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            widen<T>(rdy[k], g[k]);
+            widen<T>(rh[k], xh[k]);
             if (p.dh) {
-                load8(static_cast<const T *>(p.dh) + row * p.dh_stride + col, H - col, d[k]);
+                widen<T>(rd[k], d[k]);
             } else {
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) d[k][i] = 0.f;
             }
         }
+        // the next row is on its way while this one is reduced and written
+        if (row + int64_t(gridDim.x) * rows_at_once < p.num_tokens) fetch(row + int64_t(gridDim.x) * rows_at_once);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
 #pragma unroll
@@ -235,8 +250,17 @@ __global__ __launch_bounds__(1024) void dweight_kernel(const float *partial, int
     const int c = threadIdx.x & 15, g = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
     const int each = (groups + 63) / 64, g0 = g * each, g1 = g0 + each < groups ? g0 + each : groups;
     float v = 0.f;
-    if (col < H)
-        for (int i = g0; i < g1; ++i) v += partial[int64_t(i) * H + col];
+    if (col < H) {
+        int i = g0;
+        for (; i + 8 <= g1; i += 8) {
+            float f[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f[q] = partial[int64_t(i + q) * H + col];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v += f[q];
+        }
+        for (; i < g1; ++i) v += partial[int64_t(i) * H + col];
+    }
     red[g][c] = v;
     __syncthreads();
     for (int half = 32; half > 0; half >>= 1) {
