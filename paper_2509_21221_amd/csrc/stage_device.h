@@ -175,6 +175,7 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v)
 // 2^x and ln 2 / log2 e; the hardware's exponential and logarithm have base 2.
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLn2Low = float(0.69314718055994530942 - double(kLn2));
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 } // namespace gwtf

@@ -1,37 +1,56 @@
 // Log probabilities of given tokens, entropy and the most likely tokens
 // (gwtf_stage_logprob), and the gradient (gwtf_stage_logprob_grad).
 //
-// One pass over a row with the running maximum m of each lane,
-//   s = sum e^(x - m)   and   t = sum e^(x - m) (x - m) / ln 2,
+// One pass over a row in base 2, y = x log2 e, with the running maximum m of
+// each lane's y,
+//   s = sum 2^(y - m)   and   t = sum 2^(y - m) (y - m),
 // both rescaled when m grows; parts with different m join the same way.  Then
-//   lse = m + ln s,   entropy = ln s - ln 2 * t / s,
-// where every term of t has one sign, so nothing cancels.  (x - m) log2 e as
-// one fused operation with m log2 e at hand would overflow for masks of the
-// type's lowest value.
+//   lse = ln 2 (m + log2 s),   entropy = ln 2 (log2 s - t / s),
+// where every term of t has one sign, so nothing cancels.  m is a rounded
+// product, which does no harm: it is the same number in y - m, one fused
+// operation, and in the result.  A row whose largest y is beyond 2^100, or
+// -infinity though its largest x is not (entries of the type's lowest value
+// overflow in y), is gone through again with (x - m) log2 e in place of y - m
+// (WIDE).
 //
-// Alternatives: each wave keeps its largest entries as keys (order of the
-// value, then lower index) sorted over its lanes, and looks closer at a step
-// only where a lane's largest value passes the last of them.
+// Alternatives: a lane reads 16 adjacent columns at a time, a unit, and keeps
+// the two units with the largest entries that it has met.  The `top` largest
+// of these over the workgroup hold all alternatives, since any other unit has
+// `top` entries before its first -- unless both of a lane's units are among
+// them and a third might be: then that lane's columns are looked through.  With
+// many alternatives, or too few units or entries that are numbers, the row is
+// gone through again with a list that is right for every input (list_pass).
+// Ties go by index throughout: units are ordered as their columns are.
 #include "stage_device.h"
 #include "stage_internal.h"
 
 namespace gwtf {
 namespace {
 
+constexpr int kLpWaves = 4;
+constexpr int kLpThreads = kLpWaves * 64;
+constexpr int kUnit = 16;
+constexpr int kStep = kLpThreads * kUnit; // columns of a workgroup's step
+// Two of the 24 largest units fall to one of 256 lanes in two rows of three, two
+// of 8 in one of nine.
+constexpr int kUnitTop = 24;
 constexpr float kLowest = -200.f; // 2^-200 is 0: keeps 0 * -infinity out of t
+constexpr float kNone = -__builtin_inff();
+constexpr float kLargeRef = 0x1p100f;
 
 struct Softmax {
     float m, s, t;
 };
 
-__device__ __forceinline__ float finite_or_zero(float m) { return m == -__builtin_inff() ? 0.f : m; }
+__device__ __forceinline__ float finite_or_zero(float m) { return m == kNone ? 0.f : m; }
 
+template <bool WIDE>
 __device__ __forceinline__ Softmax join(const Softmax &a, const Softmax &b)
 {
     Softmax r;
     r.m = fmaxf(a.m, b.m);
-    const float ms = finite_or_zero(r.m);
-    const float da = (a.m - ms) * kLog2e, db = (b.m - ms) * kLog2e;
+    const float ms = finite_or_zero(r.m), f = WIDE ? kLog2e : 1.f;
+    const float da = (a.m - ms) * f, db = (b.m - ms) * f;
     const float ea = exp2_(da), eb = exp2_(db);
     r.s = a.s * ea + b.s * eb;
     r.t = ea * (a.t + fmaxf(da, kLowest) * a.s) + eb * (b.t + fmaxf(db, kLowest) * b.s);
@@ -47,13 +66,38 @@ __device__ __forceinline__ Softmax lane_of(const Softmax &a, int lane)
 {
     return {lane_value(a.m, lane), lane_value(a.s, lane), lane_value(a.t, lane)};
 }
+template <bool WIDE>
 __device__ __forceinline__ Softmax wave_join(Softmax a)
 {
-    a = join(a, row_ror<8>(a));
-    a = join(a, row_ror<4>(a));
-    a = join(a, row_ror<2>(a));
-    a = join(a, row_ror<1>(a));
-    return join(join(lane_of(a, 0), lane_of(a, 16)), join(lane_of(a, 32), lane_of(a, 48)));
+    a = join<WIDE>(a, row_ror<8>(a));
+    a = join<WIDE>(a, row_ror<4>(a));
+    a = join<WIDE>(a, row_ror<2>(a));
+    a = join<WIDE>(a, row_ror<1>(a));
+    return join<WIDE>(join<WIDE>(lane_of(a, 0), lane_of(a, 16)), join<WIDE>(lane_of(a, 32), lane_of(a, 48)));
+}
+
+// A lane's 16 columns; `x_max`: their largest with the lane's former ones.
+template <bool WIDE>
+__device__ __forceinline__ void add_unit(Softmax &r, const float v[kUnit], float x_max)
+{
+    const float m = WIDE ? x_max : x_max * kLog2e, ms = finite_or_zero(m);
+    const float d0 = (r.m - ms) * (WIDE ? kLog2e : 1.f), e0 = exp2_(d0);
+    r.t = e0 * (r.t + fmaxf(d0, kLowest) * r.s);
+    r.s *= e0;
+    r.m = m;
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) {
+        const float d = WIDE ? (v[i] - ms) * kLog2e : fmaf(v[i], kLog2e, -ms), e = exp2_(d);
+        r.s += e;
+        r.t = fmaf(e, fmaxf(d, kLowest), r.t);
+    }
+}
+__device__ __forceinline__ float unit_max(const float v[kUnit])
+{
+    float most = v[0];
+#pragma unroll
+    for (int i = 1; i < kUnit; ++i) most = fmaxf(most, v[i]); // the other one of a NaN
+    return most;
 }
 
 // Order of a float as a signed integer; -0 counts as +0.
@@ -68,6 +112,8 @@ __device__ __forceinline__ uint64_t key_of(int order, uint32_t index)
 {
     return (uint64_t(uint32_t(order) ^ 0x80000000u) << 32) | (0xffffffffu - index);
 }
+__device__ __forceinline__ uint32_t key_order(uint64_t k) { return uint32_t(k >> 32); } // unsigned
+__device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xffffffffu - uint32_t(k); }
 
 __device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane)
 {
@@ -75,14 +121,22 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane)
     return (uint64_t(hi) << 32) | lo;
 }
 
+// Orders LDS accesses of one wave's lanes.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+constexpr int kSlots = GWTF_STAGE_MAX_TOP;
+
 // The wave's `top` largest keys, the j-th in lane j, 0 in the other lanes.
 // Keys join by rank: every new key is compared with the others and with the
 // list in independent steps, where inserting them one after another is a
-// chain of some 400 cycles for each (seven rows of 131,072 with eight
-// alternatives: 96 us inserting, see the kernel for the present time).
+// chain of some 400 cycles for each.
 struct TopList {
     uint64_t key, last; // this lane's; the smallest that counts (uniform)
-    uint64_t *slots;    // `top` of this wave's, in LDS
+    uint64_t *slots;    // kSlots of this wave's, in LDS
     int top;
     __device__ __forceinline__ void start(int k, uint64_t *lds)
     {
@@ -90,37 +144,93 @@ struct TopList {
         slots = lds;
         top = k;
     }
-    __device__ __forceinline__ bool list_empty() const { return lane_key(key, 0) == 0; }
-    __device__ __forceinline__ int last_order() const { return int(uint32_t(last >> 32) ^ 0x80000000u); }
     // Takes the keys of the lanes with key > last (`some`, not empty).
     __device__ __forceinline__ void merge(uint64_t k, uint64_t some)
     {
         const int lane = __lane_id();
         int rank = 0, mine = lane;
-        if (list_empty()) {
-            for (uint64_t m = some; m; m &= m - 1) rank += lane_key(k, __builtin_ctzll(m)) > k;
-            mine += __popcll(some);
-        } else {
-            for (uint64_t m = some; m; m &= m - 1) {
-                const uint64_t other = lane_key(k, __builtin_ctzll(m));
-                rank += other > k;
-                mine += other > key;
-            }
-            for (int j = 0; j < top; ++j) rank += lane_key(key, j) > k;
+        for (uint64_t m = some; m; m &= m - 1) {
+            const uint64_t other = lane_key(k, __builtin_ctzll(m));
+            rank += other > k;
+            mine += other > key;
         }
+        if (lane_key(key, 0)) // not the first keys
+            for (int j = 0; j < top; ++j) rank += lane_key(key, j) > k;
         if ((some >> lane & 1) && rank < top) slots[rank] = k;
         if (lane < top && mine < top) slots[mine] = key;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
         key = lane < top ? slots[lane] : 0;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
         last = lane_key(key, top - 1);
     }
     __device__ __forceinline__ void offer(uint64_t k)
     {
         const uint64_t some = __ballot(k > last);
         if (some) merge(k, some);
+    }
+    // A bound that enough of the lanes' words reach: the lanes are dealt out in
+    // as many groups as there are keys wanted (or more), and it is the least of
+    // the groups' largest words.
+    __device__ __forceinline__ uint32_t bound_of(uint32_t w) const
+    {
+        auto fold = [](uint32_t a, uint32_t b, bool larger) { return (a > b) == larger ? a : b; };
+        w = fold(w, uint32_t(__builtin_amdgcn_update_dpp(int(w), int(w), 0xB1, 0xf, 0xf, false)), top <= 32); // quad 1 0 3 2
+        w = fold(w, uint32_t(__builtin_amdgcn_update_dpp(int(w), int(w), 0x4E, 0xf, 0xf, false)), top <= 16); // quad 2 3 0 1
+        w = fold(w, uint32_t(__builtin_amdgcn_update_dpp(int(w), int(w), 0x141, 0xf, 0xf, false)), top <= 8); // half mirror
+        w = fold(w, uint32_t(gwtf::row_ror<8>(int(w))), top <= 4);
+        const uint32_t a = fold(__builtin_amdgcn_readlane(w, 0), __builtin_amdgcn_readlane(w, 16), top <= 2);
+        const uint32_t b = fold(__builtin_amdgcn_readlane(w, 32), __builtin_amdgcn_readlane(w, 48), top <= 2);
+        return fold(a, b, top <= 1);
+    }
+    // The largest of M keys a lane, into an empty list: those that reach a
+    // bound, mostly no more than 64, join at once.  Where many share the
+    // bound's order, their indices give a second one.
+    template <int M>
+    __device__ __forceinline__ void select(const uint64_t (&k)[M])
+    {
+        const int lane = __lane_id();
+        uint32_t best = 0;
+#pragma unroll
+        for (int i = 0; i < M; ++i) best = umax(best, key_order(k[i]));
+        const uint32_t order = bound_of(best);
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < M; ++i) count += __popcll(__ballot(k[i] != 0 && key_order(k[i]) >= order));
+        uint64_t least = uint64_t(order) << 32;
+        if (count > kSlots) {
+            best = 0;
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+                best = umax(best, key_order(k[i]) > order ? 0xffffffffu : key_order(k[i]) == order ? uint32_t(k[i]) : 0u);
+            least |= bound_of(best);
+        }
+        count = 0;
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const bool in = k[i] != 0 && k[i] >= least;
+            const uint64_t some = __ballot(in);
+            const int place = count + __popcll(some & ((uint64_t(1) << lane) - 1));
+            if (in && place < kSlots) slots[place] = k[i];
+            count += __popcll(some);
+        }
+        if (count <= kSlots) {
+            wave_sync();
+            const uint64_t one = lane < count ? slots[lane] : 0;
+            wave_sync();
+            int rank = 0;
+            for (int j = 0; j < count; j += 4) { // lanes past the last hold 0
+#pragma unroll
+                for (int q = 0; q < 4; ++q) rank += lane_key(one, j + q) > one;
+            }
+            if (lane < count && rank < top) slots[rank] = one;
+            wave_sync();
+            key = lane < top && lane < count ? slots[lane] : 0;
+            wave_sync();
+            last = lane_key(key, top - 1);
+        } else {
+#pragma unroll
+            for (int i = 0; i < M; ++i) offer(k[i]);
+        }
     }
 };
 
@@ -132,36 +242,28 @@ struct LogprobParams {
     uint32_t *arrived;  // [rows], 0 between calls
 };
 
-constexpr int kLpWaves = 4;
-constexpr int kStep = kLpWaves * 64 * kVec * 2; // columns of a workgroup's step
+__device__ __forceinline__ float log_prob(float x, float lse) { return x == kNone && lse == lse ? x : x - lse; }
 
 // The values that a row's sums give, from lane 0 of the wave that joined it;
 // then its alternatives, from lanes below `top`.
-__device__ __forceinline__ float log_prob(float x, float lse)
+template <bool WIDE>
+__device__ __forceinline__ void finish_row(const gwtf_stage_logprob_t &a, int64_t row, const Softmax &r, const TopList &list,
+                                           bool there, float xt)
 {
-    return x == -__builtin_inff() && lse == lse ? x : x - lse;
-}
-
-template <class T>
-__device__ __forceinline__ void finish_row(const gwtf_stage_logprob_t &a, int64_t row, const Softmax &r, const TopList &list)
-{
-    const int lane = threadIdx.x & 63;
-    const float ln_s = logf(r.s), lse = finite_or_zero(r.m) + ln_s;
+    const int lane = __lane_id();
+    const float ln_s = logf(r.s), m = finite_or_zero(r.m);
+    // ln 2 in two parts: one product would lose the last bits of m
+    const float lse = WIDE ? m + ln_s : fmaf(m, kLn2, fmaf(m, kLn2Low, ln_s));
     if (lane == 0) {
         if (a.lse) a.lse[row] = lse;
         if (a.entropy) a.entropy[row] = r.s == 0.f ? 0.f : ln_s - kLn2 * (r.t / r.s);
-        if (a.logp) {
-            const int64_t t = load_token(a.targets, a.token_type, row);
-            float v = 0.f;
-            if (t >= 0 && t < a.vocab) v = log_prob(float(static_cast<const T *>(a.logits)[row * a.logits_stride + t]), lse);
-            a.logp[row] = v;
-        }
+        if (a.logp) a.logp[row] = there ? log_prob(xt, lse) : 0.f;
     }
     if (lane < a.top) {
         const bool none = list.key == 0;
-        const float x = value_of(int(uint32_t(list.key >> 32) ^ 0x80000000u));
+        const float x = value_of(int(key_order(list.key) ^ 0x80000000u));
         a.top_logp[row * a.top + lane] = none ? __builtin_nanf("") : log_prob(x, lse);
-        a.top_ids[row * a.top + lane] = none ? -1 : int32_t(0xffffffffu - uint32_t(list.key));
+        a.top_ids[row * a.top + lane] = none ? -1 : int32_t(key_index(list.key));
     }
 }
 
@@ -179,128 +281,295 @@ __device__ __forceinline__ uint64_t get_key(const uint64_t *p)
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// The wave's part of the sums over a whole row with (x - m) log2 e.
+template <class T>
+__device__ __attribute__((noinline)) Softmax wide_pass(const T *x, int64_t vocab)
+{
+    Softmax r = {kNone, 0.f, 0.f};
+    for (int64_t base = 0; base < vocab; base += kStep) {
+        const int64_t col = base + threadIdx.x * kUnit;
+        float v[kUnit];
+        load8(x + col, vocab - col, v, kNone);
+        load8(x + col + kVec, vocab - col - kVec, v + kVec, kNone);
+        add_unit<true>(r, v, fmaxf(r.m, unit_max(v)));
+    }
+    return wave_join<true>(r);
+}
+
+// The wave's largest entries of columns [c0, c1) of a row, from all of them:
+// each step, a lane offers its largest entry that is left, the lowest index of
+// equal ones, until none is above the list's last.
+template <class T>
+__device__ __attribute__((noinline)) uint64_t list_pass(uint64_t *slots, int top, const T *x, int64_t c0, int64_t c1)
+{
+    TopList list;
+    list.start(top, slots);
+    for (int64_t base = c0; base < c1; base += kStep) {
+        const int64_t col = base + threadIdx.x * kUnit;
+        float v[kUnit];
+        load8(x + col, c1 - col, v, __builtin_nanf(""));
+        load8(x + col + kVec, c1 - col - kVec, v + kVec, __builtin_nanf(""));
+        for (;;) {
+            const float best = unit_max(v);
+            int slot = -1;
+#pragma unroll
+            for (int i = kUnit - 1; i >= 0; --i) slot = v[i] == best ? i : slot;
+            const uint64_t k = slot < 0 ? 0 : key_of(order_of(best), uint32_t(col + slot));
+            const uint64_t some = __ballot(k > list.last);
+            if (!some) break;
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i)
+                if (slot == i) v[i] = __builtin_nanf("");
+            list.merge(k, some);
+        }
+    }
+    return list.key;
+}
+
+// The entries of the units that `units` lists (16 a unit), largest first.
+template <class T>
+__device__ __forceinline__ void resolve_units(TopList &list, const TopList &units, const T *x, int64_t c0, int64_t c1)
+{
+    constexpr int kBatch = kUnitTop * kUnit / 64;
+    const int lane = __lane_id();
+    const uint32_t least = key_order(units.last);
+    uint64_t k[kBatch];
+    float v[kBatch];
+    uint32_t at[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+        const int i = q * 64 + lane;
+        v[q] = __builtin_nanf("");
+        at[q] = 0;
+        if (q * 64 < units.top * kUnit) {
+            const uint32_t unit = 0xffffffffu - uint32_t(__shfl(int(uint32_t(units.key)), i / kUnit & 63));
+            const int64_t col = c0 + int64_t(unit) * kUnit + i % kUnit;
+            at[q] = uint32_t(col);
+            if (i < units.top * kUnit && col < c1) v[q] = float(x[col]);
+        }
+    }
+    list.start(units.top, units.slots);
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+        k[q] = v[q] == v[q] ? key_of(order_of(v[q]), at[q]) : 0;
+        if (key_order(k[q]) < least) k[q] = 0;
+    }
+    list.select(k);
+}
+
+// Offers the entries of every unit of those lanes whose two units are both in
+// `units`, but for these two, which are resolved.
+template <class T>
+__device__ __forceinline__ void resolve_lanes(TopList &list, const TopList &units, const T *x, int64_t c0, int64_t c1)
+{
+    const int lane = __lane_id();
+    const uint32_t unit = key_index(units.key), owner = unit % kLpThreads;
+    const int64_t total = (c1 - c0 + kUnit - 1) / kUnit;
+    for (int j = 0; j + 1 < units.top; ++j) {
+        const uint32_t o = __builtin_amdgcn_readlane(int(owner), j);
+        const uint64_t both = __ballot(lane < units.top && owner == o);
+        if (__popcll(both) < 2 || __builtin_ctzll(both) != j) continue;
+        const uint32_t done0 = __builtin_amdgcn_readlane(int(unit), j);
+        const uint32_t done1 = __builtin_amdgcn_readlane(int(unit), 63 - __builtin_clzll(both));
+        for (int64_t u0 = o; u0 < total; u0 += 16 * kLpThreads) {
+            float v[4];
+            int64_t col[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t u = u0 + (q * 4 + lane / kUnit) * kLpThreads;
+                col[q] = c0 + u * kUnit + lane % kUnit;
+                v[q] = u < total && col[q] < c1 && u != done0 && u != done1 ? float(x[col[q]]) : __builtin_nanf("");
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) list.offer(v[q] == v[q] ? key_of(order_of(v[q]), uint32_t(col[q])) : 0);
+        }
+    }
+}
+
 template <class T, bool TOP>
-__global__ __launch_bounds__(kLpWaves * 64) void logprob_kernel(LogprobParams p)
+__global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
 {
     __shared__ Softmax parts[kLpWaves];
-    __shared__ uint64_t keys[TOP ? kLpWaves * GWTF_STAGE_MAX_TOP : 1];
-    __shared__ uint32_t last_one;
+    __shared__ uint64_t units_of[TOP ? 2 * kLpThreads : 1]; // and each wave's slots
+    __shared__ uint32_t flag, alive[kLpWaves];
     const gwtf_stage_logprob_t &a = p.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row = blockIdx.x / uint32_t(p.segments), segment = blockIdx.x - uint32_t(row) * uint32_t(p.segments);
     const int64_t c0 = segment * p.width, c1 = c0 + p.width < a.vocab ? c0 + p.width : a.vocab;
     const T *x = static_cast<const T *>(a.logits) + row * a.logits_stride;
-    Softmax r = {-__builtin_inff(), 0.f, 0.f};
-    TopList list;
-    list.start(a.top, keys + (TOP ? wave * GWTF_STAGE_MAX_TOP : 0));
-    for (int64_t base = c0; base < c1; base += kStep) {
-        const int64_t col = base + (wave * 64 + lane) * kVec;
-        float v[16];
-        load8(x + col, c1 - col, v, -__builtin_inff());
-        load8(x + col + kStep / 2, c1 - col - kStep / 2, v + 8, -__builtin_inff());
-        float most = v[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) most = fmaxf(most, v[i]);
-        const float m = fmaxf(r.m, most), ms = finite_or_zero(m);
-        const float d0 = (r.m - ms) * kLog2e, e0 = exp2_(d0);
-        r.t = e0 * (r.t + fmaxf(d0, kLowest) * r.s);
-        r.s *= e0;
-        r.m = m;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float d = (v[i] - ms) * kLog2e, e = exp2_(d);
-            r.s += e;
-            r.t += e * fmaxf(d, kLowest);
-        }
+    // The wave that joins the others' results: its work would pile up on one
+    // SIMD if it were the same in all workgroups of a CU, which are 256 apart.
+    const int chief = blockIdx.x >> 8 & (kLpWaves - 1);
+    uint64_t *const slots = units_of + (TOP ? wave * kSlots : 0);
+    // the target's entry is needed last and read first: two dependent reads
+    int64_t target = -1;
+    if (a.logp) target = load_token(a.targets, a.token_type, row);
+    const bool there = target >= 0 && target < a.vocab;
+    float xt = 0.f;
+    if (there) xt = float(x[target]);
+    Softmax r = {kNone, 0.f, 0.f};
+    float first = kNone, second = kNone; // the largest entries of the lane's two units
+    // The lane's first unit counts whatever it holds, so that rows of masked
+    // entries have units too; others of -infinity come after 256 of these.
+    int unit = threadIdx.x, unit1 = c0 + unit * kUnit < c1 ? unit : -1, unit2 = -1;
+    auto add = [&](const float (&v)[kUnit]) {
+        const float most = unit_max(v);
         if constexpr (TOP) {
-            // A wave goes up through its columns, so what only equals the
-            // last of the list in a later step has the higher index.
-            if (!__ballot(list.last == 0 || order_of(most) > list.last_order())) continue;
+            const bool above = most > first, between = most > second;
+            unit2 = above ? unit1 : between ? unit : unit2;
+            second = above ? first : fmaxf(second, most);
+            unit1 = above ? unit : unit1;
+        }
+        first = fmaxf(first, most);
+        add_unit<false>(r, v, first);
+        unit += kLpThreads;
+    };
+    // whole steps with the next one on its way, then what is left
+    typedef typename Vec8<T>::type Raw;
+    const int64_t whole = c0 + (c1 - c0) / kStep * kStep;
+    const T *at = x + c0 + threadIdx.x * kUnit;
+    Raw lo = {}, hi = {};
+    if (c0 < whole) {
+        lo = *reinterpret_cast<const Raw *>(at);
+        hi = *reinterpret_cast<const Raw *>(at + kVec);
+    }
+    for (int64_t base = c0; base < whole; base += kStep) {
+        float v[kUnit];
+        widen<T>(lo, v);
+        widen<T>(hi, v + kVec);
+        at += kStep;
+        if (base + kStep < whole) {
+            lo = *reinterpret_cast<const Raw *>(at);
+            hi = *reinterpret_cast<const Raw *>(at + kVec);
+        }
+        add(v);
+    }
+    if (whole < c1) {
+        const int64_t n = c1 - whole - threadIdx.x * kUnit;
+        float v[kUnit];
+        load8(at, n, v, kNone);
+        load8(at + kVec, n - kVec, v + kVec, kNone);
+        add(v);
+    }
+    TopList list;
+    if constexpr (TOP) {
+        bool again = a.top > kUnitTop;
+        if (!again) {
+            units_of[threadIdx.x] = unit1 < 0 ? 0 : key_of(order_of(first), uint32_t(unit1));
+            units_of[kLpThreads + threadIdx.x] = unit2 < 0 || unit2 == unit1 ? 0 : key_of(order_of(second), uint32_t(unit2));
+            __syncthreads();
+            if (wave == chief) {
+                uint64_t k[2 * kLpWaves];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (col + (i < 8 ? 0 : kStep / 2) + (i & 7) >= c1) v[i] = __builtin_nanf("");
-            // Each lane offers its largest entry that is left, the lowest
-            // index of equal ones, until none is above the list's last.
-            for (;;) {
-                float best = v[0];
+                for (int i = 0; i < 2 * kLpWaves; ++i) k[i] = units_of[i * 64 + lane];
+                wave_sync();
+                list.start(a.top, slots);
+                list.select(k);
+                again = list.last == 0;
+                if (!again) {
+                    const TopList units = list;
+                    resolve_units(list, units, x, c0, c1);
+                    if (c1 - c0 > 2 * kStep) resolve_lanes(list, units, x, c0, c1);
+                    again = list.last == 0;
+                }
+                if (lane == 0) flag = again;
+            }
+            __syncthreads();
+            again = flag;
+        }
+        if (again) {
+            const uint64_t mine = list_pass(slots, a.top, x, c0, c1);
+            __syncthreads();
+            units_of[threadIdx.x] = mine;
+            __syncthreads();
+            if (wave == chief) {
+                uint64_t k[kLpWaves];
 #pragma unroll
-                for (int i = 1; i < 16; ++i) best = fmaxf(best, v[i]); // the other one of a NaN
-                int slot = -1;
-#pragma unroll
-                for (int i = 15; i >= 0; --i) slot = v[i] == best ? i : slot;
-                const uint32_t at = uint32_t(col) + (slot < 8 ? 0 : kStep / 2) + (slot & 7);
-                const uint64_t k = slot < 0 ? 0 : key_of(order_of(best), at);
-                const uint64_t some = __ballot(k > list.last);
-                if (!some) break;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (slot == i) v[i] = __builtin_nanf("");
-                list.merge(k, some);
+                for (int i = 0; i < kLpWaves; ++i) k[i] = units_of[i * 64 + lane];
+                wave_sync();
+                list.start(a.top, slots);
+                list.select(k);
             }
         }
     }
-    r = wave_join(r);
-    if (lane == 0) parts[wave] = r;
-    if constexpr (TOP) {
-        if (lane < a.top) keys[wave * GWTF_STAGE_MAX_TOP + lane] = list.key;
+    const bool some = __ballot(first > kNone) != 0; // an entry that is not masked
+    r = wave_join<false>(r);
+    if (lane == 0) {
+        parts[wave] = r;
+        alive[wave] = some;
     }
     __syncthreads();
-    if (wave == 0) {
-        r = join(join(parts[0], parts[1]), join(parts[2], parts[3]));
-        if constexpr (TOP) {
-            for (int w = 1; w < kLpWaves; ++w) list.offer(lane < a.top ? keys[w * GWTF_STAGE_MAX_TOP + lane] : 0);
-        }
-    }
-    if (p.segments == 1) {
-        if (wave == 0) finish_row<T>(a, row, r, list);
-        return;
-    }
-    // The workgroup that arrives last joins the row's records.  Records and
-    // counter are words of agent scope; the wait puts a record in memory before
-    // its arrival is counted.  (A fence of agent scope would write back and
-    // drop the whole L2 of the XCD: 8 us on seven rows of 131,072.)
-    unsigned char *record = p.records + int64_t(blockIdx.x) * kLogprobRecord;
-    if (wave == 0) {
-        if (lane == 0) {
-            uint32_t *w = reinterpret_cast<uint32_t *>(record);
-            put(w, __float_as_uint(r.m));
-            put(w + 1, __float_as_uint(r.s));
-            put(w + 2, __float_as_uint(r.t));
-        }
-        if constexpr (TOP) {
-            if (lane < a.top) put(reinterpret_cast<uint64_t *>(record + 16) + lane, list.key);
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (lane == 0)
-            last_one = __hip_atomic_fetch_add(p.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+    r = join<false>(join<false>(parts[0], parts[1]), join<false>(parts[2], parts[3]));
+    bool live = alive[0] | alive[1] | alive[2] | alive[3];
+    if (p.segments > 1) {
+        // The workgroup that arrives last joins the row's records.  Records and
+        // counter are words of agent scope; the wait puts a record in memory
+        // before its arrival is counted.  (A fence of agent scope would write
+        // back and drop the whole L2 of the XCD: 5 us on seven rows of 131,072.)
+        if (wave == chief) {
+            unsigned char *record = p.records + int64_t(blockIdx.x) * kLogprobRecord;
+            if (lane == 0) {
+                uint32_t *w = reinterpret_cast<uint32_t *>(record);
+                put(w, __float_as_uint(r.m));
+                put(w + 1, __float_as_uint(r.s));
+                put(w + 2, __float_as_uint(r.t));
+                put(w + 3, live);
+            }
+            if constexpr (TOP) {
+                if (lane < a.top) put(reinterpret_cast<uint64_t *>(record + 16) + lane, list.key);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (lane == 0)
+                flag = __hip_atomic_fetch_add(p.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                        uint32_t(p.segments - 1);
-    }
-    __syncthreads();
-    if (!last_one) return;
-    const unsigned char *first = p.records + row * p.segments * kLogprobRecord;
-    if constexpr (TOP) {
-        // all waves take parts of the keys, then the first one theirs
-        list.start(a.top, keys + wave * GWTF_STAGE_MAX_TOP);
-        const int all = p.segments * a.top;
-        for (int i0 = wave * 64; i0 < all; i0 += kLpWaves * 64) {
-            const int i = i0 + lane, seg = i / a.top;
-            list.offer(i < all ? get_key(reinterpret_cast<const uint64_t *>(first + seg * kLogprobRecord + 16) + (i - seg * a.top)) : 0);
         }
-        if (lane < a.top) keys[wave * GWTF_STAGE_MAX_TOP + lane] = list.key;
         __syncthreads();
+        if (!flag) return;
+        const unsigned char *records = p.records + row * p.segments * kLogprobRecord;
+        r = {kNone, 0.f, 0.f};
+        live = false;
+        for (int i = lane; i < p.segments; i += 64) { // in all waves alike
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(records + i * kLogprobRecord);
+            r = join<false>(r, Softmax{get_float(w), get_float(w + 1), get_float(w + 2)});
+            live |= __float_as_uint(get_float(w + 3)) != 0;
+        }
+        live = __ballot(live) != 0;
+        r = wave_join<false>(r);
+        if constexpr (TOP) {
+            if (wave == chief) {
+                constexpr int kBatch = 8; // keys of a lane read side by side
+                const int all = p.segments * a.top;
+                list.start(a.top, slots);
+                for (int i0 = 0; i0 < all; i0 += kBatch * 64) {
+                    uint64_t k[kBatch];
+#pragma unroll
+                    for (int q = 0; q < kBatch; ++q) {
+                        const int i = i0 + q * 64 + lane, seg = i / a.top;
+                        k[q] = i < all ? get_key(reinterpret_cast<const uint64_t *>(records + seg * kLogprobRecord + 16) + (i - seg * a.top)) : 0;
+                    }
+                    if (i0 == 0) {
+                        list.select(k);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < kBatch; ++q) list.offer(k[q]);
+                    }
+                }
+            }
+        }
+        if (threadIdx.x == 0) p.arrived[row] = 0;
     }
-    if (wave != 0) return;
-    r = {-__builtin_inff(), 0.f, 0.f};
-    for (int i = lane; i < p.segments; i += 64) {
-        const uint32_t *w = reinterpret_cast<const uint32_t *>(first + i * kLogprobRecord);
-        r = join(r, Softmax{get_float(w), get_float(w + 1), get_float(w + 2)});
+    // r is the row's, in all waves
+    if (live && !(fabsf(r.m) <= kLargeRef)) {
+        r = wide_pass(x, a.vocab);
+        __syncthreads();
+        if (lane == 0) parts[wave] = r;
+        __syncthreads();
+        if (wave != chief) return;
+        r = join<true>(join<true>(parts[0], parts[1]), join<true>(parts[2], parts[3]));
+        finish_row<true>(a, row, r, list, there, xt);
+    } else if (wave == chief) {
+        finish_row<false>(a, row, r, list, there, xt);
     }
-    r = wave_join(r);
-    if constexpr (TOP) {
-        for (int w = 1; w < kLpWaves; ++w) list.offer(lane < a.top ? keys[w * GWTF_STAGE_MAX_TOP + lane] : 0);
-    }
-    finish_row<T>(a, row, r, list);
-    if (lane == 0) p.arrived[row] = 0;
 }
 
 // ---- gradient ----

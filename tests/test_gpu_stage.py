@@ -407,6 +407,31 @@ def test_logprob(dtype, kind, n, v, top):
     assert bare[0] is None and torch_().equal(bare[2], got[2])
 
 
+@pytest.mark.parametrize("v, top", [(20000, 3), (20001, 8), (131072, 24), (131072, 25), (300, 64)])
+def test_logprob_alternatives_in_few_columns(v, top):
+    """Largest entries 4096 columns apart, side by side, few, and tied over the row."""
+    r = np.random.default_rng(v)
+    a = np.full((520, v), -1, np.float32)  # whole rows by one workgroup
+    a[:40] = r.standard_normal((40, v))
+    a[0, 37::4096] = 50 + r.standard_normal(len(a[0, 37::4096]))
+    a[1, 100:100 + top] = np.arange(top) + 20
+    a[2] = -np.inf
+    a[2, 5] = 1
+    a[3] = np.where(np.arange(v) % 4096 == 17, 9, -np.inf)
+    a[4] = 3
+    a[5, ::16] = 30
+    a[6, v - 1] = a[6, 0] = 40
+    a[7, 37::4096] = 50
+    for rows in (a[:8], a):
+        x, xv = matrix(r, *rows.shape, "bfloat16", a=rows)
+        with ops(len(rows), 1, v) as s:
+            _, _, lse, top_logp, top_ids = s.logprob(x, top=top)
+        want = O.logprob(xv[:41], None, top)
+        assert (top_ids.cpu().numpy()[:41] == want[4]).all()
+        same(f64(top_logp)[:41], want[3], 1e-4, "top")
+        assert (top_ids[40:].cpu().numpy() == np.arange(top)).all()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_logprob_of_the_types_lowest_value(dtype):
     """Masks of the lowest finite value: no probability beside others, uniform alone."""
