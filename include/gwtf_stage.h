@@ -83,10 +83,10 @@ typedef struct {
 
 /* Creates a handle on shape->device that enqueues on `hip_stream` (a
  * hipStream_t; NULL = the device's null stream) and allocates its workspace:
- * 16 bytes a token, max_tokens * max_hidden / 2 bytes for the embedding's
- * gradient (at most 256 MiB and at least 1 MiB), 4 bytes * max_hidden for each of
- * up to 512 workgroups of the norm's gradient and about 1 MiB for
- * gwtf_stage_logprob.  *out receives the handle, or NULL on failure. */
+ * 16 bytes a token; for the embedding's gradient up to 17 MB (2 * max_hidden
+ * bytes a token where that is less); for the norm's 2048 bytes a column, up to
+ * 34 MB; and 1.1 MB for gwtf_stage_logprob.  *out receives the handle, or NULL
+ * on failure. */
 gwtf_status_t gwtf_stage_create(const gwtf_stage_shape_t *shape, void *hip_stream, gwtf_stage_t **out);
 
 /* Frees the handle and its workspace after draining its stream; NULL-safe. */

@@ -42,16 +42,6 @@ struct DeviceScope {
     }
 };
 
-void free_ws(StageWorkspace &w)
-{
-    (void)hipFree(w.sort_a);
-    (void)hipFree(w.sort_b);
-    (void)hipFree(w.partial);
-    (void)hipFree(w.dweight);
-    (void)hipFree(w.logprob);
-    w = StageWorkspace();
-}
-
 size_t size_of(int32_t type) { return type == GWTF_TYPE_F32 ? 4 : 2; }
 bool type_ok(int32_t t) { return t == GWTF_TYPE_F32 || t == GWTF_TYPE_F16 || t == GWTF_TYPE_BF16; }
 bool token_ok(int32_t t) { return t == GWTF_TOKEN_I32 || t == GWTF_TOKEN_I64; }
@@ -107,24 +97,32 @@ extern "C" gwtf_status_t gwtf_stage_create(const gwtf_stage_shape_t *shape, void
         delete h;
         return fail(nullptr, GWTF_ERR_DEVICE, "hipDeviceGetAttribute", e);
     }
-    const size_t lp_records = size_t(kLogprobItems) * kLogprobRecord, lp_bytes = lp_records + sizeof(uint32_t) * kLogprobRows;
-    hipError_t first = hipSuccess;
-    auto take = [&](void **p, size_t bytes) {
-        if (first != hipSuccess) return;
-        if ((first = hipMalloc(p, bytes)) != hipSuccess) *p = nullptr;
+    // one allocation, its parts on 256-byte boundaries
+    const size_t lp_records = size_t(kLogprobItems) * kLogprobRecord;
+    const int64_t wide = shape->max_hidden < GWTF_STAGE_MAX_HIDDEN ? shape->max_hidden : GWTF_STAGE_MAX_HIDDEN;
+    size_t total = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = total;
+        total += (bytes + 255) / 256 * 256;
+        return at;
     };
-    take((void **)&w.sort_a, sizeof(uint64_t) * size_t(shape->max_tokens));
-    take((void **)&w.sort_b, sizeof(uint64_t) * size_t(shape->max_tokens));
-    take((void **)&w.partial, size_t(embed_partial_bytes(shape->max_tokens, shape->max_hidden)));
-    take((void **)&w.dweight, sizeof(float) * kNormGradGroups * size_t(shape->max_hidden < GWTF_STAGE_MAX_HIDDEN ? shape->max_hidden : GWTF_STAGE_MAX_HIDDEN));
-    take((void **)&w.logprob, lp_bytes);
-    if (first != hipSuccess) {
-        free_ws(w);
+    const size_t sort_a = take(sizeof(uint64_t) * size_t(shape->max_tokens));
+    const size_t sort_b = take(sizeof(uint64_t) * size_t(shape->max_tokens));
+    const size_t partial = take(size_t(embed_partial_bytes(shape->max_tokens, shape->max_hidden)));
+    const size_t dweight = take(sizeof(float) * kNormGradGroups * size_t(wide));
+    const size_t logprob = take(lp_records + sizeof(uint32_t) * kLogprobRows);
+    if ((e = hipMalloc(&w.base, total)) != hipSuccess) {
         delete h;
-        return fail(nullptr, GWTF_ERR_OUT_OF_MEMORY, "hipMalloc workspace", first);
+        return fail(nullptr, GWTF_ERR_OUT_OF_MEMORY, "hipMalloc workspace", e);
     }
+    unsigned char *const base = static_cast<unsigned char *>(w.base);
+    w.sort_a = reinterpret_cast<uint64_t *>(base + sort_a);
+    w.sort_b = reinterpret_cast<uint64_t *>(base + sort_b);
+    w.partial = reinterpret_cast<float *>(base + partial);
+    w.dweight = reinterpret_cast<float *>(base + dweight);
+    w.logprob = base + logprob;
     if ((e = hipMemsetAsync(w.logprob + lp_records, 0, sizeof(uint32_t) * kLogprobRows, h->stream)) != hipSuccess) {
-        free_ws(w);
+        (void)hipFree(w.base);
         delete h;
         return fail(nullptr, GWTF_ERR_DEVICE, "hipMemsetAsync", e);
     }
@@ -137,7 +135,7 @@ extern "C" void gwtf_stage_destroy(gwtf_stage_t *h)
     if (!h) return;
     DeviceScope scope(h->shape.device);
     if (scope.e == hipSuccess) (void)hipStreamSynchronize(h->stream);
-    free_ws(h->ws);
+    (void)hipFree(h->ws.base);
     delete h;
 }
 

@@ -60,11 +60,15 @@ __device__ __forceinline__ void store_part(T *p, int n, const typename Vec8<T>::
 }
 
 // Columns [0, n) of p as they lie in memory, the rest `fill`; n >= 8 is the
-// common case, n <= 0 reads nothing.
-template <class T>
+// common case, n <= 0 reads nothing.  STREAM: a read that leaves the caches to
+// others (see streams()).
+template <class T, bool STREAM = false>
 __device__ __forceinline__ typename Vec8<T>::type load8_raw(const T *p, int64_t n, T fill = T(0.f))
 {
-    if (n >= kVec) return *reinterpret_cast<const typename Vec8<T>::type *>(p);
+    if (n >= kVec) {
+        if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const typename Vec8<T>::type *>(p));
+        else return *reinterpret_cast<const typename Vec8<T>::type *>(p);
+    }
     return load_part(p, n > 0 ? int(n) : 0, fill);
 }
 
@@ -77,21 +81,25 @@ __device__ __forceinline__ void widen(const typename Vec8<T>::type &raw, float v
 }
 
 // The same in 32 bits.
-template <class T>
+template <class T, bool STREAM = false>
 __device__ __forceinline__ void load8(const T *p, int64_t n, float v[8], float fill = 0.f)
 {
-    widen<T>(load8_raw(p, n, T(fill)), v);
+    widen<T>(load8_raw<T, STREAM>(p, n, T(fill)), v);
 }
 
-template <class T>
+template <class T, bool STREAM = false>
 __device__ __forceinline__ void store8(T *p, int64_t n, const float v[8])
 {
     f32x8 f;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) f[i] = v[i];
     const typename Vec8<T>::type r = __builtin_convertvector(f, typename Vec8<T>::type);
-    if (n >= kVec) *reinterpret_cast<typename Vec8<T>::type *>(p) = r;
-    else if (n > 0) store_part(p, int(n), r);
+    if (n >= kVec) {
+        if constexpr (STREAM) __builtin_nontemporal_store(r, reinterpret_cast<typename Vec8<T>::type *>(p));
+        else *reinterpret_cast<typename Vec8<T>::type *>(p) = r;
+    } else if (n > 0) {
+        store_part(p, int(n), r);
+    }
 }
 
 __device__ __forceinline__ int64_t load_token(const void *t, int is64, int64_t i)

@@ -44,7 +44,7 @@ __device__ __forceinline__ void philox4x32(uint32_t k0, uint32_t k1, uint32_t c[
 // Steps of eight columns a thread takes, with their reads side by side.
 constexpr uint32_t kUnits = 2;
 
-template <class T, bool RES>
+template <class T, bool RES, bool STREAM>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutParams p)
 {
     const uint32_t u0 = blockIdx.x * (256u * kUnits) + threadIdx.x;
@@ -58,8 +58,8 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutParams p)
         step[q] = (u < p.units ? u : 0) - r * p.steps.d;
         row[q] = p.row0 + r;
         const int64_t col = int64_t(step[q]) * kVec, n = p.H - col;
-        raw[q] = load8_raw(static_cast<const T *>(p.x) + row[q] * p.xs + col, n);
-        if constexpr (RES) rraw[q] = load8_raw(static_cast<const T *>(p.res) + row[q] * p.rs + col, n);
+        raw[q] = load8_raw<T, STREAM>(static_cast<const T *>(p.x) + row[q] * p.xs + col, n);
+        if constexpr (RES) rraw[q] = load8_raw<T, STREAM>(static_cast<const T *>(p.res) + row[q] * p.rs + col, n);
         id[q] = p.rows ? uint64_t(p.rows[row[q]]) : uint64_t(row[q]);
     }
 #pragma unroll
@@ -101,13 +101,16 @@ hipError_t run(const gwtf_stage_dropout_t &a, uint32_t limit, hipStream_t s)
     p.site = a.site;
     p.limit = limit;
     p.keep_scale = 65536.f / float(65536 - limit);
+    const bool stream = streams(a.x, a.x_stride, a.num_tokens, a.hidden, sizeof(T)) &&
+                        (!a.residual || streams(a.residual, a.residual_stride, a.num_tokens, a.hidden, sizeof(T)));
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
         p.row0 = r;
         p.units = uint32_t(n * steps);
         const dim3 grid((p.units + 256 * kUnits - 1) / (256 * kUnits));
-        if (p.res) dropout_kernel<T, true><<<grid, dim3(256), 0, s>>>(p);
-        else dropout_kernel<T, false><<<grid, dim3(256), 0, s>>>(p);
+        auto kernel = p.res ? (stream ? dropout_kernel<T, true, true> : dropout_kernel<T, true, false>)
+                            : (stream ? dropout_kernel<T, false, true> : dropout_kernel<T, false, false>);
+        kernel<<<grid, dim3(256), 0, s>>>(p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -68,7 +68,7 @@ __device__ __forceinline__ void quantise(float y[8], float s)
     }
 }
 
-template <class T, int K, int WAVES>
+template <class T, int K, int WAVES, bool STREAM>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwtf_stage_norm_t p)
 {
     __shared__ float red[WAVES];
@@ -86,10 +86,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwt
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int col = ((k * WAVES + part) * 64 + lane) * kVec;
-        load8(x + col, H - col, h[k]);
+        load8<T, STREAM>(x + col, H - col, h[k]);
         if (p.residual) {
             float r[8];
-            load8(res + col, H - col, r);
+            load8<T, STREAM>(res + col, H - col, r);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) h[k][i] += r[i];
         }
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwt
 
 // Every workgroup takes the rows blockIdx.x, blockIdx.x + gridDim.x, .. (four
 // at a time with one wave a row) and keeps its sum of dweight in registers.
-template <class T, int K, int WAVES>
+template <class T, int K, int WAVES, bool STREAM>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_grad_kernel(gwtf_stage_norm_grad_t p, float *partial)
 {
     __shared__ float red[2][WAVES];
@@ -178,9 +178,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_grad_kerne
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int col = ((k * WAVES + part) * 64 + lane) * kVec;
-            rdy[k] = load8_raw(dy + col, H - col);
-            rh[k] = load8_raw(hp + col, H - col);
-            if (p.dh) rd[k] = load8_raw(dh + col, H - col);
+            rdy[k] = load8_raw<T, STREAM>(dy + col, H - col);
+            rh[k] = load8_raw<T, STREAM>(hp + col, H - col);
+            if (p.dh) rd[k] = load8_raw<T, STREAM>(dh + col, H - col);
         }
     };
     int turn = 0;
@@ -280,7 +280,10 @@ template <class T, int K, int WAVES>
 hipError_t run_norm(const gwtf_stage_norm_t &a, hipStream_t s)
 {
     const int64_t rows = WAVES == 1 ? 4 : 1;
-    norm_kernel<T, K, WAVES><<<dim3(uint32_t((a.num_tokens + rows - 1) / rows)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a);
+    const bool stream = streams(a.x, a.x_stride, a.num_tokens, a.hidden, sizeof(T)) &&
+                        (!a.residual || streams(a.residual, a.residual_stride, a.num_tokens, a.hidden, sizeof(T)));
+    auto kernel = stream ? norm_kernel<T, K, WAVES, true> : norm_kernel<T, K, WAVES, false>;
+    kernel<<<dim3(uint32_t((a.num_tokens + rows - 1) / rows)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -290,8 +293,11 @@ hipError_t run_norm_grad(const gwtf_stage_norm_grad_t &a, const StageWorkspace &
     const int64_t rows = WAVES == 1 ? 4 : 1;
     int64_t groups = (a.num_tokens + rows - 1) / rows;
     if (groups > kNormGradGroups) groups = kNormGradGroups;
-    norm_grad_kernel<T, K, WAVES>
-        <<<dim3(uint32_t(groups)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a, a.dweight ? w.dweight : nullptr);
+    const bool stream = streams(a.dy, a.dy_stride, a.num_tokens, a.hidden, sizeof(T)) &&
+                        streams(a.h, a.h_stride, a.num_tokens, a.hidden, sizeof(T)) &&
+                        (!a.dh || streams(a.dh, a.dh_stride, a.num_tokens, a.hidden, sizeof(T)));
+    auto kernel = stream ? norm_grad_kernel<T, K, WAVES, true> : norm_grad_kernel<T, K, WAVES, false>;
+    kernel<<<dim3(uint32_t(groups)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a, a.dweight ? w.dweight : nullptr);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.dweight) return e;
     dweight_kernel<<<dim3(uint32_t((a.hidden + 15) / 16)), dim3(1024), 0, s>>>(w.dweight, int(groups), int(a.hidden), a.dweight);
