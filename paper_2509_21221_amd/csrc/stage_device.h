@@ -87,6 +87,37 @@ __device__ __forceinline__ void load8(const T *p, int64_t n, float v[8], float f
     widen<T>(load8_raw<T, STREAM>(p, n, T(fill)), v);
 }
 
+// Columns [col, col + 8) of a row of `width`, for reads that are to be in
+// flight for long: a row's last ones come with the columns before them, in one
+// access like all others, and columns_of() puts them into place when they are
+// needed.  (Put together from parts here, they would be waited for at once.)
+// WIDE: the caller knows that the width is 8 at least.
+template <class T, bool STREAM = false, bool WIDE = false>
+__device__ __forceinline__ typename Vec8<T>::type load_columns(const T *row, int64_t col, int64_t width)
+{
+    if (!WIDE && width < kVec) return load_part(row, col == 0 ? int(width) : 0, T(0.f));
+    return load8_raw<T, STREAM>(row + (col + kVec <= width ? col : width - kVec), kVec);
+}
+// Whether any lane of the wave has columns past the row's end (uniform).
+__device__ __forceinline__ bool ends_within(int64_t col, int64_t width) { return __ballot(col + kVec > width) != 0; }
+template <class T>
+__device__ __forceinline__ void columns_of(const typename Vec8<T>::type &raw, bool ends, int64_t col, int64_t width, float v[8])
+{
+    widen<T>(raw, v);
+    if (!ends || width < kVec) return;
+    const int over = int(col + kVec - width > 0 ? col + kVec - width : 0);
+#pragma unroll
+    for (int step = 4; step > 0; step >>= 1) {
+        const bool move = over >= kVec || (over & step);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = move ? (i + step < kVec ? v[i + step] : 0.f) : v[i];
+    }
+    if (over >= kVec) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = 0.f;
+    }
+}
+
 template <class T, bool STREAM = false>
 __device__ __forceinline__ void store8(T *p, int64_t n, const float v[8])
 {

@@ -57,9 +57,9 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutParams p)
         const uint32_t u = u0 + q * 256u, r = p.steps.div(u < p.units ? u : 0);
         step[q] = (u < p.units ? u : 0) - r * p.steps.d;
         row[q] = p.row0 + r;
-        const int64_t col = int64_t(step[q]) * kVec, n = p.H - col;
-        raw[q] = load8_raw<T, STREAM>(static_cast<const T *>(p.x) + row[q] * p.xs + col, n);
-        if constexpr (RES) rraw[q] = load8_raw<T, STREAM>(static_cast<const T *>(p.res) + row[q] * p.rs + col, n);
+        const int64_t col = int64_t(step[q]) * kVec;
+        raw[q] = load_columns<T, STREAM>(static_cast<const T *>(p.x) + row[q] * p.xs, col, p.H);
+        if constexpr (RES) rraw[q] = load_columns<T, STREAM>(static_cast<const T *>(p.res) + row[q] * p.rs, col, p.H);
         id[q] = p.rows ? uint64_t(p.rows[row[q]]) : uint64_t(row[q]);
     }
 #pragma unroll
@@ -67,15 +67,16 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutParams p)
         uint32_t c[4] = {step[q], p.site, uint32_t(id[q]), uint32_t(id[q] >> 32)};
         philox4x32(p.k0, p.k1, c);
         float v[8], res[8];
-        widen<T>(raw[q], v);
-        if constexpr (RES) widen<T>(rraw[q], res);
+        const int64_t col = int64_t(step[q]) * kVec;
+        const bool ends = ends_within(col, p.H);
+        columns_of<T>(raw[q], ends, col, p.H, v);
+        if constexpr (RES) columns_of<T>(rraw[q], ends, col, p.H, res);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             const uint32_t bits = (i & 1) ? c[i / 2] >> 16 : c[i / 2] & 0xffffu;
             v[i] = bits >= p.limit ? v[i] * p.keep_scale : 0.f;
             if constexpr (RES) v[i] += res[i];
         }
-        const int64_t col = int64_t(step[q]) * kVec;
         if (u0 + q * 256u < p.units) store8(static_cast<T *>(p.out) + row[q] * p.os + col, p.H - col, v);
     }
 }

@@ -305,17 +305,17 @@ __device__ __forceinline__ void write_grad(const gwtf_stage_embed_grad_t &a, int
     store8(g, n, v);
 }
 
-// One chunk and slab.  FULL: the slab has all of its 512 columns, so that
-// reads stand side by side with no branch between them.  Lane l holds the key
-// of entry l of 64; two batches of rows are in flight.
-template <class T, class G, bool FULL, bool STREAM>
+// One chunk and slab.  Lane l holds the key of entry l of 64; two batches of
+// rows are in flight.
+template <class T, class G, bool STREAM>
 __device__ __forceinline__ void sum_chunk(const EmbedGradParams &p, int64_t c, int64_t slab_col, int lane)
 {
     const gwtf_stage_embed_grad_t &a = p.a;
     constexpr int U = kRowsInFlight * 2 / int(sizeof(T));
-    const int64_t N = a.num_tokens, col = slab_col + lane * kVec, n = FULL ? kVec : a.hidden - col;
+    const int64_t N = a.num_tokens, col = slab_col + lane * kVec, n = a.hidden - col;
     const int64_t e0 = c * p.chunk, e1 = e0 + p.chunk < N ? e0 + p.chunk : N;
-    const T *dout = static_cast<const T *>(a.dout) + col;
+    const T *dout = static_cast<const T *>(a.dout);
+    const bool ends = ends_within(col, a.hidden);
     // tokens just outside the chunk, with the keys of its first entries
     const uint64_t before_key = e0 > 0 ? p.sorted[e0 - 1] : ~uint64_t(0), after_key = e1 < N ? p.sorted[e1] : ~uint64_t(0);
     uint64_t mine = p.sorted[e0 + lane < e1 ? e0 + lane : e1 - 1];
@@ -332,9 +332,7 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradParams &p, int64_t c, i
 #pragma unroll
             for (int q = 0; q < U; ++q) {
                 const uint32_t pos = __builtin_amdgcn_readlane(int(uint32_t(mine)), (at + q) & 63); // entries past the end read the last row
-                const T *r = dout + int64_t(pos) * a.dout_stride;
-                if constexpr (FULL) row[q] = load8_raw<T, STREAM>(r, kVec);
-                else row[q] = load8_raw(r, n);
+                row[q] = load_columns<T, STREAM>(dout + int64_t(pos) * a.dout_stride, col, a.hidden);
             }
         };
         fetch(0, v);
@@ -353,7 +351,8 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradParams &p, int64_t c, i
 #pragma unroll
                     for (int i = 0; i < kVec; ++i) acc[i] = 0.f;
                 }
-                const f32x8 f = __builtin_convertvector(v[q], f32x8);
+                float f[8];
+                columns_of<T>(v[q], ends, col, a.hidden, f);
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) acc[i] += f[i];
             }
@@ -397,9 +396,8 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradParams p)
     }
     const int64_t item = int64_t(blockIdx.x) * 4 + wave, c = item / p.slabs, slab_col = (item - c * p.slabs) * 512;
     if (c >= p.chunks) return;
-    if (slab_col + 512 > a.hidden) sum_chunk<T, G, false, false>(p, c, slab_col, lane);
-    else if (p.stream) sum_chunk<T, G, true, true>(p, c, slab_col, lane);
-    else sum_chunk<T, G, true, false>(p, c, slab_col, lane);
+    if (p.stream) sum_chunk<T, G, true>(p, c, slab_col, lane);
+    else sum_chunk<T, G, false>(p, c, slab_col, lane);
 }
 
 // Runs that cross chunks, each by the wave of the chunk in which it begins.
@@ -426,28 +424,21 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradParams p)
         if (run < 64) break;
     }
     const int64_t slab_col = (item - c * p.slabs) * 512, col = slab_col + lane * kVec, n = a.hidden - col;
-    if (n <= 0) return;
     float acc[8];
     load8(p.partial + (c * 2 + 1) * a.hidden + col, n, acc);
-    const float *next_part = p.partial + (c + 1) * 2 * a.hidden + col;
-    if (slab_col + 512 <= a.hidden) {
-        for (int64_t d = 0; d < more; d += kPartsInFlight) {
-            Vec8<float>::type v[kPartsInFlight];
+    const bool ends = ends_within(col, a.hidden);
+    const float *next_part = p.partial + (c + 1) * 2 * a.hidden;
+    for (int64_t d = 0; d < more; d += kPartsInFlight) {
+        Vec8<float>::type v[kPartsInFlight];
 #pragma unroll
-            for (int q = 0; q < kPartsInFlight; ++q)
-                v[q] = *reinterpret_cast<const Vec8<float>::type *>(next_part + (d + q < more ? d + q : more - 1) * 2 * a.hidden);
+        for (int q = 0; q < kPartsInFlight; ++q)
+            v[q] = load_columns(next_part + (d + q < more ? d + q : more - 1) * 2 * a.hidden, col, a.hidden);
 #pragma unroll
-            for (int q = 0; q < kPartsInFlight; ++q) {
+        for (int q = 0; q < kPartsInFlight; ++q) {
+            float f[8];
+            columns_of<float>(v[q], ends, col, a.hidden, f);
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) acc[i] += d + q < more ? v[q][i] : 0.f;
-            }
-        }
-    } else {
-        for (int64_t d = 0; d < more; ++d) {
-            float v[8];
-            load8(next_part + d * 2 * a.hidden, n, v);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) acc[i] += v[i];
+            for (int i = 0; i < kVec; ++i) acc[i] += d + q < more ? f[i] : 0.f;
         }
     }
     write_grad<G>(a, token, col, n, acc);

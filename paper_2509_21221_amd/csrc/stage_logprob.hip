@@ -57,23 +57,17 @@ __device__ __forceinline__ Softmax join(const Softmax &a, const Softmax &b)
     return r;
 }
 
-template <int n>
-__device__ __forceinline__ Softmax row_ror(const Softmax &a)
-{
-    return {gwtf::row_ror<n>(a.m), gwtf::row_ror<n>(a.s), gwtf::row_ror<n>(a.t)};
-}
-__device__ __forceinline__ Softmax lane_of(const Softmax &a, int lane)
-{
-    return {lane_value(a.m, lane), lane_value(a.s, lane), lane_value(a.t, lane)};
-}
+// All lanes' parts, in every lane: each is rescaled once, then they add up.
 template <bool WIDE>
-__device__ __forceinline__ Softmax wave_join(Softmax a)
+__device__ __forceinline__ Softmax wave_join(const Softmax &a)
 {
-    a = join<WIDE>(a, row_ror<8>(a));
-    a = join<WIDE>(a, row_ror<4>(a));
-    a = join<WIDE>(a, row_ror<2>(a));
-    a = join<WIDE>(a, row_ror<1>(a));
-    return join<WIDE>(join<WIDE>(lane_of(a, 0), lane_of(a, 16)), join<WIDE>(lane_of(a, 32), lane_of(a, 48)));
+    float m = fmaxf(a.m, row_ror<8>(a.m));
+    m = fmaxf(m, row_ror<4>(m));
+    m = fmaxf(m, row_ror<2>(m));
+    m = fmaxf(m, row_ror<1>(m));
+    m = fmaxf(fmaxf(lane_value(m, 0), lane_value(m, 16)), fmaxf(lane_value(m, 32), lane_value(m, 48)));
+    const float d = (a.m - finite_or_zero(m)) * (WIDE ? kLog2e : 1.f), e = exp2_(d);
+    return {m, wave_sum(a.s * e), wave_sum(e * (a.t + fmaxf(d, kLowest) * a.s))};
 }
 
 // A lane's 16 columns; `x_max`: their largest with the lane's former ones.
@@ -182,36 +176,41 @@ struct TopList {
         const uint32_t b = fold(__builtin_amdgcn_readlane(w, 32), __builtin_amdgcn_readlane(w, 48), top <= 2);
         return fold(a, b, top <= 1);
     }
-    // The largest of M keys a lane, into an empty list: those that reach a
-    // bound, mostly no more than 64, join at once.  Where many share the
-    // bound's order, their indices give a second one.
+    // Puts the keys from `least` on into the slots; returns their number.
     template <int M>
-    __device__ __forceinline__ void select(const uint64_t (&k)[M])
+    __device__ __forceinline__ int gather(const uint64_t (&k)[M], int m, uint64_t least) const
+    {
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            if (i >= m) break;
+            const bool in = k[i] != 0 && k[i] >= least;
+            const uint64_t some = __ballot(in);
+            const int place = count + __builtin_amdgcn_mbcnt_hi(uint32_t(some >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(some), 0));
+            if (in && place < kSlots) slots[place] = k[i];
+            count += __popcll(some);
+        }
+        return count;
+    }
+    // The largest of the first m of M keys a lane, into an empty list: those
+    // that reach a bound, mostly no more than 64, join at once.  Where many
+    // share the bound's order, their indices give a second one.
+    template <int M>
+    __device__ __forceinline__ void select(const uint64_t (&k)[M], int m = M)
     {
         const int lane = __lane_id();
         uint32_t best = 0;
 #pragma unroll
         for (int i = 0; i < M; ++i) best = umax(best, key_order(k[i]));
         const uint32_t order = bound_of(best);
-        int count = 0;
-#pragma unroll
-        for (int i = 0; i < M; ++i) count += __popcll(__ballot(k[i] != 0 && key_order(k[i]) >= order));
-        uint64_t least = uint64_t(order) << 32;
+        int count = gather(k, m, uint64_t(order) << 32);
         if (count > kSlots) {
             best = 0;
 #pragma unroll
             for (int i = 0; i < M; ++i)
                 best = umax(best, key_order(k[i]) > order ? 0xffffffffu : key_order(k[i]) == order ? uint32_t(k[i]) : 0u);
-            least |= bound_of(best);
-        }
-        count = 0;
-#pragma unroll
-        for (int i = 0; i < M; ++i) {
-            const bool in = k[i] != 0 && k[i] >= least;
-            const uint64_t some = __ballot(in);
-            const int place = count + __popcll(some & ((uint64_t(1) << lane) - 1));
-            if (in && place < kSlots) slots[place] = k[i];
-            count += __popcll(some);
+            wave_sync();
+            count = gather(k, m, uint64_t(order) << 32 | bound_of(best));
         }
         if (count <= kSlots) {
             wave_sync();
@@ -354,7 +353,7 @@ __device__ __forceinline__ void resolve_units(TopList &list, const TopList &unit
         k[q] = v[q] == v[q] ? key_of(order_of(v[q]), at[q]) : 0;
         if (key_order(k[q]) < least) k[q] = 0;
     }
-    list.select(k);
+    list.select(k, (units.top * kUnit + 63) / 64);
 }
 
 // Offers the entries of every unit of those lanes whose two units are both in
@@ -464,7 +463,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
                 for (int i = 0; i < 2 * kLpWaves; ++i) k[i] = units_of[i * 64 + lane];
                 wave_sync();
                 list.start(a.top, slots);
-                list.select(k);
+                list.select(k, c1 - c0 > kStep ? 2 * kLpWaves : kLpWaves); // one step: no second units
                 again = list.last == 0;
                 if (!again) {
                     const TopList units = list;
@@ -499,7 +498,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
         alive[wave] = some;
     }
     __syncthreads();
-    r = join<false>(join<false>(parts[0], parts[1]), join<false>(parts[2], parts[3]));
+    r = wave_join<false>(lane < kLpWaves ? parts[lane] : Softmax{kNone, 0.f, 0.f});
     bool live = alive[0] | alive[1] | alive[2] | alive[3];
     if (p.segments > 1) {
         // The workgroup that arrives last joins the row's records.  Records and
@@ -548,7 +547,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
                         k[q] = i < all ? get_key(reinterpret_cast<const uint64_t *>(records + seg * kLogprobRecord + 16) + (i - seg * a.top)) : 0;
                     }
                     if (i0 == 0) {
-                        list.select(k);
+                        list.select(k, (all + 63) / 64);
                     } else {
 #pragma unroll
                         for (int q = 0; q < kBatch; ++q) list.offer(k[q]);
@@ -565,7 +564,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
         if (lane == 0) parts[wave] = r;
         __syncthreads();
         if (wave != chief) return;
-        r = join<true>(join<true>(parts[0], parts[1]), join<true>(parts[2], parts[3]));
+        r = wave_join<true>(lane < kLpWaves ? parts[lane] : Softmax{kNone, 0.f, 0.f});
         finish_row<true>(a, row, r, list, there, xt);
     } else if (wave == chief) {
         finish_row<false>(a, row, r, list, there, xt);

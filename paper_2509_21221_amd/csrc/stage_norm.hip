@@ -68,7 +68,7 @@ __device__ __forceinline__ void quantise(float y[8], float s)
     }
 }
 
-template <class T, int K, int WAVES, bool STREAM>
+template <class T, int K, int WAVES, bool STREAM, bool WIDE>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwtf_stage_norm_t p)
 {
     __shared__ float red[WAVES];
@@ -83,19 +83,24 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwt
     const int H = int(p.hidden);
 
     float h[K][8], sq = 0.f;
+    typename Vec8<T>::type rx[K], rres[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int col = ((k * WAVES + part) * 64 + lane) * kVec;
-        load8<T, STREAM>(x + col, H - col, h[k]);
-        if (p.residual) {
-            float r[8];
-            load8<T, STREAM>(res + col, H - col, r);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) h[k][i] += r[i];
-        }
+        rx[k] = load_columns<T, STREAM, WIDE>(x, col, H);
+        if (p.residual) rres[k] = load_columns<T, STREAM, WIDE>(res, col, H);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
+        const int col = ((k * WAVES + part) * 64 + lane) * kVec;
+        const bool ends = ends_within(col, H);
+        columns_of<T>(rx[k], ends, col, H, h[k]);
+        if (p.residual) {
+            float r[8];
+            columns_of<T>(rres[k], ends, col, H, r);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) h[k][i] += r[i];
+        }
 #pragma unroll
         for (int i = 0; i < kVec; ++i) sq += h[k][i] * h[k][i];
     }
@@ -150,7 +155,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwt
 
 // Every workgroup takes the rows blockIdx.x, blockIdx.x + gridDim.x, .. (four
 // at a time with one wave a row) and keeps its sum of dweight in registers.
-template <class T, int K, int WAVES, bool STREAM>
+template <class T, int K, int WAVES, bool STREAM, bool WIDE>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_grad_kernel(gwtf_stage_norm_grad_t p, float *partial)
 {
     __shared__ float red[2][WAVES];
@@ -161,47 +166,68 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_grad_kerne
     const int H = int(p.hidden);
     const T *weight = static_cast<const T *>(p.weight);
     float w[K][8], dw[K][8];
+    bool ends[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int col = ((k * WAVES + part) * 64 + lane) * kVec;
         load8(weight + col, H - col, w[k]);
+        ends[k] = ends_within(col, H);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) dw[k][i] = 0.f;
     }
-    typename Vec8<T>::type rdy[K], rh[K], rd[K];
-    float rrstd = 0.f;
-    auto fetch = [&](int64_t row) {
+    // Rows on their way while one is reduced and written: two where a lane has
+    // eight columns, one where it has sixteen, none with 16 waves, whose
+    // registers would spill.
+    constexpr bool AHEAD = WAVES < 16;
+    constexpr int DEPTH = K == 1 ? 2 : 1;
+    typename Vec8<T>::type rdy[DEPTH][K], rh[DEPTH][K], rd[DEPTH][K];
+    float rrstd[DEPTH];
+    const int64_t stride = int64_t(gridDim.x) * rows_at_once;
+    auto fetch = [&](int64_t row, int slot) {
+        if (row >= p.num_tokens) return;
         const T *dy = static_cast<const T *>(p.dy) + row * p.dy_stride;
         const T *hp = static_cast<const T *>(p.h) + row * p.h_stride;
         const T *dh = static_cast<const T *>(p.dh) + row * p.dh_stride;
-        rrstd = p.rstd[row];
+        rrstd[slot] = p.rstd[row];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int col = ((k * WAVES + part) * 64 + lane) * kVec;
-            rdy[k] = load8_raw<T, STREAM>(dy + col, H - col);
-            rh[k] = load8_raw<T, STREAM>(hp + col, H - col);
-            if (p.dh) rd[k] = load8_raw<T, STREAM>(dh + col, H - col);
+            rdy[slot][k] = load_columns<T, STREAM, WIDE>(dy, col, H);
+            rh[slot][k] = load_columns<T, STREAM, WIDE>(hp, col, H);
+            if (p.dh) rd[slot][k] = load_columns<T, STREAM, WIDE>(dh, col, H);
         }
     };
     int turn = 0;
     int64_t row = blockIdx.x * rows_at_once + mine;
-    if (row < p.num_tokens) fetch(row);
-    for (; row < p.num_tokens; row += gridDim.x * rows_at_once, turn ^= 1) {
-        const float rstd = rrstd;
+#pragma unroll
+    for (int q = 0; q < (AHEAD ? DEPTH : 0); ++q) fetch(row + q * stride, q);
+    for (; row < p.num_tokens; row += stride, turn ^= 1) {
+        if constexpr (!AHEAD) fetch(row, 0);
+        const float rstd = rrstd[0];
         float g[K][8], xh[K][8], d[K][8], c = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            widen<T>(rdy[k], g[k]);
-            widen<T>(rh[k], xh[k]);
+            const int col = ((k * WAVES + part) * 64 + lane) * kVec;
+            columns_of<T>(rdy[0][k], ends[k], col, H, g[k]);
+            columns_of<T>(rh[0][k], ends[k], col, H, xh[k]);
             if (p.dh) {
-                widen<T>(rd[k], d[k]);
+                columns_of<T>(rd[0][k], ends[k], col, H, d[k]);
             } else {
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) d[k][i] = 0.f;
             }
         }
-        // the next row is on its way while this one is reduced and written
-        if (row + int64_t(gridDim.x) * rows_at_once < p.num_tokens) fetch(row + int64_t(gridDim.x) * rows_at_once);
+#pragma unroll
+        for (int q = 0; q + 1 < DEPTH; ++q) {
+            rrstd[q] = rrstd[q + 1];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                rdy[q][k] = rdy[q + 1][k];
+                rh[q][k] = rh[q + 1][k];
+                rd[q][k] = rd[q + 1][k];
+            }
+        }
+        if constexpr (AHEAD) fetch(row + DEPTH * stride, DEPTH - 1);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
 #pragma unroll
@@ -282,7 +308,8 @@ hipError_t run_norm(const gwtf_stage_norm_t &a, hipStream_t s)
     const int64_t rows = WAVES == 1 ? 4 : 1;
     const bool stream = streams(a.x, a.x_stride, a.num_tokens, a.hidden, sizeof(T)) &&
                         (!a.residual || streams(a.residual, a.residual_stride, a.num_tokens, a.hidden, sizeof(T)));
-    auto kernel = stream ? norm_kernel<T, K, WAVES, true> : norm_kernel<T, K, WAVES, false>;
+    auto kernel = stream ? norm_kernel<T, K, WAVES, true, true> : norm_kernel<T, K, WAVES, false, true>;
+    if (K == 1 && WAVES == 1 && a.hidden < kVec) kernel = norm_kernel<T, 1, 1, false, false>;
     kernel<<<dim3(uint32_t((a.num_tokens + rows - 1) / rows)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a);
     return hipGetLastError();
 }
@@ -296,7 +323,8 @@ hipError_t run_norm_grad(const gwtf_stage_norm_grad_t &a, const StageWorkspace &
     const bool stream = streams(a.dy, a.dy_stride, a.num_tokens, a.hidden, sizeof(T)) &&
                         streams(a.h, a.h_stride, a.num_tokens, a.hidden, sizeof(T)) &&
                         (!a.dh || streams(a.dh, a.dh_stride, a.num_tokens, a.hidden, sizeof(T)));
-    auto kernel = stream ? norm_grad_kernel<T, K, WAVES, true> : norm_grad_kernel<T, K, WAVES, false>;
+    auto kernel = stream ? norm_grad_kernel<T, K, WAVES, true, true> : norm_grad_kernel<T, K, WAVES, false, true>;
+    if (K == 1 && WAVES == 1 && a.hidden < kVec) kernel = norm_grad_kernel<T, 1, 1, false, false>;
     kernel<<<dim3(uint32_t(groups)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a, a.dweight ? w.dweight : nullptr);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.dweight) return e;

@@ -562,6 +562,8 @@ def test_refusals():
             (GwtfError, lambda: s.norm(x, w, eps=float("nan"))),
             (ValueError, lambda: s.norm_grad(x, x, w, w)),
             (GwtfError, lambda: s.logprob(x[:, :8].contiguous(), t, top=9)),
+            (ValueError, lambda: s.logprob(x[:, :8].contiguous(), t, top=-1)),
+            (ValueError, lambda: s.logprob(x[:, :8].contiguous(), t, top=65)),
             (GwtfError, lambda: s.logprob(x, t)),
             (ValueError, lambda: s.logprob(x[:, :8], t[:2])),
             (ValueError, lambda: s.logprob_grad(x[:, :8], None, w[:4].contiguous(), dlogp=w[:4].contiguous())),
