@@ -102,8 +102,8 @@ hipError_t run(const gwtf_stage_dropout_t &a, uint32_t limit, hipStream_t s)
     p.site = a.site;
     p.limit = limit;
     p.keep_scale = 65536.f / float(65536 - limit);
-    const bool stream = streams(a.x, a.x_stride, a.num_tokens, a.hidden, sizeof(T)) &&
-                        (!a.residual || streams(a.residual, a.residual_stride, a.num_tokens, a.hidden, sizeof(T)));
+    const bool stream = a.num_tokens * a.hidden * int64_t(sizeof(T)) * (a.residual ? 3 : 2) >= kMemoryCacheBytes &&
+                        on_lines(a.x, a.x_stride, sizeof(T)) && (!a.residual || on_lines(a.residual, a.residual_stride, sizeof(T)));
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
         p.row0 = r;

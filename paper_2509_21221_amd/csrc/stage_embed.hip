@@ -51,10 +51,12 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p)
 //
 // Most of the gradient's bytes are zeros that depend on nothing but which
 // tokens are there, so they are written beside the sorting, whose few
-// workgroups leave the memory idle: each of kFillGroups workgroups looks
-// through all tokens for those of its own rows.
+// workgroups leave the memory idle: each of the other workgroups that fit on
+// the device with them looks through all tokens for those of its own rows,
+// every so many of the table, so that all have as many absent ones.  (32,000 x
+// 4096 bf16 and 16,384 tokens, rows side by side and 64 workgroups more than
+// fit: 51 us in both launches, against 37.)
 
-constexpr int kFillGroups = 512;
 constexpr int kFillRows = 4096;           // most rows of one workgroup
 constexpr int64_t kFillTokens = 32768;    // with more tokens a look through them costs more than the sort hides:
                                           // then embed_grad_kernel writes the zeros
@@ -65,7 +67,7 @@ struct FillParams {
     const void *tokens;
     int64_t N, v0, v1; // rows [v0, v1)
     int32_t token_type, wide; // wide: 32-bit gradient
-    int32_t rows;      // of one workgroup
+    FastDiv groups;    // row v0 + r belongs to workgroup r % groups
     int32_t stream;
 };
 
@@ -89,9 +91,9 @@ __device__ __forceinline__ void zero_row(char *g, int64_t bytes)
 template <int THREADS>
 __device__ void fill_absent(const FillParams &p, int group, uint32_t *there /* [kFillRows / 32] */)
 {
-    const int64_t first = p.v0 + int64_t(group) * p.rows;
-    const int rows = int(p.v1 - first < p.rows ? p.v1 - first : p.rows);
-    for (int i = threadIdx.x; i < (p.rows + 31) / 32; i += THREADS) there[i] = 0;
+    const uint32_t groups = p.groups.d, all = uint32_t(p.v1 - p.v0);
+    const int rows = int((all + groups - 1 - group) / groups);
+    for (int i = threadIdx.x; i < (rows + 31) / 32; i += THREADS) there[i] = 0;
     __syncthreads();
     for (int64_t i = threadIdx.x; i < p.N; i += 8 * THREADS) {
         int64_t t[8];
@@ -99,15 +101,17 @@ __device__ void fill_absent(const FillParams &p, int group, uint32_t *there /* [
         for (int q = 0; q < 8; ++q) t[q] = i + q * THREADS < p.N ? load_token(p.tokens, p.token_type, i + q * THREADS) : -1;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const uint64_t r = uint64_t(t[q] - first);
-            if (t[q] >= 0 && r < uint64_t(rows)) atomicOr(&there[r >> 5], 1u << (r & 31));
+            const uint64_t r = uint64_t(t[q] - p.v0);
+            if (t[q] < 0 || r >= all) continue;
+            const uint32_t own = p.groups.div(uint32_t(r));
+            if (uint32_t(r) - own * groups == uint32_t(group)) atomicOr(&there[own >> 5], 1u << (own & 31));
         }
     }
     __syncthreads();
     const int64_t size = p.wide ? 4 : 2;
     for (int r = threadIdx.x >> 6; r < rows; r += THREADS / 64)
         if (!(there[r >> 5] >> (r & 31) & 1)) {
-            char *row = static_cast<char *>(p.grad) + (first + r) * p.stride * size;
+            char *row = static_cast<char *>(p.grad) + (p.v0 + group + int64_t(r) * groups) * p.stride * size;
             if (p.stream) zero_row<true>(row, p.hidden * size);
             else zero_row<false>(row, p.hidden * size);
         }
@@ -448,7 +452,8 @@ template <class T>
 hipError_t run_embed(const gwtf_stage_embed_t &a, hipStream_t s)
 {
     const int64_t steps = (a.hidden + kVec - 1) / kVec, slab = (int64_t(1) << 30) / steps;
-    auto kernel = streams(a.out, a.out_stride, a.num_tokens, a.hidden, sizeof(T)) ? embed_kernel<T, true> : embed_kernel<T, false>;
+    const bool stream = 2 * a.num_tokens * a.hidden * int64_t(sizeof(T)) >= kMemoryCacheBytes && on_lines(a.out, a.out_stride, sizeof(T));
+    auto kernel = stream ? embed_kernel<T, true> : embed_kernel<T, false>;
     EmbedParams p;
     p.a = a;
     p.steps = FastDiv::make(uint32_t(steps));
@@ -479,32 +484,37 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
     EmbedGradParams p;
     p.a = a;
     p.sorted = w.sort_a;
-    p.stream = N > 0 && streams(a.dout, a.dout_stride, N, a.hidden, sizeof(T));
+    const bool large = ((a.accumulate ? 0 : a.vocab) * int64_t(sizeof(G)) + N * int64_t(sizeof(T))) * a.hidden >= kMemoryCacheBytes;
+    p.stream = large && on_lines(a.dout, a.dout_stride, sizeof(T));
     p.partial = w.partial;
     p.chunk = chunk_of(N, a.hidden);
     p.chunks = (N + p.chunk - 1) / p.chunk;
     p.slabs = int(slabs_of(a.hidden));
     // zeros beside the sort, half of them beside the merge where there is one
     const bool beside = !a.accumulate && N > 0 && N <= kFillTokens;
-    FillParams f{a.grad, a.grad_stride, a.hidden, a.tokens, N, 0, 0, a.token_type, a.grad_type == GWTF_TYPE_F32, 1,
-                 streams(a.grad, a.grad_stride, a.vocab, a.hidden, sizeof(G))};
-    auto fill_groups = [&](int64_t v0, int64_t v1) -> uint32_t {
+    FillParams f{a.grad, a.grad_stride, a.hidden, a.tokens, N, 0, 0, a.token_type, a.grad_type == GWTF_TYPE_F32, FastDiv::make(1),
+                 large && on_lines(a.grad, a.grad_stride, sizeof(G))};
+    auto fill_groups = [&](int64_t v0, int64_t v1, uint32_t sorting) -> uint32_t {
         f.v0 = v0;
         f.v1 = v1;
-        const int64_t rows = (v1 - v0 + kFillGroups - 1) / kFillGroups;
-        f.rows = int(rows < 1 ? 1 : rows > kFillRows ? kFillRows : rows);
-        return uint32_t((v1 - v0 + f.rows - 1) / f.rows);
+        if (v0 == v1) return 0;
+        int64_t groups = 2 * int64_t(w.cus) - sorting; // two workgroups of 1024 threads on a CU
+        if (groups < w.cus) groups = w.cus;
+        if (groups > v1 - v0) groups = v1 - v0;
+        if (groups < (v1 - v0 + kFillRows - 1) / kFillRows) groups = (v1 - v0 + kFillRows - 1) / kFillRows;
+        f.groups = FastDiv::make(uint32_t(groups));
+        return uint32_t(groups);
     };
     if (N > 0) {
         uint32_t blocks = uint32_t((N + kSortBlock - 1) / kSortBlock);
         const int64_t half = !beside ? 0 : N > kSortBlock ? a.vocab / 2 : a.vocab;
-        uint32_t fill = fill_groups(0, half);
+        uint32_t fill = fill_groups(0, half, blocks);
         auto sort = a.vocab < int64_t(1) << 21 ? sort_block_kernel<uint32_t> : sort_block_kernel<uint64_t>;
         sort<<<dim3(blocks + fill), dim3(1024), 0, s>>>(a.tokens, a.token_type, a.vocab, N, w.sort_a, blocks, f);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         uint64_t *from = w.sort_a, *to = w.sort_b;
         blocks = uint32_t((N + kMergeKeys - 1) / kMergeKeys);
-        fill = beside ? fill_groups(half, a.vocab) : 0; // one merge at most: N <= kSortBlock * kMergeWays
+        fill = beside ? fill_groups(half, a.vocab, blocks) : 0; // one merge at most: N <= kSortBlock * kMergeWays
         for (int64_t len = kSortBlock; len < N; len *= kMergeWays) {
             int shift = 4;
             while ((len * kMergeWays) >> shift > kSamples) ++shift;

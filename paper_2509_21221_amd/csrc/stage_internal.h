@@ -35,16 +35,18 @@ constexpr int kLogprobRows = 512;
 constexpr int kLogprobItems = 2048;
 constexpr int kLogprobRecord = 16 + 8 * GWTF_STAGE_MAX_TOP;
 
-// Whether a matrix is read, or written, past the caches: larger than they are
-// and with rows on 16-byte boundaries, so that no cache line is needed twice.
-// (Reads of dropout with a residual, 16,384 x 4096 bf16: 62 us, 73 kept in the
-// caches; of the norm's gradient 91 and 105.  Rows on odd addresses, 4095 x 1111
-// f32: 27.7 and 20.1; 2,048 x 1024 bf16: 9.9 and 8.6.)
-constexpr int64_t kStreamBytes = int64_t(32) << 20;
-inline bool streams(const void *p, int64_t stride, int64_t rows, int64_t width, size_t size)
+// A call that reads and writes more than the cache beside the memory holds
+// leaves nothing in it for the next one, and goes past the caches with what it
+// touches once, where rows lie on 16-byte boundaries so that no cache line is
+// needed twice.  Measured with inputs of three states in turn, kept and past:
+// dropout with residual, bf16, 8,192 x 4096 (201 MB) 33 / 34 us, 16,384 x 4096
+// (403 MB) 72 / 62; norm 43 / 43 and 96 / 81; its gradient (268, 537 MB) 53 / 49
+// and 105 / 90; 4,096 x 4096 norm 22 / 24; its gradient of 4095 x 1111 f32 with
+// rows on odd addresses 20 / 28.
+constexpr int64_t kMemoryCacheBytes = int64_t(256) << 20;
+inline bool on_lines(const void *p, int64_t stride, size_t size)
 {
-    return rows * width * int64_t(size) >= kStreamBytes && reinterpret_cast<uintptr_t>(p) % 16 == 0 &&
-           stride * int64_t(size) % 16 == 0;
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * int64_t(size) % 16 == 0;
 }
 
 hipError_t launch_embed(const gwtf_stage_embed_t &a, hipStream_t s);

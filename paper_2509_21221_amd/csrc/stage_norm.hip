@@ -306,8 +306,10 @@ template <class T, int K, int WAVES>
 hipError_t run_norm(const gwtf_stage_norm_t &a, hipStream_t s)
 {
     const int64_t rows = WAVES == 1 ? 4 : 1;
-    const bool stream = streams(a.x, a.x_stride, a.num_tokens, a.hidden, sizeof(T)) &&
-                        (!a.residual || streams(a.residual, a.residual_stride, a.num_tokens, a.hidden, sizeof(T)));
+    const int64_t values = 1 + (a.residual != nullptr) + (a.h_out != nullptr) + (a.form == GWTF_NORM_PLAIN);
+    const int64_t bytes = a.num_tokens * a.hidden * (values * int64_t(sizeof(T)) + (a.form != GWTF_NORM_PLAIN));
+    const bool stream = bytes >= kMemoryCacheBytes && on_lines(a.x, a.x_stride, sizeof(T)) &&
+                        (!a.residual || on_lines(a.residual, a.residual_stride, sizeof(T)));
     auto kernel = stream ? norm_kernel<T, K, WAVES, true, true> : norm_kernel<T, K, WAVES, false, true>;
     if (K == 1 && WAVES == 1 && a.hidden < kVec) kernel = norm_kernel<T, 1, 1, false, false>;
     kernel<<<dim3(uint32_t((a.num_tokens + rows - 1) / rows)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a);
@@ -320,9 +322,9 @@ hipError_t run_norm_grad(const gwtf_stage_norm_grad_t &a, const StageWorkspace &
     const int64_t rows = WAVES == 1 ? 4 : 1;
     int64_t groups = (a.num_tokens + rows - 1) / rows;
     if (groups > kNormGradGroups) groups = kNormGradGroups;
-    const bool stream = streams(a.dy, a.dy_stride, a.num_tokens, a.hidden, sizeof(T)) &&
-                        streams(a.h, a.h_stride, a.num_tokens, a.hidden, sizeof(T)) &&
-                        (!a.dh || streams(a.dh, a.dh_stride, a.num_tokens, a.hidden, sizeof(T)));
+    const int64_t bytes = a.num_tokens * a.hidden * int64_t(sizeof(T)) * (a.dh ? 4 : 3);
+    const bool stream = bytes >= kMemoryCacheBytes && on_lines(a.dy, a.dy_stride, sizeof(T)) &&
+                        on_lines(a.h, a.h_stride, sizeof(T)) && (!a.dh || on_lines(a.dh, a.dh_stride, sizeof(T)));
     auto kernel = stream ? norm_grad_kernel<T, K, WAVES, true, true> : norm_grad_kernel<T, K, WAVES, false, true>;
     if (K == 1 && WAVES == 1 && a.hidden < kVec) kernel = norm_grad_kernel<T, 1, 1, false, false>;
     kernel<<<dim3(uint32_t(groups)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a, a.dweight ? w.dweight : nullptr);
