@@ -53,9 +53,7 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p)
 // tokens are there, so they are written beside the sorting, whose few
 // workgroups leave the memory idle: each of the other workgroups that fit on
 // the device with them looks through all tokens for those of its own rows,
-// every so many of the table, so that all have as many absent ones.  (32,000 x
-// 4096 bf16 and 16,384 tokens, rows side by side and 64 workgroups more than
-// fit: 51 us in both launches, against 37.)
+// every so many of the table, so that all have as many absent ones.
 
 constexpr int kFillRows = 4096;           // most rows of one workgroup
 constexpr int64_t kFillTokens = 32768;    // with more tokens a look through them costs more than the sort hides:
@@ -68,20 +66,15 @@ struct FillParams {
     int64_t N, v0, v1; // rows [v0, v1)
     int32_t token_type, wide; // wide: 32-bit gradient
     FastDiv groups;    // row v0 + r belongs to workgroup r % groups
-    int32_t stream;
 };
 
-// STREAM: past the caches, for whole tables (32,000 x 4096 bf16: 98 us for the
-// gradient of 16,384 tokens, 108 without).
-template <bool STREAM>
 __device__ __forceinline__ void zero_row(char *g, int64_t bytes)
 {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
     const u32x4 z = {0, 0, 0, 0};
     for (int64_t at = (threadIdx.x & 63) * 16; at < bytes; at += 64 * 16) {
         if (at + 16 <= bytes) {
-            if constexpr (STREAM) __builtin_nontemporal_store(z, reinterpret_cast<u32x4 *>(g + at));
-            else *reinterpret_cast<u32x4 *>(g + at) = z;
+            *reinterpret_cast<u32x4 *>(g + at) = z;
         } else {
             for (int64_t i = at; i < bytes; i += 2) *reinterpret_cast<uint16_t *>(g + i) = 0;
         }
@@ -110,11 +103,8 @@ __device__ void fill_absent(const FillParams &p, int group, uint32_t *there /* [
     __syncthreads();
     const int64_t size = p.wide ? 4 : 2;
     for (int r = threadIdx.x >> 6; r < rows; r += THREADS / 64)
-        if (!(there[r >> 5] >> (r & 31) & 1)) {
-            char *row = static_cast<char *>(p.grad) + (p.v0 + group + int64_t(r) * groups) * p.stride * size;
-            if (p.stream) zero_row<true>(row, p.hidden * size);
-            else zero_row<false>(row, p.hidden * size);
-        }
+        if (!(there[r >> 5] >> (r & 31) & 1))
+            zero_row(static_cast<char *>(p.grad) + (p.v0 + group + int64_t(r) * groups) * p.stride * size, p.hidden * size);
 }
 
 // ---- sorting tokens ----
@@ -394,7 +384,7 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradParams p)
         while (rows) {
             const int r = __builtin_ctzll(rows);
             rows &= rows - 1;
-            zero_row<false>(static_cast<char *>(a.grad) + (v0 + r) * a.grad_stride * int64_t(sizeof(G)), a.hidden * int64_t(sizeof(G)));
+            zero_row(static_cast<char *>(a.grad) + (v0 + r) * a.grad_stride * int64_t(sizeof(G)), a.hidden * int64_t(sizeof(G)));
         }
         return;
     }
@@ -470,10 +460,16 @@ hipError_t run_embed(const gwtf_stage_embed_t &a, hipStream_t s)
 
 int64_t slabs_of(int64_t H) { return (H + 511) / 512; }
 
+// Entries of a chunk: few enough for kEmbedItems waves, but no fewer than about
+// sqrt(N / 32), since the parts of a frequent token's run are added one after
+// another (words that come as 1 / rank, 16,384 x 512: chunks of 4 62 us, of 23
+// 42; 2,048 x 1024: of 4 31, of 8 30).
 int64_t chunk_of(int64_t N, int64_t H)
 {
     const int64_t c = (N * slabs_of(H) + kEmbedItems - 1) / kEmbedItems;
-    return c > kEmbedMinChunk ? c : kEmbedMinChunk;
+    int64_t least = kEmbedMinChunk;
+    while (least * least * 32 < N) ++least;
+    return c > least ? c : least;
 }
 
 template <class T, class G>
@@ -484,16 +480,17 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
     EmbedGradParams p;
     p.a = a;
     p.sorted = w.sort_a;
-    const bool large = ((a.accumulate ? 0 : a.vocab) * int64_t(sizeof(G)) + N * int64_t(sizeof(T))) * a.hidden >= kMemoryCacheBytes;
-    p.stream = large && on_lines(a.dout, a.dout_stride, sizeof(T));
+    // dout past the caches, the zeros not (16,384 x 4096 bf16 into 32,000 rows:
+    // 89 us, both past the caches 96, neither 108)
+    const int64_t bytes = ((a.accumulate ? 0 : a.vocab) * int64_t(sizeof(G)) + N * int64_t(sizeof(T))) * a.hidden;
+    p.stream = bytes >= kMemoryCacheBytes && on_lines(a.dout, a.dout_stride, sizeof(T));
     p.partial = w.partial;
     p.chunk = chunk_of(N, a.hidden);
     p.chunks = (N + p.chunk - 1) / p.chunk;
     p.slabs = int(slabs_of(a.hidden));
     // zeros beside the sort, half of them beside the merge where there is one
     const bool beside = !a.accumulate && N > 0 && N <= kFillTokens;
-    FillParams f{a.grad, a.grad_stride, a.hidden, a.tokens, N, 0, 0, a.token_type, a.grad_type == GWTF_TYPE_F32, FastDiv::make(1),
-                 large && on_lines(a.grad, a.grad_stride, sizeof(G))};
+    FillParams f{a.grad, a.grad_stride, a.hidden, a.tokens, N, 0, 0, a.token_type, a.grad_type == GWTF_TYPE_F32, FastDiv::make(1)};
     auto fill_groups = [&](int64_t v0, int64_t v1, uint32_t sorting) -> uint32_t {
         f.v0 = v0;
         f.v1 = v1;

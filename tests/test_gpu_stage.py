@@ -523,6 +523,59 @@ def test_logprob_gradient_against_differences():
     assert abs((g * dirn).sum() - slope) <= 100 * E * (np.abs(g * dirn).sum() + 32 * n) + 1e-6
 
 
+# ---- calls larger than the caches ----
+
+def parts_of(n, pieces=5):
+    step = -(-n // pieces)
+    return [slice(i, min(n, i + step)) for i in range(0, n, step)]
+
+
+@pytest.mark.parametrize("dtype, h", [("bfloat16", 4096), ("float32", 2056), ("float16", 1000)])
+def test_large_calls_match_small_ones(dtype, h):
+    """A row's result does not depend on the call's size: calls of more than 256
+    MB against the same rows in pieces, bit for bit."""
+    torch = torch_()
+    size = 4 if dtype == "float32" else 2
+    n = (300 << 20) // (2 * size * h)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    new = lambda: torch.randn((n, h), device="cuda", generator=gen).to(dt(dtype))  # noqa: E731
+    x, res, w = new(), new(), torch.randn(h, device="cuda", generator=gen).to(dt(dtype))
+    tok = torch.randint(-1, 4000, (n,), device="cuda", generator=gen)
+    ident = torch.arange(n, device="cuda") * 7919
+    with ops(n, h, 4000) as s:
+        table = x[:4000]
+        calls = [lambda r: (s.embed(tok[r], table, 1.5),),
+                 lambda r: (s.dropout(x[r], 0.3, 11, 2, rows=ident[r]),),
+                 lambda r: (s.dropout(x[r], 0.3, 11, 2, rows=ident[r], residual=res[r]),)]
+        calls += [lambda r, q=q: [t for t in s.norm(x[r], w, 1e-5, res[r], q) if t is not None] for q in ("none", "row", "block")]
+        rstd = s.norm(x, w)[3]
+        calls.append(lambda r: (s.norm_grad(x[r], res[r], w, rstd[r], dh=x[r])[0],))
+        for call in calls:
+            whole = call(slice(0, n))
+            pieces = [call(r) for r in parts_of(n)]
+            for i, t in enumerate(whole):
+                assert torch.equal(t.view(torch.uint8), torch.cat([p[i] for p in pieces]).view(torch.uint8))
+
+
+def test_large_embedding_gradient():
+    torch = torch_()
+    n, h, v = 9000, 4096, 32000
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    dout = torch.randn((n, h), device="cuda", generator=gen).to(torch.bfloat16)
+    tok = torch.randint(-1, v, (n,), device="cuda", generator=gen) % 9001 - 1
+    there = tok >= 0
+    want = torch.zeros((v, h), device="cuda", dtype=torch.float64).index_add_(0, tok[there], dout[there].double())
+    size = torch.zeros((v, h), device="cuda", dtype=torch.float64).index_add_(0, tok[there], dout[there].double().abs())
+    with ops(n, h, v) as s:
+        got = s.embed_grad(tok, dout, v, dtype=torch.float32)
+        again = s.embed_grad(tok, dout, v, dtype=torch.float32)
+    most = int(torch.bincount(tok[there]).max())
+    assert bool(((got.double() - want).abs() <= (most + 2) * E * size).all())
+    assert torch.equal(got, again)
+
+
 # ---- refusals, streams, graphs ----
 
 def test_refusals():
