@@ -109,6 +109,7 @@ extern "C" gwtf_status_t gwtf_stage_create(const gwtf_stage_shape_t *shape, void
     const size_t sort_a = take(sizeof(uint64_t) * size_t(shape->max_tokens));
     const size_t sort_b = take(sizeof(uint64_t) * size_t(shape->max_tokens));
     const size_t partial = take(size_t(embed_partial_bytes(shape->max_tokens, shape->max_hidden)));
+    const size_t absent = take(size_t(embed_absent_bytes(shape->max_vocab, w.cus)));
     const size_t dweight = take(sizeof(float) * kNormGradGroups * size_t(wide));
     const size_t logprob = take(lp_records + sizeof(uint32_t) * kLogprobRows);
     if ((e = hipMalloc(&w.base, total)) != hipSuccess) {
@@ -119,6 +120,7 @@ extern "C" gwtf_status_t gwtf_stage_create(const gwtf_stage_shape_t *shape, void
     w.sort_a = reinterpret_cast<uint64_t *>(base + sort_a);
     w.sort_b = reinterpret_cast<uint64_t *>(base + sort_b);
     w.partial = reinterpret_cast<float *>(base + partial);
+    w.absent = reinterpret_cast<uint32_t *>(base + absent);
     w.dweight = reinterpret_cast<float *>(base + dweight);
     w.logprob = base + logprob;
     if ((e = hipMemsetAsync(w.logprob + lp_records, 0, sizeof(uint32_t) * kLogprobRows, h->stream)) != hipSuccess) {

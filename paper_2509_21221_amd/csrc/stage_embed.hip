@@ -50,22 +50,29 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p)
 // ---- zeros for the rows of absent tokens ----
 //
 // Most of the gradient's bytes are zeros that depend on nothing but which
-// tokens are there, so they are written beside the sorting, whose few
-// workgroups leave the memory idle: each of the other workgroups that fit on
-// the device with them looks through all tokens for those of its own rows,
-// every so many of the table, so that all have as many absent ones.
+// tokens are there, so they are written beside the launches that wait for
+// their reads rather than for the memory: the sort, the merge, the join, and
+// the sums where they are short.  Workgroup g of the fill has the rows g, g +
+// groups, .. of the table, a share of them in each launch; in the first one it
+// looks through all tokens for its own and keeps what it found as a bit a row.
+// (2,048 x 1024 28 us, 16,384 x 4096 86; all zeros beside sort and merge 31 and
+// 89, no launch beside another 56 and 157.)
 
-constexpr int kFillRows = 4096;           // most rows of one workgroup
-constexpr int64_t kFillTokens = 32768;    // with more tokens a look through them costs more than the sort hides:
-                                          // then embed_grad_kernel writes the zeros
+constexpr int kFillRows = 65536;             // most rows of one workgroup
+constexpr int64_t kFillTokens = 32768;       // with more tokens a look through them costs more than the sort hides:
+                                             // then embed_grad_kernel writes the zeros
+constexpr int64_t kShortSums = int64_t(16) << 20; // bytes of dout whose sums wait for reads
 
 struct FillParams {
     void *grad;
     int64_t stride, hidden;
     const void *tokens;
-    int64_t N, v0, v1; // rows [v0, v1)
+    int64_t N, vocab;
     int32_t token_type, wide; // wide: 32-bit gradient
-    FastDiv groups;    // row v0 + r belongs to workgroup r % groups
+    FastDiv groups;
+    uint32_t *absent; // [groups][words], or NULL: all rows belong to the first launch
+    int32_t words;
+    int32_t r0, r1;   // this launch's share of a workgroup's rows
 };
 
 __device__ __forceinline__ void zero_row(char *g, int64_t bytes)
@@ -81,12 +88,22 @@ __device__ __forceinline__ void zero_row(char *g, int64_t bytes)
     }
 }
 
-template <int THREADS>
-__device__ void fill_absent(const FillParams &p, int group, uint32_t *there /* [kFillRows / 32] */)
+__device__ __forceinline__ void fill_rows(const FillParams &p, int group, const uint32_t *absent, int threads)
 {
-    const uint32_t groups = p.groups.d, all = uint32_t(p.v1 - p.v0);
-    const int rows = int((all + groups - 1 - group) / groups);
-    for (int i = threadIdx.x; i < (rows + 31) / 32; i += THREADS) there[i] = 0;
+    const uint32_t groups = p.groups.d;
+    const int64_t size = p.wide ? 4 : 2;
+    const int rows = int((uint32_t(p.vocab) + groups - 1 - group) / groups), r1 = p.r1 < rows ? p.r1 : rows;
+    for (int r = p.r0 + (threadIdx.x >> 6); r < r1; r += threads / 64)
+        if (absent[r >> 5] >> (r & 31) & 1)
+            zero_row(static_cast<char *>(p.grad) + (group + int64_t(r) * groups) * p.stride * size, p.hidden * size);
+}
+
+// The first launch's part, with kFillRows / 32 words of LDS.
+template <int THREADS>
+__device__ void fill_first(const FillParams &p, int group, uint32_t *absent)
+{
+    const uint32_t groups = p.groups.d;
+    for (int i = threadIdx.x; i < p.words; i += THREADS) absent[i] = 0xffffffffu;
     __syncthreads();
     for (int64_t i = threadIdx.x; i < p.N; i += 8 * THREADS) {
         int64_t t[8];
@@ -94,17 +111,19 @@ __device__ void fill_absent(const FillParams &p, int group, uint32_t *there /* [
         for (int q = 0; q < 8; ++q) t[q] = i + q * THREADS < p.N ? load_token(p.tokens, p.token_type, i + q * THREADS) : -1;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const uint64_t r = uint64_t(t[q] - p.v0);
-            if (t[q] < 0 || r >= all) continue;
-            const uint32_t own = p.groups.div(uint32_t(r));
-            if (uint32_t(r) - own * groups == uint32_t(group)) atomicOr(&there[own >> 5], 1u << (own & 31));
+            if (t[q] < 0 || t[q] >= p.vocab) continue;
+            const uint32_t own = p.groups.div(uint32_t(t[q]));
+            if (uint32_t(t[q]) - own * groups == uint32_t(group)) atomicAnd(&absent[own >> 5], ~(1u << (own & 31)));
         }
     }
     __syncthreads();
-    const int64_t size = p.wide ? 4 : 2;
-    for (int r = threadIdx.x >> 6; r < rows; r += THREADS / 64)
-        if (!(there[r >> 5] >> (r & 31) & 1))
-            zero_row(static_cast<char *>(p.grad) + (p.v0 + group + int64_t(r) * groups) * p.stride * size, p.hidden * size);
+    if (p.absent)
+        for (int i = threadIdx.x; i < p.words; i += THREADS) p.absent[int64_t(group) * p.words + i] = absent[i];
+    fill_rows(p, group, absent, THREADS);
+}
+__device__ __forceinline__ void fill_later(const FillParams &p, int group, int threads)
+{
+    fill_rows(p, group, p.absent + int64_t(group) * p.words, threads);
 }
 
 // ---- sorting tokens ----
@@ -159,8 +178,9 @@ __global__ __launch_bounds__(1024) void sort_block_kernel(const void *tokens, in
                                                           uint64_t *out, uint32_t blocks, FillParams f)
 {
     __shared__ K key[2][kSortBlock];
+    static_assert(kFillRows / 8 <= sizeof key, "a bit for each row of a workgroup of the fill");
     if (blockIdx.x >= blocks) {
-        fill_absent<1024>(f, int(blockIdx.x - blocks), reinterpret_cast<uint32_t *>(key));
+        fill_first<1024>(f, int(blockIdx.x - blocks), reinterpret_cast<uint32_t *>(key));
         return;
     }
     constexpr int kShift = sizeof(K) == 4 ? 11 : 32;
@@ -224,7 +244,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(const uint64_t *in
 {
     __shared__ uint64_t sample[kSamples];
     if (blockIdx.x >= blocks) {
-        fill_absent<kMergeThreads>(f, int(blockIdx.x - blocks), reinterpret_cast<uint32_t *>(sample));
+        fill_later(f, int(blockIdx.x - blocks), kMergeThreads);
         return;
     }
     // a workgroup's adjacent keys lie within one block, as len is a multiple of
@@ -275,6 +295,8 @@ struct EmbedGradParams {
     int64_t chunk, chunks;
     int slabs;                // of 512 columns
     int64_t fill_block;       // first workgroup that writes zeros
+    bool search;              // it looks its rows up in the sorted list
+    FillParams fill;
     bool stream;              // dout is read past the caches
 };
 
@@ -366,7 +388,10 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradParams p)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t N = a.num_tokens;
     if (blockIdx.x >= p.fill_block) {
-        // zeros for the rows whose token is absent
+        if (!p.search) {
+            fill_later(p.fill, int(blockIdx.x - p.fill_block), 256);
+            return;
+        }
         const int64_t v0 = ((blockIdx.x - p.fill_block) * 4 + wave) * int64_t(kSearchRows);
         if (v0 >= a.vocab) return;
         bool absent = false;
@@ -400,6 +425,10 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradParams p)
 {
     const gwtf_stage_embed_grad_t &a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (blockIdx.x >= p.fill_block) {
+        fill_later(p.fill, int(blockIdx.x - p.fill_block), 256);
+        return;
+    }
     const int64_t item = int64_t(blockIdx.x) * 4 + wave;
     const int64_t c = item / p.slabs, N = a.num_tokens;
     const int64_t e0 = c * p.chunk, e1 = e0 + p.chunk;
@@ -488,33 +517,49 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
     p.chunk = chunk_of(N, a.hidden);
     p.chunks = (N + p.chunk - 1) / p.chunk;
     p.slabs = int(slabs_of(a.hidden));
-    // zeros beside the sort, half of them beside the merge where there is one
-    const bool beside = !a.accumulate && N > 0 && N <= kFillTokens;
-    FillParams f{a.grad, a.grad_stride, a.hidden, a.tokens, N, 0, 0, a.token_type, a.grad_type == GWTF_TYPE_F32, FastDiv::make(1)};
-    auto fill_groups = [&](int64_t v0, int64_t v1, uint32_t sorting) -> uint32_t {
-        f.v0 = v0;
-        f.v1 = v1;
-        if (v0 == v1) return 0;
-        int64_t groups = 2 * int64_t(w.cus) - sorting; // two workgroups of 1024 threads on a CU
-        if (groups < w.cus) groups = w.cus;
-        if (groups > v1 - v0) groups = v1 - v0;
-        if (groups < (v1 - v0 + kFillRows - 1) / kFillRows) groups = (v1 - v0 + kFillRows - 1) / kFillRows;
-        f.groups = FastDiv::make(uint32_t(groups));
-        return uint32_t(groups);
+    p.search = !a.accumulate && (N == 0 || N > kFillTokens);
+    FillParams &f = p.fill;
+    f = FillParams{a.grad, a.grad_stride, a.hidden, a.tokens, N, a.vocab, a.token_type, a.grad_type == GWTF_TYPE_F32,
+                   FastDiv::make(1), nullptr, 0, 0, 0};
+    const bool merged = N > kSortBlock, joined = p.chunks > 1, short_sums = N * a.hidden * int64_t(sizeof(T)) < kShortSums;
+    uint32_t groups = 0; // of the fill, in every launch that has a share
+    int rows = 0, shares = 1, share = 0;
+    if (!a.accumulate && !p.search) {
+        // with the sorting or merging workgroups, two of 1024 threads on a CU
+        const int64_t busy = (N + (merged ? kMergeKeys : kSortBlock) - 1) / (merged ? kMergeKeys : kSortBlock);
+        int64_t g = 2 * int64_t(w.cus) - busy;
+        if (g < w.cus) g = w.cus;
+        if (g > a.vocab) g = a.vocab;
+        if (a.vocab <= kAbsentRows) {
+            f.absent = w.absent;
+            shares = 1 + merged + short_sums + joined;
+        } else if (g < (a.vocab + kFillRows - 1) / kFillRows) {
+            g = (a.vocab + kFillRows - 1) / kFillRows;
+        }
+        groups = uint32_t(g);
+        rows = int((a.vocab + g - 1) / g);
+        f.groups = FastDiv::make(groups);
+        f.words = (rows + 31) / 32;
+    }
+    // the next share of the fill: its workgroups
+    auto take_share = [&](bool has) -> uint32_t {
+        if (!has || share == shares) return 0;
+        f.r0 = int(int64_t(rows) * share / shares);
+        f.r1 = int(int64_t(rows) * ++share / shares);
+        return groups;
     };
     if (N > 0) {
         uint32_t blocks = uint32_t((N + kSortBlock - 1) / kSortBlock);
-        const int64_t half = !beside ? 0 : N > kSortBlock ? a.vocab / 2 : a.vocab;
-        uint32_t fill = fill_groups(0, half, blocks);
+        uint32_t fill = take_share(true);
         auto sort = a.vocab < int64_t(1) << 21 ? sort_block_kernel<uint32_t> : sort_block_kernel<uint64_t>;
         sort<<<dim3(blocks + fill), dim3(1024), 0, s>>>(a.tokens, a.token_type, a.vocab, N, w.sort_a, blocks, f);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         uint64_t *from = w.sort_a, *to = w.sort_b;
         blocks = uint32_t((N + kMergeKeys - 1) / kMergeKeys);
-        fill = beside ? fill_groups(half, a.vocab, blocks) : 0; // one merge at most: N <= kSortBlock * kMergeWays
         for (int64_t len = kSortBlock; len < N; len *= kMergeWays) {
             int shift = 4;
             while ((len * kMergeWays) >> shift > kSamples) ++shift;
+            fill = groups ? take_share(true) : 0; // one merge at most beside a fill: N <= kSortBlock * kMergeWays
             merge_kernel<<<dim3(blocks + fill), dim3(kMergeThreads), 0, s>>>(from, uint32_t(N), uint32_t(len), shift, to, blocks, f);
             if ((e = hipGetLastError()) != hipSuccess) return e;
             uint64_t *t = from;
@@ -524,12 +569,13 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
         p.sorted = from;
     }
     p.fill_block = (p.chunks * p.slabs + 3) / 4;
-    const int64_t fill = a.accumulate || beside ? 0 : (a.vocab + 4 * kSearchRows - 1) / (4 * kSearchRows);
+    const int64_t fill = p.search ? (a.vocab + 4 * kSearchRows - 1) / (4 * kSearchRows) : take_share(short_sums);
     if (p.fill_block + fill == 0) return hipSuccess;
     embed_grad_kernel<T, G><<<dim3(uint32_t(p.fill_block + fill)), dim3(256), 0, s>>>(p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (p.chunks > 1) {
-        embed_join_kernel<G><<<dim3(uint32_t(p.fill_block)), dim3(256), 0, s>>>(p);
+    if (joined) {
+        const uint32_t last = take_share(true);
+        embed_join_kernel<G><<<dim3(uint32_t(p.fill_block) + last), dim3(256), 0, s>>>(p);
         e = hipGetLastError();
     }
     return e;
@@ -543,6 +589,14 @@ int64_t embed_partial_bytes(int64_t max_tokens, int64_t max_hidden)
 {
     const int64_t by_items = kEmbedItems * 512 + max_hidden, by_tokens = (max_tokens / kEmbedMinChunk + 1) * max_hidden;
     return (by_items < by_tokens ? by_items : by_tokens) * 2 * int64_t(sizeof(float));
+}
+
+// A word more than the bits for each workgroup of the fill, of which there are
+// at most two a CU.
+int64_t embed_absent_bytes(int64_t max_vocab, int cus)
+{
+    const int64_t rows = max_vocab < kAbsentRows ? max_vocab : kAbsentRows;
+    return (rows / 32 + 2 * (2 * int64_t(cus) + 1)) * int64_t(sizeof(uint32_t));
 }
 
 hipError_t launch_embed(const gwtf_stage_embed_t &a, hipStream_t s)

@@ -15,6 +15,7 @@ struct StageWorkspace {
     void *base = nullptr;                          // the allocation that holds the parts
     uint64_t *sort_a = nullptr, *sort_b = nullptr; // [max_tokens] each: token << 32 | position
     float *partial = nullptr;                      // embedding gradient: sums of runs that cross chunks
+    uint32_t *absent = nullptr;                    // embedding gradient: a bit for each row of the table
     float *dweight = nullptr;                      // norm gradient: [kNormGradGroups][max_hidden]
     unsigned char *logprob = nullptr;              // kLogprobItems records, then kLogprobRows counters (0 between calls)
     int cus = 0;
@@ -25,6 +26,8 @@ struct StageWorkspace {
 constexpr int64_t kEmbedItems = 4096;
 constexpr int kEmbedMinChunk = 4;
 int64_t embed_partial_bytes(int64_t max_tokens, int64_t max_hidden);
+constexpr int64_t kAbsentRows = int64_t(1) << 22; // tables up to here have their absent rows kept between launches
+int64_t embed_absent_bytes(int64_t max_vocab, int cus);
 
 // Norm gradient: most workgroups that sum dweight over their rows.
 constexpr int kNormGradGroups = 512;
