@@ -394,7 +394,8 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
 {
     __shared__ Softmax parts[kLpWaves];
     __shared__ uint64_t units_of[TOP ? 2 * kLpThreads : 1]; // and each wave's slots
-    __shared__ uint32_t flag, alive[kLpWaves];
+    // two words: a wave may still read the first when another writes the second
+    __shared__ uint32_t again_flag, last_flag, alive[kLpWaves];
     const gwtf_stage_logprob_t &a = p.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row = blockIdx.x / uint32_t(p.segments), segment = blockIdx.x - uint32_t(row) * uint32_t(p.segments);
@@ -466,19 +467,36 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
         add(v);
     }
     if (base < c1) ragged(base);
+    {
+        const bool some = __ballot(first > kNone) != 0; // an entry that is not masked
+        const Softmax mine = wave_join<false>(r);
+        if (lane == 0) {
+            parts[wave] = mine;
+            alive[wave] = some;
+        }
+    }
+    if constexpr (TOP) {
+        units_of[threadIdx.x] = unit1 < 0 ? 0 : key_of(order_of(first), uint32_t(unit1));
+        units_of[kLpThreads + threadIdx.x] = unit2 < 0 || unit2 == unit1 ? 0 : key_of(order_of(second), uint32_t(unit2));
+    }
+    __syncthreads();
+    r = wave_join<false>(lane < kLpWaves ? parts[lane] : Softmax{kNone, 0.f, 0.f});
+    bool live = alive[0] | alive[1] | alive[2] | alive[3];
     TopList list;
     if constexpr (TOP) {
-        bool again = a.top > kUnitTop;
-        if (!again) {
-            units_of[threadIdx.x] = unit1 < 0 ? 0 : key_of(order_of(first), uint32_t(unit1));
-            units_of[kLpThreads + threadIdx.x] = unit2 < 0 || unit2 == unit1 ? 0 : key_of(order_of(second), uint32_t(unit2));
-            __syncthreads();
+        // Nothing but masked entries (a NaN would show in s): the first columns.
+        const bool masked = !live && r.s == 0.f;
+        bool again = a.top > kUnitTop && !masked;
+        list.start(a.top, slots);
+        if (masked) {
+            const int64_t col = (c0 > off ? c0 - off : 0) + lane;
+            if (lane < a.top && col < c1 - off) list.key = key_of(order_of(kNone), uint32_t(col));
+        } else if (!again) {
             if (wave == chief) {
                 uint64_t k[2 * kLpWaves];
 #pragma unroll
                 for (int i = 0; i < 2 * kLpWaves; ++i) k[i] = units_of[i * 64 + lane];
                 wave_sync();
-                list.start(a.top, slots);
                 list.select(k, c1 - c0 > kStep ? 2 * kLpWaves : kLpWaves); // one step: no second units
                 again = list.last == 0;
                 if (!again) {
@@ -487,12 +505,13 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
                     if (c1 - c0 > 2 * kStep) resolve_lanes(list, units, x, off, c0, c1);
                     again = list.last == 0;
                 }
-                if (lane == 0) flag = again;
+                if (lane == 0) again_flag = again;
             }
             __syncthreads();
-            again = flag;
+            again = again_flag;
         }
         if (again) {
+            __syncthreads();
             const uint64_t mine = list_pass(slots, a.top, x, c0 > off ? c0 - off : 0, c1 - off);
             __syncthreads();
             units_of[threadIdx.x] = mine;
@@ -507,15 +526,6 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
             }
         }
     }
-    const bool some = __ballot(first > kNone) != 0; // an entry that is not masked
-    r = wave_join<false>(r);
-    if (lane == 0) {
-        parts[wave] = r;
-        alive[wave] = some;
-    }
-    __syncthreads();
-    r = wave_join<false>(lane < kLpWaves ? parts[lane] : Softmax{kNone, 0.f, 0.f});
-    bool live = alive[0] | alive[1] | alive[2] | alive[3];
     if (p.segments > 1) {
         // The workgroup that arrives last joins the row's records.  Records and
         // counter are words of agent scope; the wait puts a record in memory
@@ -535,11 +545,11 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             if (lane == 0)
-                flag = __hip_atomic_fetch_add(p.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                last_flag = __hip_atomic_fetch_add(p.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                        uint32_t(p.segments - 1);
         }
         __syncthreads();
-        if (!flag) return;
+        if (!last_flag) return;
         const unsigned char *records = p.records + row * p.segments * kLogprobRecord;
         r = {kNone, 0.f, 0.f};
         live = false;
@@ -553,7 +563,8 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
         if constexpr (TOP) {
             if (wave == chief) {
                 constexpr int kBatch = 8; // keys of a lane read side by side
-                const int all = p.segments * a.top;
+                // of a masked row, the first segment's
+                const int all = (!live && r.s == 0.f ? 1 : p.segments) * a.top;
                 list.start(a.top, slots);
                 for (int i0 = 0; i0 < all; i0 += kBatch * 64) {
                     uint64_t k[kBatch];

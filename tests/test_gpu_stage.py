@@ -376,7 +376,7 @@ def logits_case(r, n, v, kind):
 
 
 LP_SHAPES = [(1, 1, 1), (1, 2, 2), (2, 63, 5), (3, 1000, 20), (5, 4097, 64), (1, 50021, 8), (2, 131072, 4), (600, 300, 3),
-             (513, 4100, 0)]
+             (513, 4100, 0), (3, 65535, 9), (1, 65537, 30)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -451,7 +451,7 @@ def test_logprob_of_the_types_lowest_value(dtype):
     assert f64(logp)[2] == 0
 
 
-@pytest.mark.parametrize("v", [40, 9000])
+@pytest.mark.parametrize("v", [40, 9000, 90001])
 def test_logprob_with_nan_and_infinity(v):
     torch = torch_()
     x = torch.randn((4, v), device="cuda")
