@@ -61,7 +61,7 @@ __device__ __forceinline__ void store_part(T *p, int n, const typename Vec8<T>::
 
 // Columns [0, n) of p as they lie in memory, the rest `fill`; n >= 8 is the
 // common case, n <= 0 reads nothing.  STREAM: a read that leaves the caches to
-// others (kMemoryCacheBytes).
+// others (kStreamBytes).
 template <class T, bool STREAM = false>
 __device__ __forceinline__ typename Vec8<T>::type load8_raw(const T *p, int64_t n, T fill = T(0.f))
 {

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutParams p)
             v[i] = bits >= p.limit ? v[i] * p.keep_scale : 0.f;
             if constexpr (RES) v[i] += res[i];
         }
-        if (u0 + q * 256u < p.units) store8(static_cast<T *>(p.out) + row[q] * p.os + col, p.H - col, v);
+        if (u0 + q * 256u < p.units) store8<T, STREAM>(static_cast<T *>(p.out) + row[q] * p.os + col, p.H - col, v);
     }
 }
 
@@ -102,8 +102,9 @@ hipError_t run(const gwtf_stage_dropout_t &a, uint32_t limit, hipStream_t s)
     p.site = a.site;
     p.limit = limit;
     p.keep_scale = 65536.f / float(65536 - limit);
-    const bool stream = a.num_tokens * a.hidden * int64_t(sizeof(T)) * (a.residual ? 3 : 2) >= kMemoryCacheBytes &&
-                        on_lines(a.x, a.x_stride, sizeof(T)) && (!a.residual || on_lines(a.residual, a.residual_stride, sizeof(T)));
+    const bool stream = a.num_tokens * a.hidden * int64_t(sizeof(T)) * (a.residual ? 3 : 2) >= kStreamBytes &&
+                        on_lines(a.x, a.x_stride, sizeof(T)) && on_lines(a.out, a.out_stride, sizeof(T)) &&
+                        (!a.residual || on_lines(a.residual, a.residual_stride, sizeof(T)));
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
         p.row0 = r;

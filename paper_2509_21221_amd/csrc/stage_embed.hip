@@ -26,7 +26,7 @@ struct EmbedParams {
 };
 
 // STREAM: rows written past the caches, which the table's rows can then stay in
-// (16,384 x 4096 bf16: 29 us, 39 without).
+// (16,384 x 4096 bf16: 29 us, 48 without).
 template <class T, bool STREAM>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedParams p)
 {
@@ -73,15 +73,18 @@ struct FillParams {
     uint32_t *absent; // [groups][words], or NULL: all rows belong to the first launch
     int32_t words;
     int32_t r0, r1;   // this launch's share of a workgroup's rows
+    int32_t stream;   // zeros past the caches
 };
 
+template <bool STREAM>
 __device__ __forceinline__ void zero_row(char *g, int64_t bytes)
 {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
     const u32x4 z = {0, 0, 0, 0};
     for (int64_t at = (threadIdx.x & 63) * 16; at < bytes; at += 64 * 16) {
         if (at + 16 <= bytes) {
-            *reinterpret_cast<u32x4 *>(g + at) = z;
+            if constexpr (STREAM) __builtin_nontemporal_store(z, reinterpret_cast<u32x4 *>(g + at));
+            else *reinterpret_cast<u32x4 *>(g + at) = z;
         } else {
             for (int64_t i = at; i < bytes; i += 2) *reinterpret_cast<uint16_t *>(g + i) = 0;
         }
@@ -94,8 +97,11 @@ __device__ __forceinline__ void fill_rows(const FillParams &p, int group, const 
     const int64_t size = p.wide ? 4 : 2;
     const int rows = int((uint32_t(p.vocab) + groups - 1 - group) / groups), r1 = p.r1 < rows ? p.r1 : rows;
     for (int r = p.r0 + (threadIdx.x >> 6); r < r1; r += threads / 64)
-        if (absent[r >> 5] >> (r & 31) & 1)
-            zero_row(static_cast<char *>(p.grad) + (group + int64_t(r) * groups) * p.stride * size, p.hidden * size);
+        if (absent[r >> 5] >> (r & 31) & 1) {
+            char *row = static_cast<char *>(p.grad) + (group + int64_t(r) * groups) * p.stride * size;
+            if (p.stream) zero_row<true>(row, p.hidden * size);
+            else zero_row<false>(row, p.hidden * size);
+        }
 }
 
 // The first launch's part, with kFillRows / 32 words of LDS.
@@ -409,7 +415,7 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradParams p)
         while (rows) {
             const int r = __builtin_ctzll(rows);
             rows &= rows - 1;
-            zero_row(static_cast<char *>(a.grad) + (v0 + r) * a.grad_stride * int64_t(sizeof(G)), a.hidden * int64_t(sizeof(G)));
+            zero_row<false>(static_cast<char *>(a.grad) + (v0 + r) * a.grad_stride * int64_t(sizeof(G)), a.hidden * int64_t(sizeof(G)));
         }
         return;
     }
@@ -471,7 +477,7 @@ template <class T>
 hipError_t run_embed(const gwtf_stage_embed_t &a, hipStream_t s)
 {
     const int64_t steps = (a.hidden + kVec - 1) / kVec, slab = (int64_t(1) << 30) / steps;
-    const bool stream = 2 * a.num_tokens * a.hidden * int64_t(sizeof(T)) >= kMemoryCacheBytes && on_lines(a.out, a.out_stride, sizeof(T));
+    const bool stream = 2 * a.num_tokens * a.hidden * int64_t(sizeof(T)) >= kStreamBytes && on_lines(a.out, a.out_stride, sizeof(T));
     auto kernel = stream ? embed_kernel<T, true> : embed_kernel<T, false>;
     EmbedParams p;
     p.a = a;
@@ -509,10 +515,12 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
     EmbedGradParams p;
     p.a = a;
     p.sorted = w.sort_a;
-    // dout past the caches, the zeros not (16,384 x 4096 bf16 into 32,000 rows:
-    // 89 us, both past the caches 96, neither 108)
+    // zeros past the caches where the table is larger than the L2s together
+    // (2,048 x 1024 into 131 MB 27 us, 32 through them; 16,384 x 4096 into 262 MB
+    // 89 and 93)
+    const bool large_table = a.vocab * a.hidden * int64_t(sizeof(G)) >= kL2Bytes && on_lines(a.grad, a.grad_stride, sizeof(G));
     const int64_t bytes = ((a.accumulate ? 0 : a.vocab) * int64_t(sizeof(G)) + N * int64_t(sizeof(T))) * a.hidden;
-    p.stream = bytes >= kMemoryCacheBytes && on_lines(a.dout, a.dout_stride, sizeof(T));
+    p.stream = bytes >= kStreamBytes && on_lines(a.dout, a.dout_stride, sizeof(T));
     p.partial = w.partial;
     p.chunk = chunk_of(N, a.hidden);
     p.chunks = (N + p.chunk - 1) / p.chunk;
@@ -520,7 +528,7 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
     p.search = !a.accumulate && (N == 0 || N > kFillTokens);
     FillParams &f = p.fill;
     f = FillParams{a.grad, a.grad_stride, a.hidden, a.tokens, N, a.vocab, a.token_type, a.grad_type == GWTF_TYPE_F32,
-                   FastDiv::make(1), nullptr, 0, 0, 0};
+                   FastDiv::make(1), nullptr, 0, 0, 0, large_table};
     const bool merged = N > kSortBlock, joined = p.chunks > 1, short_sums = N * a.hidden * int64_t(sizeof(T)) < kShortSums;
     uint32_t groups = 0; // of the fill, in every launch that has a share
     int rows = 0, shares = 1, share = 0;

@@ -38,15 +38,17 @@ constexpr int kLogprobRows = 512;
 constexpr int kLogprobItems = 2048;
 constexpr int kLogprobRecord = 16 + 8 * GWTF_STAGE_MAX_TOP;
 
-// A call that reads and writes more than the cache beside the memory holds
-// leaves nothing in it for the next one, and goes past the caches with what it
-// touches once, where rows lie on 16-byte boundaries so that no cache line is
-// needed twice.  Measured with inputs of three states in turn, kept and past:
-// dropout with residual, bf16, 8,192 x 4096 (201 MB) 33 / 34 us, 16,384 x 4096
-// (403 MB) 72 / 62; norm 43 / 43 and 96 / 81; its gradient (268, 537 MB) 53 / 49
-// and 105 / 90; 4,096 x 4096 norm 22 / 24; its gradient of 4095 x 1111 f32 with
-// rows on odd addresses 20 / 28.
-constexpr int64_t kMemoryCacheBytes = int64_t(256) << 20;
+// A call that reads and writes this much or more goes past the caches with what
+// it touches once, where rows lie on 16-byte boundaries so that no cache line is
+// needed twice.  Measured with inputs and results of three calls in turn, bf16,
+// through / past: dropout with residual 2,048 x 4096 (50 MB) 9.7 / 10.3 us, 4,096
+// (101 MB) 19.1 / 18.6, 8,192 38 / 34, 16,384 72 / 65; norm to 8 bits 12.6 /
+// 13.2, 26 / 23, 46 / 41, 84 / 75; its gradient 18.7 / 20.2, 32 / 30, 57 / 52, 104 /
+// 95; gradient of log probabilities, 512 x 32,000 (66 MB) 12.8 / 15.1, 2,048 57 /
+// 50.  With rows on odd addresses the norm's gradient of 4095 x 1111 f32 takes
+// 20 / 28.
+constexpr int64_t kStreamBytes = int64_t(96) << 20;
+constexpr int64_t kL2Bytes = int64_t(32) << 20; // of all XCDs
 inline bool on_lines(const void *p, int64_t stride, size_t size)
 {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * int64_t(size) % 16 == 0;

@@ -609,7 +609,8 @@ struct LogprobGradParams {
 constexpr int kGradStep = 256 * kVec;
 constexpr int kGradSteps = 2; // with their reads side by side
 
-template <class T>
+// STREAM: whole steps past the caches; they lie on lines whatever the rows do.
+template <class T, bool STREAM>
 __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobGradParams p)
 {
     const gwtf_stage_logprob_grad_t &a = p.a;
@@ -654,13 +655,13 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobGradParams p)
         const int64_t col = base + threadIdx.x * kVec;
         Raw raw[kGradSteps];
 #pragma unroll
-        for (int q = 0; q < kGradSteps; ++q) raw[q] = *reinterpret_cast<const Raw *>(x + col + q * kGradStep);
+        for (int q = 0; q < kGradSteps; ++q) raw[q] = load8_raw<T, STREAM>(x + col + q * kGradStep, kVec);
 #pragma unroll
         for (int q = 0; q < kGradSteps; ++q) {
             float v[8];
             widen<T>(raw[q], v);
             grad(v, col + q * kGradStep);
-            store8(out + col + q * kGradStep, kVec, v);
+            store8<T, STREAM>(out + col + q * kGradStep, kVec, v);
         }
     }
     for (; base < c1; base += kGradStep) {
@@ -734,6 +735,8 @@ hipError_t run_logprob_grad(const gwtf_stage_logprob_grad_t &a, hipStream_t s)
 {
     LogprobGradParams p;
     split_rows(p, a.num_tokens, a.vocab, kGradStep, 2048);
+    const bool stream = 2 * a.num_tokens * a.vocab * int64_t(sizeof(T)) >= kStreamBytes;
+    auto kernel = stream ? logprob_grad_kernel<T, true> : logprob_grad_kernel<T, false>;
     const int64_t slab = (int64_t(1) << 30) / p.segments;
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
@@ -746,7 +749,7 @@ hipError_t run_logprob_grad(const gwtf_stage_logprob_grad_t &a, hipStream_t s)
         if (a.entropy) p.a.entropy += r;
         if (a.dlogp) p.a.dlogp += r;
         if (a.dentropy) p.a.dentropy += r;
-        logprob_grad_kernel<T><<<dim3(uint32_t(n * p.segments)), dim3(256), 0, s>>>(p);
+        kernel<<<dim3(uint32_t(n * p.segments)), dim3(256), 0, s>>>(p);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
     }

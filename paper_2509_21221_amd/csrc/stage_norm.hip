@@ -112,13 +112,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwt
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int col = ((k * WAVES + part) * 64 + lane) * kVec, n = H - col;
-        if (p.h_out) store8(static_cast<T *>(p.h_out) + row * p.h_stride + col, n, h[k]);
+        if (p.h_out) store8<T, STREAM>(static_cast<T *>(p.h_out) + row * p.h_stride + col, n, h[k]);
         float w[8];
         load8(weight + col, n, w);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) h[k][i] = h[k][i] * rstd * w[i];
         if (p.form == GWTF_NORM_PLAIN) {
-            store8(static_cast<T *>(p.y) + row * p.y_stride + col, n, h[k]);
+            store8<T, STREAM>(static_cast<T *>(p.y) + row * p.y_stride + col, n, h[k]);
             continue;
         }
         uint32_t m = 0;
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_grad_kerne
             const int col = ((k * WAVES + part) * 64 + lane) * kVec;
 #pragma unroll
             for (int i = 0; i < kVec; ++i) d[k][i] += rstd * (g[k][i] - xh[k][i] * c);
-            store8(static_cast<T *>(p.dx) + row * p.dx_stride + col, H - col, d[k]);
+            store8<T, STREAM>(static_cast<T *>(p.dx) + row * p.dx_stride + col, H - col, d[k]);
         }
     }
     if (!partial) return;
@@ -308,8 +308,10 @@ hipError_t run_norm(const gwtf_stage_norm_t &a, hipStream_t s)
     const int64_t rows = WAVES == 1 ? 4 : 1;
     const int64_t values = 1 + (a.residual != nullptr) + (a.h_out != nullptr) + (a.form == GWTF_NORM_PLAIN);
     const int64_t bytes = a.num_tokens * a.hidden * (values * int64_t(sizeof(T)) + (a.form != GWTF_NORM_PLAIN));
-    const bool stream = bytes >= kMemoryCacheBytes && on_lines(a.x, a.x_stride, sizeof(T)) &&
-                        (!a.residual || on_lines(a.residual, a.residual_stride, sizeof(T)));
+    const bool stream = bytes >= kStreamBytes && on_lines(a.x, a.x_stride, sizeof(T)) &&
+                        (!a.residual || on_lines(a.residual, a.residual_stride, sizeof(T))) &&
+                        (!a.h_out || on_lines(a.h_out, a.h_stride, sizeof(T))) &&
+                        (a.form != GWTF_NORM_PLAIN || on_lines(a.y, a.y_stride, sizeof(T)));
     auto kernel = stream ? norm_kernel<T, K, WAVES, true, true> : norm_kernel<T, K, WAVES, false, true>;
     if (K == 1 && WAVES == 1 && a.hidden < kVec) kernel = norm_kernel<T, 1, 1, false, false>;
     kernel<<<dim3(uint32_t((a.num_tokens + rows - 1) / rows)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a);
@@ -323,8 +325,9 @@ hipError_t run_norm_grad(const gwtf_stage_norm_grad_t &a, const StageWorkspace &
     int64_t groups = (a.num_tokens + rows - 1) / rows;
     if (groups > kNormGradGroups) groups = kNormGradGroups;
     const int64_t bytes = a.num_tokens * a.hidden * int64_t(sizeof(T)) * (a.dh ? 4 : 3);
-    const bool stream = bytes >= kMemoryCacheBytes && on_lines(a.dy, a.dy_stride, sizeof(T)) &&
-                        on_lines(a.h, a.h_stride, sizeof(T)) && (!a.dh || on_lines(a.dh, a.dh_stride, sizeof(T)));
+    const bool stream = bytes >= kStreamBytes && on_lines(a.dy, a.dy_stride, sizeof(T)) &&
+                        on_lines(a.h, a.h_stride, sizeof(T)) && (!a.dh || on_lines(a.dh, a.dh_stride, sizeof(T))) &&
+                        on_lines(a.dx, a.dx_stride, sizeof(T));
     auto kernel = stream ? norm_grad_kernel<T, K, WAVES, true, true> : norm_grad_kernel<T, K, WAVES, false, true>;
     if (K == 1 && WAVES == 1 && a.hidden < kVec) kernel = norm_grad_kernel<T, 1, 1, false, false>;
     kernel<<<dim3(uint32_t(groups)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a, a.dweight ? w.dweight : nullptr);
