@@ -76,19 +76,23 @@ struct FillParams {
     int32_t stream;   // zeros past the caches
 };
 
+// In accesses on 16-byte boundaries, and halfwords before the first and after
+// the last.
 template <bool STREAM>
 __device__ __forceinline__ void zero_row(char *g, int64_t bytes)
 {
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     const u32x4 z = {0, 0, 0, 0};
-    for (int64_t at = (threadIdx.x & 63) * 16; at < bytes; at += 64 * 16) {
-        if (at + 16 <= bytes) {
-            if constexpr (STREAM) __builtin_nontemporal_store(z, reinterpret_cast<u32x4 *>(g + at));
-            else *reinterpret_cast<u32x4 *>(g + at) = z;
-        } else {
-            for (int64_t i = at; i < bytes; i += 2) *reinterpret_cast<uint16_t *>(g + i) = 0;
-        }
+    const int lane = threadIdx.x & 63;
+    int64_t head = -reinterpret_cast<uintptr_t>(g) & 15;
+    if (head > bytes) head = bytes;
+    const int64_t end = head + ((bytes - head) & ~int64_t(15));
+    if (lane * 2 < head) *reinterpret_cast<uint16_t *>(g + lane * 2) = 0;
+    for (int64_t at = head + lane * 16; at < end; at += 64 * 16) {
+        if constexpr (STREAM) __builtin_nontemporal_store(z, reinterpret_cast<u32x4 *>(g + at));
+        else *reinterpret_cast<u32x4 *>(g + at) = z;
     }
+    if (end + lane * 2 < bytes) *reinterpret_cast<uint16_t *>(g + end + lane * 2) = 0;
 }
 
 __device__ __forceinline__ void fill_rows(const FillParams &p, int group, const uint32_t *absent, int threads)
@@ -517,8 +521,8 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
     p.sorted = w.sort_a;
     // zeros past the caches where the table is larger than the L2s together
     // (2,048 x 1024 into 131 MB 27 us, 32 through them; 16,384 x 4096 into 262 MB
-    // 89 and 93)
-    const bool large_table = a.vocab * a.hidden * int64_t(sizeof(G)) >= kL2Bytes && on_lines(a.grad, a.grad_stride, sizeof(G));
+    // 89 and 93; 5,000 x 777 f32 into 50,000 rows 47 and 62)
+    const bool large_table = a.vocab * a.hidden * int64_t(sizeof(G)) >= kL2Bytes;
     const int64_t bytes = ((a.accumulate ? 0 : a.vocab) * int64_t(sizeof(G)) + N * int64_t(sizeof(T))) * a.hidden;
     p.stream = bytes >= kStreamBytes && on_lines(a.dout, a.dout_stride, sizeof(T));
     p.partial = w.partial;
