@@ -27,7 +27,7 @@
 // Ties go by index throughout: units are ordered as their columns are.
 //
 // A long batch is bound by memory with vector issue close behind (4,096 rows of
-// 131,072 bf16, four alternatives: 197 us for 1.07 GB, 5.4 TB/s; about 11
+// 131,072 bf16, four alternatives: 197 us for 1.07 GB, 5.4 TB/s; nine vector
 // instructions an entry, one of them the exponential at four times the others'
 // issue).  A few rows are shared by workgroups and bound by what follows one
 // another: the read, the selection, the record, the arrival (seven rows of

@@ -162,7 +162,8 @@ class StageOps:
     A row is one token of any microbatch; matrices are two-dimensional tensors
     of float32, float16 or bfloat16 whose columns are adjacent (rows may be
     any distance apart), index vectors contiguous int32 or int64.  New tensors
-    are returned unless ``out`` is given.  Work runs on ``stream`` (by default
+    are returned unless ``out`` is given; autograd is not involved, gradients
+    are calls of their own.  Work runs on ``stream`` (by default
     the current one when the object is made); called on another stream, an
     operator waits for that stream first and that stream waits for it.
     """
@@ -191,10 +192,11 @@ class StageOps:
     # ---- arguments ----
 
     def _type(self, t, name):
-        try:
-            return self._types[t.dtype]
-        except KeyError:
-            raise ValueError(f"{name}: need float32, float16 or bfloat16, not {t.dtype}") from None
+        if not isinstance(t, self.torch.Tensor):
+            raise TypeError(f"{name}: expected a torch tensor")
+        if t.dim() != 2 or t.dtype not in self._types:
+            raise ValueError(f"{name}: need a matrix of float32, float16 or bfloat16, not {t.dtype} {tuple(t.shape)}")
+        return self._types[t.dtype]
 
     def _mat(self, t, shape, dtype, name):
         if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device:
@@ -243,10 +245,13 @@ class StageOps:
         kind = self._type(table, "table")
         ids, idk = self._ids(tokens, "tokens")
         n, (v, h) = tokens.shape[0], table.shape
+        tab = self._mat(table, table.shape, table.dtype, "table")
         if out is None:
             out = table.new_empty((n, h))
-        a = gwtf_stage_embed_t(n, h, v, kind, idk, scale, ids, *self._mat(table, table.shape, table.dtype, "table"),
-                               *self._mat(out, (n, h), table.dtype, "out"))
+            to = out.data_ptr(), h
+        else:
+            to = self._mat(out, (n, h), table.dtype, "out")
+        a = gwtf_stage_embed_t(n, h, v, kind, idk, scale, ids, *tab, *to)
         self._run("embed", a, (tokens, table, out))
         return out
 
@@ -279,13 +284,15 @@ class StageOps:
         if not 0 <= seed < 1 << 64 or not 0 <= site < 1 << 32:
             raise ValueError("seed must fit in 64 bits and site in 32, both >= 0")
         shape, dt = x.shape, x.dtype
+        xs = self._mat(x, shape, dt, "x")
         if out is None:
             out = torch.empty_like(x)
+            to = out.data_ptr(), shape[1]
+        else:
+            to = self._mat(out, shape, dt, "out")
         a = gwtf_stage_dropout_t(shape[0], shape[1], kind, site, seed, p,
-                                 None if rows is None else self._vec(rows, shape[0], torch.int64, "rows"),
-                                 *self._mat(x, shape, dt, "x"),
-                                 *((None, 0) if residual is None else self._mat(residual, shape, dt, "residual")),
-                                 *self._mat(out, shape, dt, "out"))
+                                 None if rows is None else self._vec(rows, shape[0], torch.int64, "rows"), *xs,
+                                 *((None, 0) if residual is None else self._mat(residual, shape, dt, "residual")), *to)
         self._run("dropout", a, (x, rows, residual, out))
         return out
 
@@ -303,21 +310,26 @@ class StageOps:
         n, h = shape
         groups = (n, 1 if form == GWTF_NORM_F8_ROW else -(-h // GWTF_NORM_BLOCK))
         f32, ydt = torch.float32, torch.float8_e4m3fn if form else dt
+        xs = self._mat(x, shape, dt, "x")
         if out is None:
             new = self._f32.new_empty
-            out = (torch.empty_like(x, dtype=ydt), new(groups) if form else None,
-                   None if residual is None else torch.empty_like(x), new((n,)))
-        y, scales, hout, rstd = out
-        if form:
-            sc = self._mat(scales, groups, f32, "scales")[0]
-            if not scales.is_contiguous():
+            y, scales = torch.empty_like(x, dtype=ydt), new(groups) if form else None
+            hout, rstd = None if residual is None else torch.empty_like(x), new((n,))
+            out = y, scales, hout, rstd
+            to = y.data_ptr(), h
+            ho = (None, 0) if hout is None else (hout.data_ptr(), h)
+            sc, rs = scales.data_ptr() if form else None, rstd.data_ptr()
+        else:
+            y, scales, hout, rstd = out
+            to = self._mat(y, shape, ydt, "y")
+            ho = (None, 0) if hout is None else self._mat(hout, shape, dt, "h")
+            sc = self._mat(scales, groups, f32, "scales")[0] if form else None
+            if form and not scales.is_contiguous():
                 raise ValueError("scales: must be contiguous")
-        a = gwtf_stage_norm_t(n, h, kind, form, eps, *self._mat(x, shape, dt, "x"),
+            rs = None if rstd is None else self._vec(rstd, n, f32, "rstd")
+        a = gwtf_stage_norm_t(n, h, kind, form, eps, *xs,
                               *((None, 0) if residual is None else self._mat(residual, shape, dt, "residual")),
-                              self._vec(weight, h, dt, "weight"), *self._mat(y, shape, ydt, "y"),
-                              *((None, 0) if hout is None else self._mat(hout, shape, dt, "h")),
-                              sc if form else None,
-                              None if rstd is None else self._vec(rstd, n, f32, "rstd"))
+                              self._vec(weight, h, dt, "weight"), *to, *ho, sc, rs)
         self._run("norm", a, (x, residual, weight, y, scales, hout, rstd))
         return out
 
@@ -327,15 +339,18 @@ class StageOps:
         dx is the residual's gradient too; dweight is float32."""
         kind = self._type(h, "h")
         shape, dt, f32 = h.shape, h.dtype, self.torch.float32
+        hs = self._mat(h, shape, dt, "h")
         if out is None:
-            out = (self.torch.empty_like(h), self._f32.new_empty((shape[1],)))
-        dx, dw = out
-        a = gwtf_stage_norm_grad_t(shape[0], shape[1], kind, *self._mat(dy, shape, dt, "dy"),
-                                   *self._mat(h, shape, dt, "h"),
+            dx, dw = out = self.torch.empty_like(h), self._f32.new_empty((shape[1],))
+            to, dwp = (dx.data_ptr(), shape[1]), dw.data_ptr()
+        else:
+            dx, dw = out
+            to = self._mat(dx, shape, dt, "dx")
+            dwp = None if dw is None else self._vec(dw, shape[1], f32, "dweight")
+        a = gwtf_stage_norm_grad_t(shape[0], shape[1], kind, *self._mat(dy, shape, dt, "dy"), *hs,
                                    *((None, 0) if dh is None else self._mat(dh, shape, dt, "dh")),
                                    self._vec(weight, shape[1], dt, "weight"), self._vec(rstd, shape[0], f32, "rstd"),
-                                   *self._mat(dx, shape, dt, "dx"),
-                                   None if dw is None else self._vec(dw, shape[1], f32, "dweight"))
+                                   *to, dwp)
         self._run("norm_grad", a, (dy, h, dh, weight, rstd, dx, dw))
         return out
 
@@ -388,14 +403,17 @@ class StageOps:
                 raise ValueError(f"targets: need {n} of them")
         if dentropy is not None and entropy is None:
             raise ValueError("dentropy needs entropy")
+        xs = self._mat(logits, shape, dt, "logits")
         if out is None:
             out = self.torch.empty_like(logits)
-        a = gwtf_stage_logprob_grad_t(n, v, kind, idk, *self._mat(logits, shape, dt, "logits"), ids,
+            to = out.data_ptr(), v
+        else:
+            to = self._mat(out, shape, dt, "out")
+        a = gwtf_stage_logprob_grad_t(n, v, kind, idk, *xs, ids,
                                       self._vec(lse, n, f32, "lse"),
                                       None if dentropy is None else self._vec(entropy, n, f32, "entropy"),
                                       None if dlogp is None else self._vec(dlogp, n, f32, "dlogp"),
-                                      None if dentropy is None else self._vec(dentropy, n, f32, "dentropy"),
-                                      *self._mat(out, shape, dt, "out"))
+                                      None if dentropy is None else self._vec(dentropy, n, f32, "dentropy"), *to)
         self._run("logprob_grad", a, (logits, targets, lse, entropy, dlogp, dentropy, out))
         return out
 

@@ -587,6 +587,9 @@ def test_refusals():
     with ops(4, 16, 8) as s:
         table = torch.zeros((8, 16), device="cuda")
         bad = [
+            (TypeError, lambda: s.embed(t, [[0.0]])),
+            (ValueError, lambda: s.dropout(x[0], 0.1, 0, 0)),
+            (ValueError, lambda: s.norm(x[None], w)),
             (ValueError, lambda: s.embed(t, table.double())),
             (ValueError, lambda: s.embed(t.float(), table)),
             (ValueError, lambda: s.embed(t[::2], table)),
