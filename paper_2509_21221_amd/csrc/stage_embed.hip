@@ -10,6 +10,12 @@
 // writes a run that lies within its chunk to the table; the parts of a run
 // that crosses chunks are added in order by a launch of their own.  No
 // floating-point atomics: the same inputs give the same bits.
+//
+// Bound by memory where tokens or table are many: 16,384 rows of 4096 bf16 into
+// 32,000 (396 MB) take 88 us, of which the sums read 134 MB and write 50 in 37
+// and the other launches write the rest at about 4.5 TB/s; 2,048 x 1024 into
+// 131 MB 27 us.  A short call is bound by its three launches and their reads:
+// sort 6.6 us, sums 5, join 5.
 #include "stage_device.h"
 #include "stage_internal.h"
 
@@ -143,9 +149,9 @@ __device__ __forceinline__ void fill_later(const FillParams &p, int group, int t
 // workgroup sorts kSortBlock of them (bitonic), two adjacent keys a thread:
 // exchanges over up to 64 keys stay within a thread or a wave, only those over
 // more, 10 of 66, go through LDS with a barrier (6.6 us a block with 32-bit
-// keys, 9 with 64; 15 with all exchanges in LDS).  Up to kMergeWays sorted blocks are merged in one launch, where each
-// key finds its place by a binary search in every other block.  Workgroups
-// after the sorting ones write zeros.
+// keys, 9 with 64; 15 with all exchanges in LDS).  Up to kMergeWays sorted
+// blocks are merged in one launch, where each key finds its place by a binary
+// search in every other block.  Workgroups after the sorting ones write zeros.
 
 constexpr int kSortBlock = 2048;
 constexpr int kMergeWays = 32;
