@@ -258,7 +258,7 @@ constexpr int kMergeKeys = kMergeThreads / 4;
 constexpr int kSearches = kMergeWays / 4;
 
 __global__ __launch_bounds__(kMergeThreads) void merge_kernel(const uint64_t *in, uint32_t N, uint32_t len, int shift,
-                                                              uint64_t *out, uint32_t blocks, FillParams f)
+                                                              uint64_t *out, uint32_t block0, uint32_t blocks, FillParams f)
 {
     __shared__ uint64_t sample[kSamples];
     if (blockIdx.x >= blocks) {
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(const uint64_t *in
     }
     // a workgroup's adjacent keys lie within one block, as len is a multiple of
     // their number; offsets below are within the group of blocks
-    const uint32_t i0 = blockIdx.x * uint32_t(kMergeKeys), own = i0 / len, group0 = own / kMergeWays * kMergeWays;
+    const uint32_t i0 = (block0 + blockIdx.x) * uint32_t(kMergeKeys), own = i0 / len, group0 = own / kMergeWays * kMergeWays;
     const int64_t start = int64_t(group0) * len;
     const uint64_t *const g = in + start;
     const uint32_t total = uint32_t(N - start < int64_t(len) * kMergeWays ? N - start : int64_t(len) * kMergeWays);
@@ -410,24 +410,25 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradParams p)
             fill_later(p.fill, int(blockIdx.x - p.fill_block), 256);
             return;
         }
-        const int64_t v0 = ((blockIdx.x - p.fill_block) * 4 + wave) * int64_t(kSearchRows);
-        if (v0 >= a.vocab) return;
-        bool absent = false;
-        if (lane < kSearchRows && v0 + lane < a.vocab) {
-            const uint64_t k = uint64_t(v0 + lane) << 32;
-            int64_t lo = 0, hi = N;
-            while (lo < hi) {
-                const int64_t mid = (lo + hi) >> 1;
-                if (p.sorted[mid] < k) lo = mid + 1;
-                else hi = mid;
+        const int64_t step = (gridDim.x - p.fill_block) * 4 * kSearchRows;
+        for (int64_t v0 = ((blockIdx.x - p.fill_block) * 4 + wave) * kSearchRows; v0 < a.vocab; v0 += step) {
+            bool absent = false;
+            if (lane < kSearchRows && v0 + lane < a.vocab) {
+                const uint64_t k = uint64_t(v0 + lane) << 32;
+                int64_t lo = 0, hi = N;
+                while (lo < hi) {
+                    const int64_t mid = (lo + hi) >> 1;
+                    if (p.sorted[mid] < k) lo = mid + 1;
+                    else hi = mid;
+                }
+                absent = lo == N || key_token(p.sorted[lo]) != uint32_t(v0 + lane);
             }
-            absent = lo == N || key_token(p.sorted[lo]) != uint32_t(v0 + lane);
-        }
-        uint64_t rows = __ballot(absent);
-        while (rows) {
-            const int r = __builtin_ctzll(rows);
-            rows &= rows - 1;
-            zero_row<false>(static_cast<char *>(a.grad) + (v0 + r) * a.grad_stride * int64_t(sizeof(G)), a.hidden * int64_t(sizeof(G)));
+            uint64_t rows = __ballot(absent);
+            while (rows) {
+                const int r = __builtin_ctzll(rows);
+                rows &= rows - 1;
+                zero_row<false>(static_cast<char *>(a.grad) + (v0 + r) * a.grad_stride * int64_t(sizeof(G)), a.hidden * int64_t(sizeof(G)));
+            }
         }
         return;
     }
@@ -582,8 +583,12 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
             int shift = 4;
             while ((len * kMergeWays) >> shift > kSamples) ++shift;
             fill = groups ? take_share(true) : 0; // one merge at most beside a fill: N <= kSortBlock * kMergeWays
-            merge_kernel<<<dim3(blocks + fill), dim3(kMergeThreads), 0, s>>>(from, uint32_t(N), uint32_t(len), shift, to, blocks, f);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
+            constexpr uint32_t slab = uint32_t(kLaunchThreads / kMergeThreads);
+            for (uint32_t b = 0; b < blocks; b += slab) {
+                const uint32_t n = blocks - b < slab ? blocks - b : slab;
+                merge_kernel<<<dim3(n + fill), dim3(kMergeThreads), 0, s>>>(from, uint32_t(N), uint32_t(len), shift, to, b, n, f);
+                if ((e = hipGetLastError()) != hipSuccess) return e;
+            }
             uint64_t *t = from;
             from = to;
             to = t;
@@ -591,7 +596,13 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
         p.sorted = from;
     }
     p.fill_block = (p.chunks * p.slabs + 3) / 4;
-    const int64_t fill = p.search ? (a.vocab + 4 * kSearchRows - 1) / (4 * kSearchRows) : take_share(short_sums);
+    int64_t fill = 0;
+    if (p.search) {
+        fill = (a.vocab + 4 * kSearchRows - 1) / (4 * kSearchRows);
+        if (fill > kLaunchThreads / 256 - p.fill_block) fill = kLaunchThreads / 256 - p.fill_block;
+    } else {
+        fill = take_share(short_sums);
+    }
     if (p.fill_block + fill == 0) return hipSuccess;
     embed_grad_kernel<T, G><<<dim3(uint32_t(p.fill_block + fill)), dim3(256), 0, s>>>(p);
     if ((e = hipGetLastError()) != hipSuccess) return e;

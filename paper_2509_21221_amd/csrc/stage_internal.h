@@ -49,6 +49,9 @@ constexpr int kLogprobRecord = 16 + 8 * GWTF_STAGE_MAX_TOP;
 // 20 / 28.
 constexpr int64_t kStreamBytes = int64_t(96) << 20;
 constexpr int64_t kL2Bytes = int64_t(32) << 20; // of all XCDs
+// A launch has fewer than 2^32 threads; calls that want more are cut into launches
+// of this many at most.
+constexpr int64_t kLaunchThreads = int64_t(1) << 31;
 inline bool on_lines(const void *p, int64_t stride, size_t size)
 {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * int64_t(size) % 16 == 0;

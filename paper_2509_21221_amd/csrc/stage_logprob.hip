@@ -712,8 +712,7 @@ hipError_t run_logprob(const gwtf_stage_logprob_t &a, const StageWorkspace &w, h
     // columns as the kernel counts them
     const bool aligned = on_lines(a.logits, a.num_tokens > 1 ? a.logits_stride : 0, sizeof(T));
     split_rows(p, a.num_tokens, a.vocab + (aligned ? 0 : 16 / int64_t(sizeof(T)) - 1), 2 * kStep, 1024);
-    // a launch's workgroups stay below 2^31
-    const int64_t slab = (int64_t(1) << 30) / p.segments;
+    const int64_t slab = kLaunchThreads / kLpThreads / p.segments;
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
         p.a = a;
@@ -745,7 +744,7 @@ hipError_t run_logprob_grad(const gwtf_stage_logprob_grad_t &a, hipStream_t s)
     split_rows(p, a.num_tokens, a.vocab, kGradStep, 2048);
     const bool stream = 2 * a.num_tokens * a.vocab * int64_t(sizeof(T)) >= kStreamBytes;
     auto kernel = stream ? logprob_grad_kernel<T, true> : logprob_grad_kernel<T, false>;
-    const int64_t slab = (int64_t(1) << 30) / p.segments;
+    const int64_t slab = kLaunchThreads / 256 / p.segments;
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
         p.a = a;

@@ -75,12 +75,12 @@ __device__ __forceinline__ void quantise(float y[8], float s)
 }
 
 template <class T, int K, int WAVES, bool STREAM, bool WIDE>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwtf_stage_norm_t p)
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwtf_stage_norm_t p, int64_t row0)
 {
     __shared__ float red[WAVES];
     __shared__ uint32_t redmax[WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = WAVES == 1 ? int64_t(blockIdx.x) * 4 + wave : int64_t(blockIdx.x);
+    const int64_t row = row0 + (WAVES == 1 ? int64_t(blockIdx.x) * 4 + wave : int64_t(blockIdx.x));
     if (row >= p.num_tokens) return; // WAVES == 1 only: no barrier follows
     const int part = WAVES == 1 ? 0 : wave;
     const T *x = static_cast<const T *>(p.x) + row * p.x_stride;
@@ -320,8 +320,15 @@ hipError_t run_norm(const gwtf_stage_norm_t &a, hipStream_t s)
                         (a.form != GWTF_NORM_PLAIN || on_lines(a.y, a.y_stride, sizeof(T)));
     auto kernel = stream ? norm_kernel<T, K, WAVES, true, true> : norm_kernel<T, K, WAVES, false, true>;
     if (K == 1 && WAVES == 1 && a.hidden < kVec) kernel = norm_kernel<T, 1, 1, false, false>;
-    kernel<<<dim3(uint32_t((a.num_tokens + rows - 1) / rows)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a);
-    return hipGetLastError();
+    constexpr int threads = WAVES == 1 ? 256 : WAVES * 64;
+    const int64_t slab = kLaunchThreads / threads * rows;
+    for (int64_t r = 0; r < a.num_tokens; r += slab) {
+        const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
+        kernel<<<dim3(uint32_t((n + rows - 1) / rows)), dim3(threads), 0, s>>>(a, r);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <class T, int K, int WAVES>

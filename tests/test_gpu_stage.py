@@ -703,3 +703,51 @@ def test_graph_replays():
             for a, b in zip(got, step()):
                 assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
             stream.synchronize()
+
+
+# ---- more rows than one launch has threads for ----
+
+
+@pytest.mark.parametrize("h, n", [(1, (1 << 26) + 5), (9, (1 << 25) + 3)])
+def test_norm_of_many_rows(h, n):
+    t = torch_()
+    x = t.full((n, h), 3.0, dtype=t.float16, device="cuda")
+    x[-1] = -2.0
+    w = t.ones(h, dtype=t.float16, device="cuda")
+    y = t.zeros_like(x)
+    rstd = t.zeros(n, dtype=t.float32, device="cuda")
+    with ops(n, h) as s:
+        s.norm(x, w, eps=0.0, out=(y, None, None, rstd))
+        assert bool((y[:-1] == 1).all()) and bool((y[-1] == -1).all())
+        assert bool(((rstd[:-1] - 1 / 3).abs() < 1e-6).all()) and abs(rstd[-1].item() - 0.5) < 1e-6
+
+
+def test_logprob_of_many_rows():
+    t = torch_()
+    n = (1 << 24) + 3  # one workgroup a row
+    x = t.zeros((n, 2), dtype=t.bfloat16, device="cuda")
+    x[-1, 1] = 4.0
+    target = t.ones(n, dtype=t.int32, device="cuda")
+    with ops(n, 1, 2) as s:
+        logp, entropy, lse, top_logp, top_ids = s.logprob(x, target, top=1)
+        d = s.logprob_grad(x, target, lse, dlogp=t.ones(n, device="cuda"))
+    ln2, last = np.log(2.0), np.log1p(np.exp(-4.0))
+    for got, want in ((logp, -ln2), (entropy, ln2), (lse, ln2), (top_logp[:, 0], -ln2)):
+        assert bool(((got[:-1] - want).abs() < 1e-6).all())
+    assert bool((top_ids[:-1] == 0).all()) and top_ids[-1].item() == 1
+    assert abs(logp[-1].item() + last) < 1e-6
+    assert bool((d[:-1, 0] == -0.5).all()) and bool((d[:-1, 1] == 0.5).all())
+    assert abs(d[-1, 1].item() - (1 - np.exp(-last))) < 1e-3
+
+
+@pytest.mark.parametrize("n", [0, 40000])
+def test_embed_grad_of_the_largest_tables(n):
+    t = torch_()
+    v = (1 << 30) + 5  # 16 rows a wave: more than 2^32 threads
+    tokens = t.full((n,), v - 2, dtype=t.int64, device="cuda")
+    g = t.full((v, 1), 7.0, dtype=t.float16, device="cuda")
+    with ops(max(n, 1), 1, v) as s:
+        s.embed_grad(tokens, t.ones((n, 1), dtype=t.float16, device="cuda"), v, out=g)
+    assert g[v - 2, 0].item() == n and g[v - 1, 0].item() == 0
+    g[v - 2] = 0
+    assert int(g.count_nonzero()) == 0
