@@ -553,11 +553,11 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
         int64_t g = 2 * int64_t(w.cus) - busy;
         if (g < w.cus) g = w.cus;
         if (g > a.vocab) g = a.vocab;
+        // whatever the number of CUs, a workgroup's bits fit in its LDS
+        if (g < (a.vocab + kFillRows - 1) / kFillRows) g = (a.vocab + kFillRows - 1) / kFillRows;
         if (a.vocab <= kAbsentRows) {
             f.absent = w.absent;
             shares = 1 + merged + short_sums + joined;
-        } else if (g < (a.vocab + kFillRows - 1) / kFillRows) {
-            g = (a.vocab + kFillRows - 1) / kFillRows;
         }
         groups = uint32_t(g);
         rows = int((a.vocab + g - 1) / g);
@@ -625,11 +625,12 @@ int64_t embed_partial_bytes(int64_t max_tokens, int64_t max_hidden)
 }
 
 // A word more than the bits for each workgroup of the fill, of which there are
-// at most two a CU.
+// at most two a CU, or kAbsentRows / kFillRows on a device of few.
 int64_t embed_absent_bytes(int64_t max_vocab, int cus)
 {
     const int64_t rows = max_vocab < kAbsentRows ? max_vocab : kAbsentRows;
-    return (rows / 32 + 2 * (2 * int64_t(cus) + 1)) * int64_t(sizeof(uint32_t));
+    const int64_t few = kAbsentRows / kFillRows, groups = 2 * int64_t(cus) > few ? 2 * int64_t(cus) : few;
+    return (rows / 32 + 2 * (groups + 1)) * int64_t(sizeof(uint32_t));
 }
 
 hipError_t launch_embed(const gwtf_stage_embed_t &a, hipStream_t s)
