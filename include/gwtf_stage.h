@@ -162,7 +162,8 @@ gwtf_status_t gwtf_stage_dropout(gwtf_stage_t *h, const gwtf_stage_dropout_t *a)
 /* ---- Hand-off: residual, RMS norm, 8 bits ----
  *
  * h = x + residual; rstd = 1 / sqrt(mean(h^2) + eps); y = h * rstd * weight,
- * from the 32-bit sum h (h_out receives it rounded).  With an 8-bit form each
+ * from the 32-bit sum h (h_out receives it rounded), also where h^2 leaves the
+ * range of 32 bits and rstd does not.  With an 8-bit form each
  * row, or each GWTF_NORM_BLOCK columns of a row (the last block may be
  * shorter), has a 32-bit scale s = max(max |y| / 448, 2^-126), and y / s is
  * rounded to the nearest e4m3 value: y is about q * s.  A NaN or infinity

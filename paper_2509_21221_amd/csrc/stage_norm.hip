@@ -77,7 +77,7 @@ __device__ __forceinline__ void quantise(float y[8], float s)
 template <class T, int K, int WAVES, bool STREAM, bool WIDE>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwtf_stage_norm_t p, int64_t row0)
 {
-    __shared__ float red[WAVES];
+    __shared__ float red[WAVES], red_again[WAVES];
     __shared__ uint32_t redmax[WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row = row0 + (WAVES == 1 ? int64_t(blockIdx.x) * 4 + wave : int64_t(blockIdx.x));
@@ -111,7 +111,21 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(gwt
         for (int i = 0; i < kVec; ++i) sq += h[k][i] * h[k][i];
     }
     sq = group_sum<WAVES>(sq, red, part);
-    const float rstd = 1.f / sqrtf(sq / float(H) + p.eps);
+    float rstd = 1.f / sqrtf(sq / float(H) + p.eps);
+    // The squares' range is half that of the values: where it is left (by values
+    // of 2^57 and more, or of 2^-40 and less without an eps), in other units.
+    const bool large = !(sq <= 0x1.fffffep127f), small = sq < 0x1p-80f && p.eps < 0x1p-100f;
+    if (large || small) {
+        const float unit = large ? 0x1p-80f : 0x1p100f;
+        sq = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) sq += (h[k][i] * unit) * (h[k][i] * unit);
+        }
+        sq = group_sum<WAVES>(sq, red_again, part);
+        rstd = unit / sqrtf(sq / float(H) + p.eps * unit * unit);
+    }
     if (p.rstd && part == 0 && lane == 0) p.rstd[row] = rstd;
 
     uint32_t most = 0;

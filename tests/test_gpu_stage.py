@@ -254,6 +254,31 @@ def test_norm(dtype, n, h, pad):
                 assert (kept is None) == (residual is None)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("std", [2.0 ** 62, 2.0 ** 90, 2.0 ** 125, 2.0 ** -45, 2.0 ** -70, 2.0 ** -120])
+@pytest.mark.parametrize("h", [1, 300, 1000, 4096, 8201])
+def test_norm_where_squares_leave_32_bits(dtype, std, h):
+    r = np.random.default_rng(h)
+    n = 6
+    a = r.uniform(0.25, 1.5, (n, h)) * r.choice([-1.0, 1.0], (n, h)) * std
+    a[3] /= std  # a row of its own range between the others
+    x, xv = matrix(r, n, h, dtype, a=a)
+    w, wv = matrix(r, 1, h, dtype)
+    w, wv = w[0], wv[0]
+    _, rstd, y = O.norm(xv, wv, 0.0)
+    rel = (h / 2 + 16) * E
+    subnormal = 2.0 ** -149  # of rstd where it is the inverse of a large value
+    with ops(n, h) as s:
+        got, _, _, rs = s.norm(x, w, 0.0)
+        close(f64(rs), rstd, rel * rstd + subnormal, "rstd")
+        close(f64(got), y, (rel + U[dtype]) * np.abs(y) + 2 * subnormal * np.abs(xv * wv) + TINY[dtype], "y")
+        q, sc, _, _ = s.norm(x, w, 0.0, None, "row")
+        off = 2 * subnormal * np.abs(xv * wv)
+        ws = O.scales(y, "row")
+        close(f64(sc), ws, (rel + 3 * E) * ws + off.max(1, keepdims=True) / 448, "scales")
+        close(f64(q) * f64(sc), y, (2.0 ** -4 + 2 * rel) * np.abs(y) + 2.0 ** -10 * f64(sc) * (1 + 1e-6) + 2 * off, "q")
+
+
 @pytest.mark.parametrize("quant", ["row", "block"])
 def test_norm_8_bits_of_zeros_infinities_and_tiny_values(quant):
     torch = torch_()
