@@ -36,7 +36,8 @@
  * allocates or synchronises, so all may be captured into a HIP graph (one
  * graph, or eager calls, at a time: they share the handle's workspace).
  * Results are deterministic: the same inputs give the same bits, on every
- * call with the same shapes.  Sums, statistics and gradients are held in 32
+ * call with the same shapes (of log probabilities, with rows that also lie the
+ * same way to 16-byte boundaries).  Sums, statistics and gradients are held in 32
  * bits and rounded once to the output's type.
  */
 #ifndef GWTF_STAGE_H
@@ -163,11 +164,11 @@ gwtf_status_t gwtf_stage_dropout(gwtf_stage_t *h, const gwtf_stage_dropout_t *a)
  *
  * h = x + residual; rstd = 1 / sqrt(mean(h^2) + eps); y = h * rstd * weight,
  * from the 32-bit sum h (h_out receives it rounded), also where h^2 leaves the
- * range of 32 bits and rstd does not.  With an 8-bit form each
- * row, or each GWTF_NORM_BLOCK columns of a row (the last block may be
- * shorter), has a 32-bit scale s = max(max |y| / 448, 2^-126), and y / s is
- * rounded to the nearest e4m3 value: y is about q * s.  A NaN or infinity
- * among the y of a scale makes the scale and all of its values NaN. */
+ * range of 32 bits and rstd does not.  With an 8-bit form each row, or each
+ * GWTF_NORM_BLOCK columns of a row (the last block may be shorter), has a
+ * 32-bit scale s = max(max |y| / 448, 2^-126), and y / s is rounded to the
+ * nearest e4m3 value: y is about q * s.  A NaN or infinity among the y of a
+ * scale makes the scale and all of its values NaN. */
 typedef struct {
     int64_t num_tokens, hidden; /* N >= 0, 1 <= H <= GWTF_STAGE_MAX_HIDDEN */
     int32_t type;               /* GWTF_TYPE_* of x, residual, weight, h_out and a plain y */
