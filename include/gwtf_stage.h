@@ -220,7 +220,10 @@ gwtf_status_t gwtf_stage_norm_grad(gwtf_stage_t *h, const gwtf_stage_norm_grad_t
  * log probability -infinity; a row of nothing else gives lse = -infinity,
  * entropy 0 and alternatives 0, 1, 2, .. .  A NaN or +infinity makes lse,
  * entropy and the row's log probabilities NaN; a NaN is no alternative, and
- * alternatives that are missing for that have index -1. */
+ * alternatives that are missing for that have index -1.  Finite logits may have
+ * any value, masks of -1e30 or the type's lowest value among them: where a row's
+ * largest logit is beyond 9e4 in magnitude, so that lse in 32 bits does not
+ * resolve a probability, log probabilities come from differences to it. */
 typedef struct {
     int64_t num_tokens, vocab;  /* N >= 0, V >= 1 */
     int32_t type, token_type;   /* GWTF_TYPE_* of logits, GWTF_TOKEN_* of targets */
@@ -237,7 +240,9 @@ gwtf_status_t gwtf_stage_logprob(gwtf_stage_t *h, const gwtf_stage_logprob_t *a)
 /* Gradient of logp and entropy:
  *   dlogits[j] = dlogp * ([j == target] - p_j) - dentropy * p_j * (ln p_j + entropy)
  * from lse and entropy of the forward call.  dlogp counts as 0 where the
- * target is outside [0, vocab); a row whose lse is -infinity gets zeros.
+ * target is outside [0, vocab); a row whose lse is -infinity gets zeros.  p is
+ * exp(logits - lse), no better than the 32 bits of lse: a row whose largest
+ * logit is of the order of 1e5 or more is best shifted before both calls.
  * dlogits may be logits itself (same pointer and stride). */
 typedef struct {
     int64_t num_tokens, vocab;  /* N >= 0, V >= 1 */

@@ -6,12 +6,15 @@
 //   s = sum 2^(y - m)   and   t = sum 2^(y - m) (y - m),
 // both rescaled when m grows; parts with different m join the same way.  Then
 //   lse = ln 2 (m + log2 s),   entropy = ln 2 (log2 s - t / s),
-// where every term of t has one sign, so nothing cancels.  m is a rounded
-// product, which does no harm: it is the same number in y - m, one fused
-// operation, and in the result.  A row whose largest y is beyond 2^100, or
-// -infinity though its largest x is not (entries of the type's lowest value
-// overflow in y), is gone through again with (x - m) log2 e in place of y - m
-// (WIDE).
+// where every term of t has one sign, so nothing cancels.  The reference m of a
+// lane is the rounded product y of its largest x, the same number in y - m, one
+// fused operation, and in the result; what the rounding leaves is at most 2^-7
+// as long as |m| <= 2^17 (kRange; beyond about 2^31 it would leave the range of
+// the exponential).  So m starts at -2^17 and is never below: masked entries,
+// -infinity or finite, add what they are worth under that reference, nothing.  A
+// row whose largest y is not within (-2^17, 2^17] is gone through again with
+// (x - m) log2 e in place of y - m and m the largest x (WIDE); its log
+// probabilities are (x - m) - ln s, as lse in 32 bits does not resolve them.
 //
 // Columns are counted from the 16-byte boundary at or before the row's first
 // entry (`off` columns before it), so that all reads but the first are aligned
@@ -48,20 +51,27 @@ constexpr int kStep = kLpThreads * kUnit; // columns of a workgroup's step
 constexpr int kUnitTop = 24;
 constexpr float kLowest = -200.f; // 2^-200 is 0: keeps 0 * -infinity out of t
 constexpr float kNone = -__builtin_inff();
-constexpr float kLargeRef = 0x1p100f;
+constexpr float kRange = 0x1p17f; // the largest f16 is below it
 
 struct Softmax {
     float m, s, t;
 };
 
-__device__ __forceinline__ float finite_or_zero(float m) { return m == kNone ? 0.f : m; }
+// m as it is subtracted: finite where there is nothing but entries of -infinity.
+template <bool WIDE>
+__device__ __forceinline__ float reference(float m)
+{
+    return WIDE && m == kNone ? 0.f : m;
+}
+template <bool WIDE>
+__device__ __forceinline__ Softmax nothing() { return {WIDE ? kNone : -kRange, 0.f, 0.f}; }
 
 template <bool WIDE>
 __device__ __forceinline__ Softmax join(const Softmax &a, const Softmax &b)
 {
     Softmax r;
     r.m = fmaxf(a.m, b.m);
-    const float ms = finite_or_zero(r.m), f = WIDE ? kLog2e : 1.f;
+    const float ms = reference<WIDE>(r.m), f = WIDE ? kLog2e : 1.f;
     const float da = (a.m - ms) * f, db = (b.m - ms) * f;
     const float ea = exp2_(da), eb = exp2_(db);
     r.s = a.s * ea + b.s * eb;
@@ -78,7 +88,7 @@ __device__ __forceinline__ Softmax wave_join(const Softmax &a)
     m = fmaxf(m, row_ror<2>(m));
     m = fmaxf(m, row_ror<1>(m));
     m = fmaxf(fmaxf(lane_value(m, 0), lane_value(m, 16)), fmaxf(lane_value(m, 32), lane_value(m, 48)));
-    const float d = (a.m - finite_or_zero(m)) * (WIDE ? kLog2e : 1.f), e = exp2_(d);
+    const float d = (a.m - reference<WIDE>(m)) * (WIDE ? kLog2e : 1.f), e = exp2_(d);
     return {m, wave_sum(a.s * e), wave_sum(e * (a.t + fmaxf(d, kLowest) * a.s))};
 }
 
@@ -86,7 +96,7 @@ __device__ __forceinline__ Softmax wave_join(const Softmax &a)
 template <bool WIDE>
 __device__ __forceinline__ void add_unit(Softmax &r, const float v[kUnit], float x_max)
 {
-    const float m = WIDE ? x_max : x_max * kLog2e, ms = finite_or_zero(m);
+    const float m = WIDE ? x_max : fmaxf(x_max * kLog2e, -kRange), ms = reference<WIDE>(m);
     const float d0 = (r.m - ms) * (WIDE ? kLog2e : 1.f), e0 = exp2_(d0);
     r.t = e0 * (r.t + fmaxf(d0, kLowest) * r.s);
     r.s *= e0;
@@ -253,7 +263,12 @@ struct LogprobParams {
     uint32_t *arrived;  // [rows], 0 between calls
 };
 
-__device__ __forceinline__ float log_prob(float x, float lse) { return x == kNone && lse == lse ? x : x - lse; }
+// From lse = m + ln s; WIDE: from the parts.
+template <bool WIDE>
+__device__ __forceinline__ float log_prob(float x, float lse, float m, float ln_s)
+{
+    return x == kNone && lse == lse ? x : WIDE ? (x - m) - ln_s : x - lse;
+}
 
 // The values that a row's sums give, from lane 0 of the wave that joined it;
 // then its alternatives, from lanes below `top`.
@@ -262,18 +277,18 @@ __device__ __forceinline__ void finish_row(const gwtf_stage_logprob_t &a, int64_
                                            bool there, float xt)
 {
     const int lane = __lane_id();
-    const float ln_s = logf(r.s), m = finite_or_zero(r.m);
+    const float ln_s = logf(r.s), m = reference<WIDE>(r.m);
     // ln 2 in two parts: one product would lose the last bits of m
     const float lse = WIDE ? m + ln_s : fmaf(m, kLn2, fmaf(m, kLn2Low, ln_s));
     if (lane == 0) {
         if (a.lse) a.lse[row] = lse;
         if (a.entropy) a.entropy[row] = r.s == 0.f ? 0.f : ln_s - kLn2 * (r.t / r.s);
-        if (a.logp) a.logp[row] = there ? log_prob(xt, lse) : 0.f;
+        if (a.logp) a.logp[row] = there ? log_prob<WIDE>(xt, lse, m, ln_s) : 0.f;
     }
     if (lane < a.top) {
         const bool none = list.key == 0;
         const float x = value_of(int(key_order(list.key) ^ 0x80000000u));
-        a.top_logp[row * a.top + lane] = none ? __builtin_nanf("") : log_prob(x, lse);
+        a.top_logp[row * a.top + lane] = none ? __builtin_nanf("") : log_prob<WIDE>(x, lse, m, ln_s);
         a.top_ids[row * a.top + lane] = none ? -1 : int32_t(key_index(list.key));
     }
 }
@@ -296,7 +311,7 @@ __device__ __forceinline__ uint64_t get_key(const uint64_t *p)
 template <class T>
 __device__ __attribute__((noinline)) Softmax wide_pass(const T *x, int64_t vocab)
 {
-    Softmax r = {kNone, 0.f, 0.f};
+    Softmax r = nothing<true>();
     for (int64_t base = 0; base < vocab; base += kStep) {
         const int64_t col = base + threadIdx.x * kUnit;
         float v[kUnit];
@@ -420,7 +435,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
     const bool there = target >= 0 && target < a.vocab;
     float xt = 0.f;
     if (there) xt = float(x[target]);
-    Softmax r = {kNone, 0.f, 0.f};
+    Softmax r = nothing<false>();
     float first = kNone, second = kNone; // the largest entries of the lane's two units
     // The lane's first unit counts whatever it holds, so that rows of masked
     // entries have units too; others of -infinity come after 256 of these.
@@ -488,7 +503,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
         units_of[kLpThreads + threadIdx.x] = unit2 < 0 || unit2 == unit1 ? 0 : key_of(order_of(second), uint32_t(unit2));
     }
     __syncthreads();
-    r = wave_join<false>(lane < kLpWaves ? parts[lane] : Softmax{kNone, 0.f, 0.f});
+    r = wave_join<false>(lane < kLpWaves ? parts[lane] : nothing<false>());
     bool live = alive[0] | alive[1] | alive[2] | alive[3];
     TopList list;
     if constexpr (TOP) {
@@ -559,7 +574,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
         __syncthreads();
         if (!last_flag) return;
         const unsigned char *records = p.records + row * p.segments * kLogprobRecord;
-        r = {kNone, 0.f, 0.f};
+        r = nothing<false>();
         live = false;
         for (int i = lane; i < p.segments; i += 64) { // in all waves alike
             const uint32_t *w = reinterpret_cast<const uint32_t *>(records + i * kLogprobRecord);
@@ -593,13 +608,13 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
         if (threadIdx.x == 0) p.arrived[row] = 0;
     }
     // r is the row's, in all waves
-    if (live && !(fabsf(r.m) <= kLargeRef)) {
+    if (live && !(r.m > -kRange && r.m <= kRange)) {
         r = wide_pass(x, a.vocab);
         __syncthreads();
         if (lane == 0) parts[wave] = r;
         __syncthreads();
         if (wave != chief) return;
-        r = wave_join<true>(lane < kLpWaves ? parts[lane] : Softmax{kNone, 0.f, 0.f});
+        r = wave_join<true>(lane < kLpWaves ? parts[lane] : nothing<true>());
         finish_row<true>(a, row, r, list, there, xt);
     } else if (wave == chief) {
         finish_row<false>(a, row, r, list, there, xt);
