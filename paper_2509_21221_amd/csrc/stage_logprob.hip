@@ -25,8 +25,9 @@
 // of these over the workgroup hold all alternatives, since any other unit has
 // `top` entries before its first -- unless both of a lane's units are among
 // them and a third might be: then that lane's columns are looked through.  With
-// many alternatives, or too few units or entries that are numbers, the row is
-// gone through again with a list that is right for every input (list_pass).
+// many alternatives, a NaN in the row (a unit may then hold no alternative at all),
+// or too few units, it is gone through again with a list that is right for every
+// input (list_pass).
 // Ties go by index throughout: units are ordered as their columns are.
 //
 // A long batch is bound by memory with vector issue close behind (4,096 rows of
@@ -509,7 +510,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
     if constexpr (TOP) {
         // Nothing but masked entries (a NaN would show in s): the first columns.
         const bool masked = !live && r.s == 0.f;
-        bool again = a.top > kUnitTop && !masked;
+        bool again = !masked && (a.top > kUnitTop || !(r.s == r.s));
         list.start(a.top, slots);
         if (masked) {
             const int64_t col = (c0 > off ? c0 - off : 0) + lane;
