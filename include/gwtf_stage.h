@@ -166,9 +166,10 @@ gwtf_status_t gwtf_stage_dropout(gwtf_stage_t *h, const gwtf_stage_dropout_t *a)
  * from the 32-bit sum h (h_out receives it rounded), also where h^2 leaves the
  * range of 32 bits and rstd does not.  With an 8-bit form each row, or each
  * GWTF_NORM_BLOCK columns of a row (the last block may be shorter), has a
- * 32-bit scale s = max(max |y| / 448, 2^-126), and y / s is rounded to the
- * nearest e4m3 value: y is about q * s.  A NaN or infinity among the y of a
- * scale makes the scale and all of its values NaN. */
+ * 32-bit scale s = max(max |y| / 448, 2^-126), and y / s, rounded to 32 bits, to
+ * the nearest e4m3 value, the even one of two that are as near: y is about
+ * q * s.  A NaN or infinity among the y of a scale makes the scale and all of
+ * its values NaN. */
 typedef struct {
     int64_t num_tokens, hidden; /* N >= 0, 1 <= H <= GWTF_STAGE_MAX_HIDDEN */
     int32_t type;               /* GWTF_TYPE_* of x, residual, weight, h_out and a plain y */
