@@ -185,6 +185,7 @@ class StageOps:
         # hand (1.2 to 1.4 us each, torch.empty with a device 1.6) and calls go
         # to the library's functions directly
         self._f32 = torch.empty(0, dtype=torch.float32, device=self._dev)
+        self._i32 = torch.empty(0, dtype=torch.int32, device=self._dev)
         lib = _library()
         self._calls = {name: getattr(lib, "gwtf_stage_" + name) for name in _CALLS}
         self.handle = gwtf_stage_create(max_tokens, max_hidden, max_vocab, device, self._raw)
@@ -367,20 +368,16 @@ class StageOps:
         if not 0 <= top <= GWTF_STAGE_MAX_TOP:
             raise ValueError(f"top: outside [0, {GWTF_STAGE_MAX_TOP}]")
         ids, idk, logp = None, 0, None
+        new = self._f32.new_empty
         if targets is not None:
             ids, idk = self._ids(targets, "targets")
             if targets.shape[0] != n:
                 raise ValueError(f"targets: need {n} of them")
-        top_logp = top_ids = None
-        # one new tensor, cut up: 4.8 us, five of them 7.0
+            logp = new(n)
+        # tensors of their own (5.8 us for five): parts of one (4.8) would share its version and its life
+        entropy, lse, top_logp, top_ids = new(n), new(n), None, None
         if top:
-            logp, entropy, lse, top_logp, top_ids = self._f32.new_empty(n * (3 + 2 * top)).split_with_sizes(
-                (n, n, n, n * top, n * top))
-            top_logp, top_ids = top_logp.view(n, top), top_ids.view(self.torch.int32).view(n, top)
-        else:
-            logp, entropy, lse = self._f32.new_empty((3, n)).unbind(0)
-        if targets is None:
-            logp = None
+            top_logp, top_ids = new(n, top), self._i32.new_empty(n, top)
         a = gwtf_stage_logprob_t(n, v, kind, idk, top, *self._mat(logits, shape, logits.dtype, "logits"), ids,
                                  logp.data_ptr() if logp is not None else None, entropy.data_ptr(), lse.data_ptr(),
                                  top_logp.data_ptr() if top else None, top_ids.data_ptr() if top else None)
