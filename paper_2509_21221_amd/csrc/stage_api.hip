@@ -22,6 +22,7 @@ thread_local char g_stage_err[256];
 gwtf_status_t fail(gwtf_stage_t *h, gwtf_status_t code, const char *what, hipError_t e = hipSuccess)
 {
     char *to = h ? h->err : g_stage_err;
+    if (e != hipSuccess) (void)hipGetLastError(); // it is reported here, not to the thread's next reader
     if (e != hipSuccess) snprintf(to, sizeof g_stage_err, "%s: %s", what, hipGetErrorString(e));
     else snprintf(to, sizeof g_stage_err, "%s", what);
     return code;

@@ -115,11 +115,9 @@ hipError_t run(const gwtf_stage_dropout_t &a, uint32_t limit, hipStream_t s)
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
         p.row0 = r;
         p.units = uint32_t(n * steps);
-        const dim3 grid((p.units + 256 * kUnits - 1) / (256 * kUnits));
         auto kernel = p.res ? (stream ? dropout_kernel<T, true, true> : dropout_kernel<T, true, false>)
                             : (stream ? dropout_kernel<T, false, true> : dropout_kernel<T, false, false>);
-        kernel<<<grid, dim3(256), 0, s>>>(p);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch(kernel, (p.units + 256 * kUnits - 1) / (256 * kUnits), 256, s, p);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -501,8 +501,7 @@ hipError_t run_embed(const gwtf_stage_embed_t &a, hipStream_t s)
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
         p.row0 = r;
         p.units = uint32_t(n * steps);
-        kernel<<<dim3((p.units + 255) / 256), dim3(256), 0, s>>>(p);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch(kernel, (p.units + 255) / 256, 256, s, p);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -575,8 +574,7 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
         uint32_t blocks = uint32_t((N + kSortBlock - 1) / kSortBlock);
         uint32_t fill = take_share(true);
         auto sort = a.vocab < int64_t(1) << 21 ? sort_block_kernel<uint32_t> : sort_block_kernel<uint64_t>;
-        sort<<<dim3(blocks + fill), dim3(1024), 0, s>>>(a.tokens, a.token_type, a.vocab, N, w.sort_a, blocks, f);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        if ((e = launch(sort, blocks + fill, 1024, s, a.tokens, a.token_type, a.vocab, N, w.sort_a, blocks, f)) != hipSuccess) return e;
         uint64_t *from = w.sort_a, *to = w.sort_b;
         blocks = uint32_t((N + kMergeKeys - 1) / kMergeKeys);
         for (int64_t len = kSortBlock; len < N; len *= kMergeWays) {
@@ -586,8 +584,8 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
             constexpr uint32_t slab = uint32_t(kLaunchThreads / kMergeThreads);
             for (uint32_t b = 0; b < blocks; b += slab) {
                 const uint32_t n = blocks - b < slab ? blocks - b : slab;
-                merge_kernel<<<dim3(n + fill), dim3(kMergeThreads), 0, s>>>(from, uint32_t(N), uint32_t(len), shift, to, b, n, f);
-                if ((e = hipGetLastError()) != hipSuccess) return e;
+                e = launch(merge_kernel, n + fill, kMergeThreads, s, from, uint32_t(N), uint32_t(len), shift, to, b, n, f);
+                if (e != hipSuccess) return e;
             }
             uint64_t *t = from;
             from = to;
@@ -604,14 +602,8 @@ hipError_t run_embed_grad(const gwtf_stage_embed_grad_t &a, const StageWorkspace
         fill = take_share(short_sums);
     }
     if (p.fill_block + fill == 0) return hipSuccess;
-    embed_grad_kernel<T, G><<<dim3(uint32_t(p.fill_block + fill)), dim3(256), 0, s>>>(p);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (joined) {
-        const uint32_t last = take_share(true);
-        embed_join_kernel<G><<<dim3(uint32_t(p.fill_block) + last), dim3(256), 0, s>>>(p);
-        e = hipGetLastError();
-    }
-    return e;
+    if ((e = launch(embed_grad_kernel<T, G>, p.fill_block + fill, 256, s, p)) != hipSuccess || !joined) return e;
+    return launch(embed_join_kernel<G>, p.fill_block + take_share(true), 256, s, p);
 }
 
 } // namespace

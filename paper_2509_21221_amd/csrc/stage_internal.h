@@ -8,6 +8,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace gwtf {
 
 // Device workspace of a handle, used in the order of its stream.
@@ -55,6 +57,15 @@ constexpr int64_t kLaunchThreads = int64_t(1) << 31;
 inline bool on_lines(const void *p, int64_t stride, size_t size)
 {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * int64_t(size) % 16 == 0;
+}
+
+// Enqueues a kernel; the status is the launch's own (that of hipGetLastError may
+// be one that an earlier call of the thread, anybody's, has left).
+template <class... P>
+inline hipError_t launch(void (*kernel)(P...), int64_t groups, int threads, hipStream_t s, std::common_type_t<P>... args)
+{
+    void *list[] = {&args...};
+    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3(uint32_t(groups)), dim3(uint32_t(threads)), list, 0, s);
 }
 
 hipError_t launch_embed(const gwtf_stage_embed_t &a, hipStream_t s);

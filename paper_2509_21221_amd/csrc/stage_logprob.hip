@@ -744,10 +744,7 @@ hipError_t run_logprob(const gwtf_stage_logprob_t &a, const StageWorkspace &w, h
                 p.a.top_ids += r * a.top;
             }
         }
-        const dim3 grid(uint32_t(n * p.segments)), block(kLpWaves * 64);
-        if (a.top) logprob_kernel<T, true><<<grid, block, 0, s>>>(p);
-        else logprob_kernel<T, false><<<grid, block, 0, s>>>(p);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch(a.top ? logprob_kernel<T, true> : logprob_kernel<T, false>, n * p.segments, kLpThreads, s, p);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -772,8 +769,7 @@ hipError_t run_logprob_grad(const gwtf_stage_logprob_grad_t &a, hipStream_t s)
         if (a.entropy) p.a.entropy += r;
         if (a.dlogp) p.a.dlogp += r;
         if (a.dentropy) p.a.dentropy += r;
-        kernel<<<dim3(uint32_t(n * p.segments)), dim3(256), 0, s>>>(p);
-        const hipError_t err = hipGetLastError();
+        const hipError_t err = launch(kernel, n * p.segments, 256, s, p);
         if (err != hipSuccess) return err;
     }
     return hipSuccess;

@@ -344,8 +344,7 @@ hipError_t run_norm(const gwtf_stage_norm_t &a, hipStream_t s)
     const int64_t slab = kLaunchThreads / threads * rows;
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
-        kernel<<<dim3(uint32_t((n + rows - 1) / rows)), dim3(threads), 0, s>>>(a, r);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch(kernel, (n + rows - 1) / rows, threads, s, a, r);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -363,11 +362,9 @@ hipError_t run_norm_grad(const gwtf_stage_norm_grad_t &a, const StageWorkspace &
                         on_lines(a.dx, a.dx_stride, sizeof(T));
     auto kernel = stream ? norm_grad_kernel<T, K, WAVES, true, true> : norm_grad_kernel<T, K, WAVES, false, true>;
     if (K == 1 && WAVES == 1 && a.hidden < kVec) kernel = norm_grad_kernel<T, 1, 1, false, false>;
-    kernel<<<dim3(uint32_t(groups)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, s>>>(a, a.dweight ? w.dweight : nullptr);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = launch(kernel, groups, WAVES == 1 ? 256 : WAVES * 64, s, a, a.dweight ? w.dweight : nullptr);
     if (e != hipSuccess || !a.dweight) return e;
-    dweight_kernel<<<dim3(uint32_t((a.hidden + 15) / 16)), dim3(1024), 0, s>>>(w.dweight, int(groups), int(a.hidden), a.dweight);
-    return hipGetLastError();
+    return launch(dweight_kernel, (a.hidden + 15) / 16, 1024, s, w.dweight, int(groups), int(a.hidden), a.dweight);
 }
 
 // Waves and steps of a row by its width: 512 columns a wave and step.
@@ -410,8 +407,7 @@ hipError_t launch_norm_grad(const gwtf_stage_norm_grad_t &a, const StageWorkspac
 {
     if (a.num_tokens == 0) {
         if (!a.dweight) return hipSuccess;
-        zero_kernel<<<dim3(uint32_t((a.hidden + 255) / 256)), dim3(256), 0, s>>>(a.dweight, a.hidden);
-        return hipGetLastError();
+        return launch(zero_kernel, (a.hidden + 255) / 256, 256, s, a.dweight, a.hidden);
     }
     switch (a.type) {
     case GWTF_TYPE_F32: return norm_grad_typed<float>(a, w, s);
