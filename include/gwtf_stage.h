@@ -84,10 +84,10 @@ typedef struct {
 
 /* Creates a handle on shape->device that enqueues on `hip_stream` (a
  * hipStream_t; NULL = the device's null stream) and allocates its workspace:
- * 16 bytes a token; for the embedding's gradient up to 17 MB (2 * max_hidden
- * bytes a token where that is less) and a bit for each row of the table, 0.5
- * MB at most; for the norm's 2048 bytes a column, 34 MB at most; and 1.1 MB
- * for gwtf_stage_logprob.  *out receives the handle, or NULL on failure. */
+ * 16 bytes a token; for the embedding's gradient 16.8 MB and 8 bytes a column
+ * (where that is less, 8 bytes a column and 2 a column and token), and a bit for
+ * each row of the table, 0.6 MB at most; for the norm's 2048 bytes a column, 34
+ * MB at most; and 1.1 MB for gwtf_stage_logprob.  *out receives the handle, or NULL on failure. */
 gwtf_status_t gwtf_stage_create(const gwtf_stage_shape_t *shape, void *hip_stream, gwtf_stage_t **out);
 
 /* Frees the handle and its workspace after draining its stream; NULL-safe. */

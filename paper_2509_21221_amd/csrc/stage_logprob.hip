@@ -31,11 +31,11 @@
 // Ties go by index throughout: units are ordered as their columns are.
 //
 // A long batch is bound by memory with vector issue close behind (4,096 rows of
-// 131,072 bf16, four alternatives: 197 us for 1.07 GB, 5.4 TB/s; nine vector
+// 131,072 bf16, four alternatives: 194 us for 1.07 GB, 5.5 TB/s; nine vector
 // instructions an entry, one of them the exponential at four times the others'
 // issue).  A few rows are shared by workgroups and bound by what follows one
 // another: the read, the selection, the record, the arrival (seven rows of
-// 131,072, eight alternatives 10.4 us).  The gradient is bound by memory: 2,048 x
+// 131,072, eight alternatives 10.3 us).  The gradient is bound by memory: 2,048 x
 // 32,001 bf16 56 us (262 MB, 4.7 TB/s).
 #include "stage_device.h"
 #include "stage_internal.h"
@@ -643,7 +643,7 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobGradParams p)
     const T *x = static_cast<const T *>(a.logits) + row * a.logits_stride;
     T *out = static_cast<T *>(a.dlogits) + row * a.dlogits_stride;
     // Steps begin where the row of dlogits is aligned to 16 bytes (2,048 x
-    // 32,001: 47 us in place of 56); the columns before belong to the first part.
+    // 32,001 bf16: 56 us, 58 without); the columns before belong to the first part.
     int64_t head = (-reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T);
     if (head > a.vocab) head = a.vocab;
     const int64_t c0 = head + segment * p.width, c1 = c0 + p.width < a.vocab ? c0 + p.width : a.vocab;
