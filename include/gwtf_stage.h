@@ -217,6 +217,7 @@ gwtf_status_t gwtf_stage_norm_grad(gwtf_stage_t *h, const gwtf_stage_norm_grad_t
  * Per row of logits x: lse = ln sum exp(x); logp = x[target] - lse; entropy =
  * -sum p ln p with p = exp(x - lse); and the `top` largest x, largest first,
  * equal ones by ascending index: top_ids and their log probabilities top_logp.
+ * Rounding puts no log probability above 0 and no entropy below.
  * A target outside [0, vocab) gives logp 0.  An entry of -infinity is masked: p = 0,
  * log probability -infinity; a row of nothing else gives lse = -infinity,
  * entropy 0 and alternatives 0, 1, 2, .. .  A NaN or +infinity makes lse,

@@ -192,6 +192,16 @@ __device__ __forceinline__ float wave_sum(float v)
     return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
 
+// The largest over the wave, uniform; of a number and a NaN the number.
+__device__ __forceinline__ float wave_fmax(float v)
+{
+    v = fmaxf(v, row_ror<8>(v));
+    v = fmaxf(v, row_ror<4>(v));
+    v = fmaxf(v, row_ror<2>(v));
+    v = fmaxf(v, row_ror<1>(v));
+    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+
 // The largest of unsigned words likewise (float magnitudes compare as their
 // bits do, with infinities and NaN above all numbers).
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }

@@ -84,11 +84,7 @@ __device__ __forceinline__ Softmax join(const Softmax &a, const Softmax &b)
 template <bool WIDE>
 __device__ __forceinline__ Softmax wave_join(const Softmax &a)
 {
-    float m = fmaxf(a.m, row_ror<8>(a.m));
-    m = fmaxf(m, row_ror<4>(m));
-    m = fmaxf(m, row_ror<2>(m));
-    m = fmaxf(m, row_ror<1>(m));
-    m = fmaxf(fmaxf(lane_value(m, 0), lane_value(m, 16)), fmaxf(lane_value(m, 32), lane_value(m, 48)));
+    const float m = wave_fmax(a.m);
     const float d = (a.m - reference<WIDE>(m)) * (WIDE ? kLog2e : 1.f), e = exp2_(d);
     return {m, wave_sum(a.s * e), wave_sum(e * (a.t + fmaxf(d, kLowest) * a.s))};
 }
@@ -275,15 +271,19 @@ __device__ __forceinline__ float log_prob(float x, float lse, float m, float ln_
 // then its alternatives, from lanes below `top`.
 template <bool WIDE>
 __device__ __forceinline__ void finish_row(const gwtf_stage_logprob_t &a, int64_t row, const Softmax &r, const TopList &list,
-                                           bool there, float xt)
+                                           bool there, float xt, float x_max)
 {
     const int lane = __lane_id();
     const float ln_s = logf(r.s), m = reference<WIDE>(r.m);
-    // ln 2 in two parts: one product would lose the last bits of m
-    const float lse = WIDE ? m + ln_s : fmaf(m, kLn2, fmaf(m, kLn2Low, ln_s));
+    // ln 2 in two parts: one product would lose the last bits of m.  What rounding
+    // is left may not put lse below the row's largest entry, or entropy below 0.
+    float lse = WIDE ? m + ln_s : fmaf(m, kLn2, fmaf(m, kLn2Low, ln_s));
+    float entropy = r.s == 0.f ? 0.f : ln_s - kLn2 * (r.t / r.s);
+    if (lse < x_max) lse = x_max;
+    if (entropy < 0.f) entropy = 0.f;
     if (lane == 0) {
         if (a.lse) a.lse[row] = lse;
-        if (a.entropy) a.entropy[row] = r.s == 0.f ? 0.f : ln_s - kLn2 * (r.t / r.s);
+        if (a.entropy) a.entropy[row] = entropy;
         if (a.logp) a.logp[row] = there ? log_prob<WIDE>(xt, lse, m, ln_s) : 0.f;
     }
     if (lane < a.top) {
@@ -419,7 +419,8 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
     __shared__ Softmax parts[kLpWaves];
     __shared__ uint64_t units_of[TOP ? 2 * kLpThreads : 1]; // and each wave's slots
     // two words: a wave may still read the first when another writes the second
-    __shared__ uint32_t again_flag, last_flag, alive[kLpWaves];
+    __shared__ uint32_t again_flag, last_flag;
+    __shared__ float largest[kLpWaves];
     const gwtf_stage_logprob_t &a = p.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row = blockIdx.x / uint32_t(p.segments), segment = blockIdx.x - uint32_t(row) * uint32_t(p.segments);
@@ -492,11 +493,11 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
     }
     if (base < c1) ragged(base);
     {
-        const bool some = __ballot(first > kNone) != 0; // an entry that is not masked
+        const float x_max = wave_fmax(first);
         const Softmax mine = wave_join<false>(r);
         if (lane == 0) {
             parts[wave] = mine;
-            alive[wave] = some;
+            largest[wave] = x_max;
         }
     }
     if constexpr (TOP) {
@@ -505,7 +506,8 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
     }
     __syncthreads();
     r = wave_join<false>(lane < kLpWaves ? parts[lane] : nothing<false>());
-    bool live = alive[0] | alive[1] | alive[2] | alive[3];
+    float x_max = fmaxf(fmaxf(largest[0], largest[1]), fmaxf(largest[2], largest[3]));
+    bool live = x_max > kNone; // an entry that is not masked
     TopList list;
     if constexpr (TOP) {
         // Nothing but masked entries (a NaN would show in s): the first columns.
@@ -562,7 +564,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
                 put(w, __float_as_uint(r.m));
                 put(w + 1, __float_as_uint(r.s));
                 put(w + 2, __float_as_uint(r.t));
-                put(w + 3, live);
+                put(w + 3, __float_as_uint(x_max));
             }
             if constexpr (TOP) {
                 if (lane < a.top) put(reinterpret_cast<uint64_t *>(record + 16) + lane, list.key);
@@ -576,13 +578,14 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
         if (!last_flag) return;
         const unsigned char *records = p.records + row * p.segments * kLogprobRecord;
         r = nothing<false>();
-        live = false;
+        x_max = kNone;
         for (int i = lane; i < p.segments; i += 64) { // in all waves alike
             const uint32_t *w = reinterpret_cast<const uint32_t *>(records + i * kLogprobRecord);
             r = join<false>(r, Softmax{get_float(w), get_float(w + 1), get_float(w + 2)});
-            live |= __float_as_uint(get_float(w + 3)) != 0;
+            x_max = fmaxf(x_max, get_float(w + 3));
         }
-        live = __ballot(live) != 0;
+        x_max = wave_fmax(x_max);
+        live = x_max > kNone;
         r = wave_join<false>(r);
         if constexpr (TOP) {
             if (wave == chief) {
@@ -616,9 +619,9 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobParams p)
         __syncthreads();
         if (wave != chief) return;
         r = wave_join<true>(lane < kLpWaves ? parts[lane] : nothing<true>());
-        finish_row<true>(a, row, r, list, there, xt);
+        finish_row<true>(a, row, r, list, there, xt, x_max);
     } else if (wave == chief) {
-        finish_row<false>(a, row, r, list, there, xt);
+        finish_row<false>(a, row, r, list, there, xt, x_max);
     }
 }
 
