@@ -112,3 +112,41 @@ def test_norm_grad_writes_onto_an_input(dtype, n, h):
             got = s.norm_grad(a, hh, w, rstd, dh=b, out=(a if onto == "dy" else b, torch.empty_like(dw)))
             assert torch.equal(got[0], dx) and torch.equal(got[1], dw)
             assert torch.equal(b if onto == "dy" else a, dh if onto == "dy" else dy)
+
+
+@pytest.mark.parametrize("n", [1, 700, 5000])
+def test_embed_grad_of_a_table_whose_absent_rows_are_not_kept(n):
+    """More than 2^22 rows, tokens few enough to look through: all zeros in the first launch."""
+    torch = torch_()
+    v, h = (1 << 22) + 77, 5
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n)
+    dout = torch.randn((n, h), device="cuda", generator=gen)
+    tok = torch.randint(-1, v + 1, (n,), device="cuda", generator=gen)
+    tok[::3] = v - 1
+    grad = torch.full((v, h), T.SENTINEL, device="cuda")
+    with ops(n, h, v) as s:
+        s.embed_grad(tok, dout, v, out=grad)
+    there = (tok >= 0) & (tok < v)
+    want = torch.zeros((v, h), device="cuda", dtype=torch.float64).index_add_(0, tok[there], dout[there].double())
+    size = torch.zeros((v, h), device="cuda", dtype=torch.float64).index_add_(0, tok[there], dout[there].double().abs())
+    assert bool(((grad.double() - want).abs() <= (n // 3 + 4) * E * size).all())
+
+
+@pytest.mark.parametrize("dtype, v", [("float16", 1000), ("bfloat16", (1 << 21) + 3)])
+def test_embed_grad_of_tokens_that_merge_three_times(dtype, v):
+    """More than 2^21 tokens."""
+    torch = torch_()
+    n, h = (1 << 21) + 70001, 9
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(v)
+    dout = torch.randn((n, h), device="cuda", generator=gen).to(dt(dtype))
+    tok = (torch.rand(n, device="cuda", generator=gen) ** 4 * (v + 1)).long() - 1
+    with ops(n, h, v) as s:
+        got = s.embed_grad(tok, dout, v, dtype=torch.float32)
+        assert torch.equal(got, s.embed_grad(tok.int(), dout, v, dtype=torch.float32))
+    there = tok >= 0
+    want = torch.zeros((v, h), device="cuda", dtype=torch.float64).index_add_(0, tok[there], dout[there].double())
+    size = torch.zeros((v, h), device="cuda", dtype=torch.float64).index_add_(0, tok[there], dout[there].double().abs())
+    count = torch.bincount(tok[there], minlength=v).double()[:, None]
+    assert bool(((got.double() - want).abs() <= (count + 2) * E * size).all())
