@@ -165,7 +165,8 @@ class StageOps:
     are returned unless ``out`` is given; autograd is not involved, gradients
     are calls of their own.  Work runs on ``stream`` (by default
     the current one when the object is made); called on another stream, an
-    operator waits for that stream first and that stream waits for it.
+    operator waits for that stream first and that stream waits for it.  Calls
+    that are captured into a graph need an object made with the capturing stream.
     """
 
     def __init__(self, max_tokens: int, max_hidden: int, max_vocab: int, device: int = 0, stream=None):
