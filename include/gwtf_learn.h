@@ -1,0 +1,177 @@
+/*
+ * gwtf_learn.h -- C ABI of the operators that close a training step, on AMD
+ * Instinct MI355X (gfx950), in the same library as gwtf_mcf.h and
+ * gwtf_stage.h.
+ *
+ * gwtf_stage.h takes a routed microbatch from its tokens to the gradients;
+ * these calls are what a step has before and after that (paper Sec. II and
+ * V-E: forward, backward and update phases; the data node holds the first and
+ * the last stage):
+ *
+ *   gwtf_learn_sample      data node, last stage: answers drawn from the
+ *                          logits with temperature, top k, top p and min p and
+ *                          given random numbers, for gwtf_stage_logprob to
+ *                          score and gwtf_stage_logprob_grad to learn from
+ *   gwtf_learn_grad_norm   every node, before its update: the norm of all of
+ *                          its gradients and the factor that clips them
+ *   gwtf_learn_adamw       every node, update phase: an AdamW step over all
+ *                          of its parameters, states in 32 bits or in 8
+ *
+ * Element types are GWTF_TYPE_* of gwtf_stage.h.  As there: pointers are
+ * DEVICE pointers on the handle's GPU, owned by the caller (lists of tensors
+ * are HOST arrays, read before the call returns); work is enqueued on the
+ * handle's HIP stream and calls return after enqueueing; argument errors give
+ * GWTF_ERR_INVALID_ARG with nothing enqueued; a handle serves one stream and is
+ * not thread-safe.  No call allocates or synchronises, so all may be captured
+ * into a HIP graph (one graph, or eager calls, at a time: they share the
+ * handle's workspace).  Arrays need no more alignment than their element type.
+ * Outputs must not overlap inputs or each other, except where a call says so.
+ * Results are deterministic: the same inputs give the same bits on every call.
+ */
+#ifndef GWTF_LEARN_H
+#define GWTF_LEARN_H
+
+#include "gwtf_stage.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef struct gwtf_learn gwtf_learn_t; /* opaque; owns its device workspace */
+
+/* Types of given random numbers. */
+enum {
+    GWTF_UNIFORM_F32 = 0,
+    GWTF_UNIFORM_F64 = 1
+};
+
+/* Forms of the states of gwtf_learn_adamw. */
+enum {
+    GWTF_STATE_F32 = 0, /* m and v in 32 bits */
+    GWTF_STATE_F8 = 1   /* m in OCP e4m3, v in OCP e5m2, a scale for each GWTF_STATE_BLOCK values */
+};
+
+#define GWTF_STATE_BLOCK 128
+
+/* Creates a handle on `device` that enqueues on `hip_stream` (a hipStream_t;
+ * NULL = the device's null stream) and allocates its workspace, 0.5 MB.  *out
+ * receives the handle, or NULL on failure. */
+gwtf_status_t gwtf_learn_create(int32_t device, void *hip_stream, gwtf_learn_t **out);
+
+/* Frees the handle and its workspace after draining its stream; NULL-safe. */
+void gwtf_learn_destroy(gwtf_learn_t *h);
+
+/* Text of the last error on this handle ("" if none); a NULL handle gives the
+ * last error of a gwtf_learn_create, or of a call with a NULL handle, on the
+ * calling thread. */
+const char *gwtf_learn_last_error(const gwtf_learn_t *h);
+
+/* ---- Answers drawn from logits ----
+ *
+ * Per row of logits x, with temperature T, top_k k, top_p p, min_p q and the
+ * row's random number u: w_j = exp((x_j - max x) / T), and the tokens in the
+ * order of descending x, equal ones by ascending index.  A token stays
+ * that is
+ *   among the first K, K = min(k, number of x above -infinity); k <= 0: no bound,
+ *   among the first n, the least n whose sum of w is p times that of the first
+ *     K or more; p >= 1: no bound,
+ *   and has w >= q.
+ * The first token always stays; T = 0 leaves it alone.  Of those that stay,
+ * by ascending index, the token drawn is the first whose sum of w, its own
+ * and of those before it, is above u times that of all:
+ *   ids = its index, logp = ln of its share of the sum, kept = how many stay.
+ * Sums, w and their products with u and p are held in 64 bits, so that a draw is
+ * that of exact arithmetic unless u or p falls within some 1e-13 of a border.  u counts as within [0, 1)
+ * (a NaN as 0).  An entry of -infinity is masked; a row of nothing else gives
+ * ids -1, logp -infinity, kept 0.  A row with a NaN or +infinity, and one
+ * whose settings are out of range (below), gives ids -1, logp NaN, kept 0.
+ *
+ * A setting is the same number for all rows, which the call refuses out of
+ * range, or one for each row. */
+typedef struct {
+    int64_t num_tokens, vocab;  /* N >= 0, 1 <= V < 2^31 */
+    int32_t type, uniform_type; /* GWTF_TYPE_* of logits, GWTF_UNIFORM_* of u */
+    int32_t top_k;
+    double temperature;         /* finite, >= 0 */
+    double top_p;               /* >= 0 */
+    double min_p;               /* within [0, 1] */
+    const float *temperatures;  /* [N], or NULL = temperature */
+    const int32_t *top_ks;      /* [N], or NULL = top_k */
+    const float *top_ps;        /* [N], or NULL = top_p */
+    const float *min_ps;        /* [N], or NULL = min_p */
+    const void *logits;         /* [N][V], rows any distance apart */
+    int64_t logits_stride;
+    const void *u;              /* [N] */
+    int32_t *ids;               /* [N] */
+    float *logp;                /* [N] or NULL */
+    int32_t *kept;              /* [N] or NULL */
+} gwtf_learn_sample_t;
+gwtf_status_t gwtf_learn_sample(gwtf_learn_t *h, const gwtf_learn_sample_t *a);
+
+/* ---- Parameters ----
+ *
+ * A tensor of a node's parameters: `size` adjacent values.  A call reads the
+ * members that it names. */
+typedef struct {
+    int64_t size;               /* 0 <= size < 2^35 */
+    int32_t type, grad_type;    /* GWTF_TYPE_* of param; of grad: that type or GWTF_TYPE_F32 */
+    const void *grad;           /* [size] */
+    void *param;                /* [size] */
+    float *master;              /* [size], the parameters in 32 bits, or NULL */
+    void *m, *v;                /* [size], in the form of the call */
+    float *m_scale, *v_scale;   /* [ceil(size / GWTF_STATE_BLOCK)]; with GWTF_STATE_F8 only */
+    float weight_decay;         /* finite */
+    uint32_t site;              /* number of the tensor; with GWTF_STATE_F8 only */
+} gwtf_learn_tensor_t;
+
+/* norm = scale * sqrt(sum of the squares of all gradients) and
+ * factor = scale * min(1, max_norm / norm), NaN where norm is not a finite
+ * number: what the gradients are to be multiplied with, for gwtf_learn_adamw.
+ * Sums are held in 64 bits.  Of the tensors, size, grad_type and grad count. */
+typedef struct {
+    int64_t num_tensors;                /* >= 0 */
+    const gwtf_learn_tensor_t *tensors; /* HOST array [num_tensors] */
+    double max_norm;                    /* >= 0; +infinity: no bound */
+    double scale;                       /* finite, >= 0 */
+    float *norm;                        /* [1], or NULL */
+    float *factor;                      /* [1], or NULL */
+} gwtf_learn_grad_norm_t;
+gwtf_status_t gwtf_learn_grad_norm(gwtf_learn_t *h, const gwtf_learn_grad_norm_t *a);
+
+/* One step of AdamW on every tensor, in place, in 32 bits:
+ *   g = factor * grad
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   p = p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay p)
+ * where p is master, rounded to param too, or param itself where master is
+ * NULL.  With a factor that is not a finite number nothing is written.
+ *
+ * GWTF_STATE_F8: m and v are values times the scale of their block, a power of
+ * two that puts the block's largest magnitude into (224, 448] of m, (28672, 57344]
+ * of v (2^-126 at least).  The step takes the new m and v as they are;
+ * what is kept of them is one of the two 8-bit values around, the upper one with
+ * the probability of the remainder, so that an average which moves by less
+ * than half a step of 8 bits moves at all: with r = 16 bits of Philox4x32-10
+ * under the key (low, high half of `seed`) and the counter (i / 8, site, low, high
+ * half of step), word (i % 8) / 2, its low half for even i, for value i of a
+ * tensor, the magnitude in steps of 8 bits plus (r + 0.5) 2^-16 is cut down to a
+ * whole number.  A v above 0 is kept above 0, so that m / sqrt(v) stays bounded.
+ * A NaN or infinity among a block's new values makes its scale NaN. */
+typedef struct {
+    int64_t num_tensors;                /* >= 0 */
+    const gwtf_learn_tensor_t *tensors; /* HOST array [num_tensors] */
+    int32_t form;                       /* GWTF_STATE_* of all m and v */
+    int64_t step;                       /* >= 1, number of this step */
+    const int64_t *step_at;             /* DEVICE [1] to be read in its place, or NULL */
+    double lr;                          /* finite */
+    const float *lr_at;                 /* DEVICE [1] to be read in its place, or NULL */
+    double beta1, beta2;                /* within [0, 1) */
+    double eps;                         /* finite, >= 0 */
+    uint64_t seed;                      /* with GWTF_STATE_F8 only */
+    const float *factor;                /* DEVICE [1], or NULL = 1 */
+} gwtf_learn_adamw_t;
+gwtf_status_t gwtf_learn_adamw(gwtf_learn_t *h, const gwtf_learn_adamw_t *a);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* GWTF_LEARN_H */

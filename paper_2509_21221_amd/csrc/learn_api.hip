@@ -1,0 +1,171 @@
+// Host side of the C ABI declared in include/gwtf_learn.h: argument checks and
+// the handle's workspace.
+#include "api_checks.h"
+#include "learn_internal.h"
+
+#include <cmath>
+#include <cstdio>
+#include <new>
+
+using namespace gwtf;
+
+struct gwtf_learn {
+    int32_t device;
+    hipStream_t stream;
+    LearnWorkspace ws;
+    char err[256];
+};
+
+namespace {
+
+thread_local char g_learn_err[256];
+
+gwtf_status_t fail(gwtf_learn_t *h, gwtf_status_t code, const char *what, hipError_t e = hipSuccess)
+{
+    char *to = h ? h->err : g_learn_err;
+    if (e != hipSuccess) (void)hipGetLastError(); // it is reported here, not to the thread's next reader
+    if (e != hipSuccess) snprintf(to, sizeof g_learn_err, "%s: %s", what, hipGetErrorString(e));
+    else snprintf(to, sizeof g_learn_err, "%s", what);
+    return code;
+}
+gwtf_status_t fail_at(gwtf_learn_t *h, int64_t tensor, const char *what)
+{
+    snprintf(h->err, sizeof h->err, "tensor %lld: %s", static_cast<long long>(tensor), what);
+    return GWTF_ERR_INVALID_ARG;
+}
+
+#define LEARN_BEGIN(name)                                                               \
+    if (!h) return fail(nullptr, GWTF_ERR_INVALID_ARG, name ": handle is NULL");        \
+    if (!a) return fail(h, GWTF_ERR_INVALID_ARG, name ": arguments are NULL");
+#define LEARN_REQUIRE(cond, text) \
+    if (!(cond)) return fail(h, GWTF_ERR_INVALID_ARG, text);
+#define LEARN_CHECK(expr) \
+    if (const char *bad = (expr)) return fail(h, GWTF_ERR_INVALID_ARG, bad);
+#define LEARN_CHECK_AT(i, expr) \
+    if (const char *bad = (expr)) return fail_at(h, i, bad);
+#define LEARN_LAUNCH(name, expr)                                                        \
+    DeviceScope scope(h->device);                                                       \
+    if (scope.e != hipSuccess) return fail(h, GWTF_ERR_DEVICE, "hipSetDevice", scope.e); \
+    const hipError_t e = (expr);                                                        \
+    return e == hipSuccess ? GWTF_OK : fail(h, GWTF_ERR_DEVICE, name " launch", e);
+
+constexpr int64_t kTensorSize = int64_t(1) << 35;
+
+// What every call asks of a tensor: its size, type and gradient.
+const char *bad_grad(const gwtf_learn_tensor_t &t)
+{
+    if (t.size < 0 || t.size >= kTensorSize) return "size outside [0, 2^35)";
+    if (!type_ok(t.grad_type)) return "unknown type of grad";
+    return bad_vector(t.grad, t.size, size_of(t.grad_type));
+}
+
+} // namespace
+
+extern "C" gwtf_status_t gwtf_learn_create(int32_t device, void *hip_stream, gwtf_learn_t **out)
+{
+    if (!out) return fail(nullptr, GWTF_ERR_INVALID_ARG, "out is NULL");
+    *out = nullptr;
+    if (device < 0) return fail(nullptr, GWTF_ERR_INVALID_ARG, "bad device ordinal");
+    int ndev = 0;
+    hipError_t e = hipGetDeviceCount(&ndev);
+    if (e != hipSuccess) return fail(nullptr, GWTF_ERR_DEVICE, "hipGetDeviceCount", e);
+    if (device >= ndev) return fail(nullptr, GWTF_ERR_INVALID_ARG, "bad device ordinal");
+    DeviceScope scope(device);
+    if (scope.e != hipSuccess) return fail(nullptr, GWTF_ERR_DEVICE, "hipSetDevice", scope.e);
+    gwtf_learn_t *h = new (std::nothrow) gwtf_learn_t();
+    if (!h) return fail(nullptr, GWTF_ERR_OUT_OF_MEMORY, "host allocation failed");
+    h->device = device;
+    h->stream = static_cast<hipStream_t>(hip_stream);
+    if ((e = hipDeviceGetAttribute(&h->ws.cus, hipDeviceAttributeMultiprocessorCount, device)) != hipSuccess) {
+        delete h;
+        return fail(nullptr, GWTF_ERR_DEVICE, "hipDeviceGetAttribute", e);
+    }
+    void *partial = nullptr;
+    if ((e = hipMalloc(&partial, sizeof(double) * kNormSlots)) != hipSuccess) {
+        delete h;
+        return fail(nullptr, GWTF_ERR_OUT_OF_MEMORY, "hipMalloc workspace", e);
+    }
+    h->ws.partial = static_cast<double *>(partial);
+    *out = h;
+    return GWTF_OK;
+}
+
+extern "C" void gwtf_learn_destroy(gwtf_learn_t *h)
+{
+    if (!h) return;
+    DeviceScope scope(h->device);
+    if (scope.e == hipSuccess) (void)hipStreamSynchronize(h->stream);
+    (void)hipFree(h->ws.partial);
+    delete h;
+}
+
+extern "C" const char *gwtf_learn_last_error(const gwtf_learn_t *h) { return h ? h->err : g_learn_err; }
+
+extern "C" gwtf_status_t gwtf_learn_sample(gwtf_learn_t *h, const gwtf_learn_sample_t *a)
+{
+    LEARN_BEGIN("gwtf_learn_sample")
+    const int64_t N = a->num_tokens, V = a->vocab, top = (int64_t(1) << 31) - 1;
+    LEARN_REQUIRE(N >= 0 && N <= top, "num_tokens outside [0, 2^31)")
+    LEARN_REQUIRE(V >= 1 && V <= top, "vocab outside [1, 2^31)")
+    LEARN_REQUIRE(type_ok(a->type), "unknown type")
+    LEARN_REQUIRE(a->uniform_type == GWTF_UNIFORM_F32 || a->uniform_type == GWTF_UNIFORM_F64, "unknown type of u")
+    LEARN_REQUIRE(a->temperatures || (a->temperature >= 0 && std::isfinite(a->temperature)), "temperature must be finite and >= 0")
+    LEARN_REQUIRE(a->top_ps || a->top_p >= 0, "top_p must be >= 0")
+    LEARN_REQUIRE(a->min_ps || (a->min_p >= 0 && a->min_p <= 1), "min_p outside [0, 1]")
+    if (N == 0) return GWTF_OK;
+    LEARN_CHECK(bad_matrix(a->logits, a->logits_stride, N, V, size_of(a->type)))
+    LEARN_CHECK(bad_vector(a->u, N, a->uniform_type == GWTF_UNIFORM_F64 ? 8 : 4))
+    LEARN_CHECK(a->temperatures ? bad_vector(a->temperatures, N, 4) : nullptr)
+    LEARN_CHECK(a->top_ks ? bad_vector(a->top_ks, N, 4) : nullptr)
+    LEARN_CHECK(a->top_ps ? bad_vector(a->top_ps, N, 4) : nullptr)
+    LEARN_CHECK(a->min_ps ? bad_vector(a->min_ps, N, 4) : nullptr)
+    LEARN_CHECK(bad_vector(a->ids, N, 4))
+    LEARN_CHECK(a->logp ? bad_vector(a->logp, N, 4) : nullptr)
+    LEARN_CHECK(a->kept ? bad_vector(a->kept, N, 4) : nullptr)
+    LEARN_LAUNCH("gwtf_learn_sample", launch_sample(*a, h->stream))
+}
+
+extern "C" gwtf_status_t gwtf_learn_grad_norm(gwtf_learn_t *h, const gwtf_learn_grad_norm_t *a)
+{
+    LEARN_BEGIN("gwtf_learn_grad_norm")
+    LEARN_REQUIRE(a->num_tensors >= 0, "num_tensors below 0")
+    LEARN_REQUIRE(a->num_tensors == 0 || a->tensors, "tensors is NULL")
+    LEARN_REQUIRE(a->max_norm >= 0, "max_norm must be >= 0")
+    LEARN_REQUIRE(a->scale >= 0 && std::isfinite(a->scale), "scale must be finite and >= 0")
+    LEARN_CHECK(a->norm ? bad_vector(a->norm, 1, 4) : nullptr)
+    LEARN_CHECK(a->factor ? bad_vector(a->factor, 1, 4) : nullptr)
+    for (int64_t i = 0; i < a->num_tensors; ++i) LEARN_CHECK_AT(i, bad_grad(a->tensors[i]))
+    if (!a->norm && !a->factor) return GWTF_OK;
+    LEARN_LAUNCH("gwtf_learn_grad_norm", launch_grad_norm(*a, h->ws, h->stream))
+}
+
+extern "C" gwtf_status_t gwtf_learn_adamw(gwtf_learn_t *h, const gwtf_learn_adamw_t *a)
+{
+    LEARN_BEGIN("gwtf_learn_adamw")
+    LEARN_REQUIRE(a->num_tensors >= 0, "num_tensors below 0")
+    LEARN_REQUIRE(a->num_tensors == 0 || a->tensors, "tensors is NULL")
+    LEARN_REQUIRE(a->form == GWTF_STATE_F32 || a->form == GWTF_STATE_F8, "unknown form of the states")
+    LEARN_REQUIRE(a->step_at || a->step >= 1, "step below 1")
+    LEARN_REQUIRE(a->lr_at || std::isfinite(a->lr), "lr must be finite")
+    LEARN_REQUIRE(a->beta1 >= 0 && a->beta1 < 1 && a->beta2 >= 0 && a->beta2 < 1, "beta1 or beta2 outside [0, 1)")
+    LEARN_REQUIRE(a->eps >= 0 && std::isfinite(a->eps), "eps must be finite and >= 0")
+    LEARN_CHECK(a->step_at ? bad_vector(a->step_at, 1, 8) : nullptr)
+    LEARN_CHECK(a->lr_at ? bad_vector(a->lr_at, 1, 4) : nullptr)
+    LEARN_CHECK(a->factor ? bad_vector(a->factor, 1, 4) : nullptr)
+    const bool f8 = a->form == GWTF_STATE_F8;
+    for (int64_t i = 0; i < a->num_tensors; ++i) {
+        const gwtf_learn_tensor_t &t = a->tensors[i];
+        LEARN_CHECK_AT(i, bad_grad(t))
+        LEARN_CHECK_AT(i, type_ok(t.type) ? nullptr : "unknown type")
+        LEARN_CHECK_AT(i, t.grad_type == t.type || t.grad_type == GWTF_TYPE_F32 ? nullptr : "grad_type must be type or GWTF_TYPE_F32")
+        LEARN_CHECK_AT(i, std::isfinite(t.weight_decay) ? nullptr : "weight_decay must be finite")
+        LEARN_CHECK_AT(i, bad_vector(t.param, t.size, size_of(t.type)))
+        LEARN_CHECK_AT(i, t.master ? bad_vector(t.master, t.size, 4) : nullptr)
+        LEARN_CHECK_AT(i, bad_vector(t.m, t.size, f8 ? 1 : 4))
+        LEARN_CHECK_AT(i, bad_vector(t.v, t.size, f8 ? 1 : 4))
+        LEARN_CHECK_AT(i, f8 ? bad_vector(t.m_scale, t.size, 4) : nullptr)
+        LEARN_CHECK_AT(i, f8 ? bad_vector(t.v_scale, t.size, 4) : nullptr)
+    }
+    if (a->num_tensors == 0) return GWTF_OK;
+    LEARN_LAUNCH("gwtf_learn_adamw", launch_adamw(*a, h->stream))
+}

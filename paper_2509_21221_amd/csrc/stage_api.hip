@@ -1,5 +1,6 @@
 // Host side of the C ABI declared in include/gwtf_stage.h: argument checks and
 // the handle's workspace.
+#include "api_checks.h"
 #include "stage_internal.h"
 
 #include <cmath>
@@ -28,36 +29,8 @@ gwtf_status_t fail(gwtf_stage_t *h, gwtf_status_t code, const char *what, hipErr
     return code;
 }
 
-// Makes `device` current for a call; the caller's device comes back after it.
-struct DeviceScope {
-    int before = -1, device;
-    hipError_t e;
-    explicit DeviceScope(int d) : device(d)
-    {
-        e = hipGetDevice(&before);
-        if (e == hipSuccess && before != d) e = hipSetDevice(d);
-    }
-    ~DeviceScope()
-    {
-        if (before >= 0 && before != device) (void)hipSetDevice(before);
-    }
-};
-
-size_t size_of(int32_t type) { return type == GWTF_TYPE_F32 ? 4 : 2; }
-bool type_ok(int32_t t) { return t == GWTF_TYPE_F32 || t == GWTF_TYPE_F16 || t == GWTF_TYPE_BF16; }
 bool token_ok(int32_t t) { return t == GWTF_TOKEN_I32 || t == GWTF_TOKEN_I64; }
 size_t token_size(int32_t t) { return t == GWTF_TOKEN_I64 ? 8 : 4; }
-
-// A matrix or vector of elements of `size` bytes, `rows` rows of `width`.
-const char *bad_matrix(const void *p, int64_t stride, int64_t rows, int64_t width, size_t size)
-{
-    if (rows == 0) return nullptr;
-    if (!p) return "a required array is NULL";
-    if (reinterpret_cast<uintptr_t>(p) % size) return "an array is not aligned to its element type";
-    if (rows > 1 && (stride < width || stride > (int64_t(1) << 40))) return "a row stride is below the width or above 2^40";
-    return nullptr;
-}
-const char *bad_vector(const void *p, int64_t n, size_t size) { return bad_matrix(p, n, n ? 1 : 0, n, size); }
 
 #define STAGE_BEGIN(name)                                                               \
     if (!h) return fail(nullptr, GWTF_ERR_INVALID_ARG, name ": handle is NULL");        \

@@ -1,0 +1,603 @@
+"""GPU tests of include/gwtf_learn.h against the 64-bit implementations of oracle/learn.py."""
+import itertools
+import math
+
+import numpy as np
+import pytest
+
+from oracle import learn as O
+from tests.gpu_util import have_gpu
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not have_gpu(), reason="no GPU")]
+
+if have_gpu():
+    import torch
+
+    from paper_2509_21221_amd.learn import LearnOps
+    from paper_2509_21221_amd.mcf import GwtfError
+
+    DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+HALF = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}  # a rounding is off by at most this, relatively
+
+
+@pytest.fixture(scope="module")
+def ops():
+    with LearnOps() as o:
+        yield o
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+# ---- sample ----
+
+def logits(n, v, dtype, seed, pad=0, offset=0, std=2.5):
+    """n x v logits of which every second row is nearly sure of a token, in rows `v + pad` apart."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    flat = torch.randn(n * (v + pad) + offset, device="cuda", generator=gen) * std
+    x = flat.to(DT[dtype])[offset:].view(n, v + pad)[:, :v]
+    for i in range(1, n, 2):
+        x[i, (i * 7919) % v] += 12
+    return x
+
+
+def check_rows(ops, x, u, **kw):
+    """ids and kept are the oracle's; logp is rounded once from 64 bits."""
+    ids, logp, kept = ops.sample(x, u, **{k: dev(v) if isinstance(v, np.ndarray) else v for k, v in kw.items()})
+    host, us = x.double().cpu().numpy(), u.double().cpu().numpy()
+    for i in range(len(host)):
+        one = {k: v[i].item() if isinstance(v, np.ndarray) else v for k, v in kw.items()}
+        want = O.sample_row(host[i], us[i], **one)
+        got = ids[i].item(), logp[i].item(), kept[i].item()
+        what = (i, one, us[i], got, want)
+        assert got[0] == want[0] and got[2] == want[2], what
+        if math.isnan(want[1]) or math.isinf(want[1]):
+            assert got[1] == want[1] or (math.isnan(got[1]) and math.isnan(want[1])), what
+        else:
+            # sums, weights and the logarithm in 64 bits (1e-12 covers them amply), then one rounding
+            assert abs(got[1] - want[1]) <= HALF["f32"] * abs(want[1]) + 1e-12, what
+    return ids, logp, kept
+
+
+def uniform(n, seed, dtype=None):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return torch.rand(n, device="cuda", generator=gen, dtype=dtype or torch.float64)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("v", [1, 2, 7, 8, 63, 511, 512, 513, 2047, 2048, 2049, 4097, 8192, 8193, 16384, 16385, 32001, 65536, 65537, 131071, 131072, 131073])
+def test_sample_widths(ops, v, dtype):
+    x = logits(3, v, dtype, v)
+    for kw in (dict(), dict(top_k=20, top_p=0.9, min_p=0.05, temperature=0.8), dict(top_p=0.95), dict(top_k=1500)):
+        check_rows(ops, x, uniform(3, v), **kw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sample_wide(ops, dtype):
+    """More than 1,024 steps of 512 columns: segments of several."""
+    x = logits(2, 1_200_007, dtype, 3)
+    for kw in (dict(), dict(top_p=0.9), dict(top_k=50, min_p=0.1), dict(top_k=100_000)):
+        check_rows(ops, x, uniform(2, 5), **kw)
+
+
+@pytest.mark.parametrize("dtype,v", [("f32", 700), ("bf16", 700), ("f16", 33000), ("bf16", 33000)])
+@pytest.mark.parametrize("k,p,q,t", [(0, 1.0, 0.0, 0.0), (1, 0.5, 0.5, 1.0), (2, 1.0, 0.0, 0.25), (50, 1.0, 0.0, 4.0), (0, 0.0, 0.0, 1.0),
+                                     (0, 0.3, 0.0, 1.0), (0, 0.999999, 0.0, 1.0), (0, 1.0, 1e-30, 1.0), (0, 1.0, 1.0, 1.0), (0, 1.0, 0.2, 0.5),
+                                     (699, 0.7, 0.0, 1.0), (10 ** 6, 0.99, 0.01, 2.0), (0, 0.5, 0.0, 1e-30), (40, 0.9, 0.05, 1e30),
+                                     (0, 0.99999, 1e-9, 100.0), (1024, 1.0, 0.0, 1.0), (1025, 0.9, 0.0, 1.0), (0, 7.5, 0.0, 1.0)])
+def test_sample_settings(ops, dtype, v, k, p, q, t):
+    x = logits(6, v, dtype, v + k)
+    check_rows(ops, x, uniform(6, k), top_k=k, top_p=p, min_p=q, temperature=t)
+
+
+@pytest.mark.parametrize("u", [0.0, 1e-300, 0.5, 1 - 2.0 ** -53, 1.0, 7.0, -1.0, float("nan"), float("inf")])
+def test_sample_ends_of_u(ops, u):
+    x = logits(4, 9000, "bf16", 8)
+    x[2, 5:] = float("-inf")
+    us = torch.full((4,), u, dtype=torch.float64, device="cuda")
+    for kw in (dict(), dict(top_k=7), dict(top_p=0.8), dict(temperature=0.05)):
+        check_rows(ops, x, us, **kw)
+    check_rows(ops, x, us.float(), top_k=7)
+
+
+def test_sample_float_random_numbers(ops):
+    x = logits(64, 1000, "f32", 9)
+    check_rows(ops, x, uniform(64, 9, torch.float32), temperature=1.5)
+
+
+def test_sample_settings_by_row(ops):
+    n, v = 40, 5000
+    x = logits(n, v, "bf16", 10)
+    rng = np.random.default_rng(10)
+    kw = dict(temperature=rng.choice([0.0, 0.5, 1.0, 3.0, -1.0, np.nan, np.inf], n).astype(np.float32),
+              top_k=rng.choice([-3, 0, 1, 40, 3000, 2 ** 31 - 1], n).astype(np.int32),
+              top_p=rng.choice([0.0, 0.25, 0.9, 1.0, 2.0, -0.5, np.nan], n).astype(np.float32),
+              min_p=rng.choice([0.0, 0.1, 1.0, 1.5, np.nan], n, p=[0.5, 0.2, 0.1, 0.1, 0.1]).astype(np.float32))
+    ids = check_rows(ops, x, uniform(n, 10), **kw)[0]
+    assert (ids == -1).any() and (ids >= 0).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("v", [300, 20000])
+def test_sample_special_rows(ops, dtype, v):
+    inf, nan, top = float("inf"), float("nan"), torch.finfo(DT[dtype]).max
+    x = logits(16, v, dtype, 11)
+    x[0] = -inf
+    x[1] = 0.0                                  # all equal
+    x[2] = -inf
+    x[2, v - 1] = -3.0                          # one token alone
+    x[3, v // 2] = nan
+    x[4, 0] = inf
+    x[5] = torch.where(torch.arange(v, device="cuda") % 2 == 0, -0.0, 0.0)  # zeros of both signs are equal
+    x[6] = -top                                 # masks of the lowest value, three tokens
+    x[6, 5], x[6, 6], x[6, v - 2] = 1.0, 2.0, 1.5
+    x[7] = top
+    x[7, ::2] = -top
+    x[8] = torch.where(torch.arange(v, device="cuda") % 3 == 0, 1.0, 2.0)   # two values
+    x[9] = -top                                 # masks alone
+    x[10] = x[10] * 1e-4
+    x[11] = torch.finfo(DT[dtype]).smallest_normal / 4  # below the normal numbers
+    x[12, : v - 3] = -inf
+    x[13] = 100.0 + x[13]
+    x[14, 7] = -nan if dtype == "f32" else nan
+    x[14, 8:] = -inf
+    x[15] = -inf
+    x[15, 3] = nan
+    for kw in (dict(), dict(top_k=5), dict(top_p=0.5), dict(top_p=0.25, top_k=v // 2), dict(min_p=0.5), dict(min_p=1.0, top_p=0.5),
+               dict(temperature=1e-3), dict(temperature=1e30, top_p=0.75)):
+        for seed in range(2):
+            check_rows(ops, x, uniform(16, seed), **kw)
+
+
+def test_sample_rows_of_a_wider_buffer(ops):
+    for dtype, pad, offset in itertools.product(("f32", "f16", "bf16"), (0, 1, 13), (0, 1, 3)):
+        x = logits(5, 1999, dtype, 12, pad, offset)
+        check_rows(ops, x, uniform(5, 12), top_k=100, top_p=0.9)
+        check_rows(ops, x, uniform(5, 13))
+    x = logits(2, 40001, "bf16", 12, 5, 3)
+    check_rows(ops, x, uniform(2, 12), top_p=0.9)
+    one = torch.randn(1, 6, device="cuda")[:, ::2]
+    with pytest.raises(ValueError, match="adjacent"):
+        ops.sample(one, uniform(1, 0))
+
+
+def test_sample_frequencies(ops):
+    """100,000 draws of one row: each token's share within six deviations of its probability."""
+    n, x = 100_000, torch.tensor([[0.0, 1.0, 2.0, 1.0, -1.0, 3.0]], device="cuda")
+    ids, logp, kept = ops.sample(x.expand(n, 6).contiguous(), uniform(n, 14), temperature=1.3, top_k=5)
+    w = np.exp(x[0].cpu().double().numpy() / 1.3)
+    w[4] = 0
+    p = w / w.sum()
+    got = torch.bincount(ids.long(), minlength=6).cpu().numpy() / n
+    assert (np.abs(got - p) <= 6 * np.sqrt(p * (1 - p) / n)).all() and (kept == 5).all()
+    assert np.abs(logp.cpu().numpy() - np.log(p[ids.cpu().numpy()])).max() < 1e-6
+    assert x.expand(n, 6).stride(0) == 0
+    with pytest.raises(GwtfError, match="stride"):
+        ops.sample(x.expand(n, 6), uniform(n, 14))
+
+
+def test_sample_none_and_out(ops):
+    ids, logp, kept = ops.sample(torch.empty(0, 50, device="cuda"), torch.empty(0, device="cuda"))
+    assert ids.shape == logp.shape == kept.shape == (0,)
+    x, u = logits(4, 700, "f32", 15), uniform(4, 15)
+    want = ops.sample(x, u, top_k=9)
+    out = tuple(torch.empty_like(t) for t in want)
+    assert ops.sample(x, u, top_k=9, out=out) is out and all(torch.equal(a, b) for a, b in zip(want, out))
+    ids = torch.empty_like(want[0])
+    ops.sample(x, u, top_k=9, out=(ids, None, None))
+    assert torch.equal(ids, want[0])
+
+
+def test_sample_refusals(ops):
+    x, u = logits(4, 700, "f32", 16), uniform(4, 16)
+    for kw, match in ((dict(temperature=-0.5), "temperature"), (dict(temperature=float("nan")), "temperature"),
+                      (dict(temperature=float("inf")), "temperature"), (dict(top_p=-0.1), "top_p"), (dict(top_p=float("nan")), "top_p"),
+                      (dict(min_p=1.1), "min_p"), (dict(min_p=-1.0), "min_p"), (dict(top_k=-1), "top_k"), (dict(top_k=2 ** 31), "top_k"),
+                      (dict(temperature=torch.ones(3, device="cuda")), "temperature"), (dict(top_k=torch.ones(4, device="cuda")), "top_k"),
+                      (dict(out=(u, None, None)), "ids")):
+        with pytest.raises((ValueError, GwtfError), match=match):
+            ops.sample(x, u, **kw)
+    for bad in (u[:3], u.half(), u.cpu(), torch.rand(8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            ops.sample(x, bad)
+    for bad in (x[0], x.double(), x.cpu(), x.t()):
+        with pytest.raises(ValueError):
+            ops.sample(bad, u)
+    with pytest.raises(GwtfError, match="vocab"):
+        ops.sample(x[:, :0], u)
+
+
+# ---- norm ----
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("sizes,offset", [([1], 0), ([0, 5, 0], 1), ([2047, 2048, 2049, 1], 3), ([3] * 500, 0), ([100_003, 7, 4_000_001], 1), ([], 0)])
+def test_grad_norm(ops, sizes, offset, dtype):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(len(sizes))
+    flat = (torch.randn(sum(sizes) + offset, device="cuda", generator=gen) * 0.1).to(DT[dtype])[offset:]
+    grads = list(torch.split(flat, sizes)) if sizes else []
+    group = ops.parameters(None, grads)
+    for max_norm, scale in ((math.inf, 1.0), (1e-3, 1.0), (1e6, 0.125), (0.0, 1.0)):
+        norm, factor = ops.grad_norm(group, max_norm, scale)
+        want = O.grad_norm([g.double().cpu().numpy() for g in grads], max_norm, scale)
+        # sums in 64 bits, one rounding
+        for got, w in zip((norm, factor), want):
+            assert abs(got.item() - w) <= HALF["f32"] * abs(w) * (1 + 1e-6) + 1e-45, (got.item(), w)
+
+
+def test_grad_norm_of_mixed_types_and_ranges(ops):
+    grads = [torch.full((1000,), 1e30, device="cuda"), torch.full((9,), 2.0, device="cuda", dtype=torch.float16),
+             torch.full((1000,), 1e-30, device="cuda"), torch.full((77,), 3.0, device="cuda", dtype=torch.bfloat16)]
+    norm, factor = ops.grad_norm(ops.parameters(None, grads), 1.0)
+    assert abs(norm.item() / (1e30 * math.sqrt(1000)) - 1) < 2e-7 and abs(factor.item() * norm.item() - 1) < 2e-7
+    norm, _ = ops.grad_norm(ops.parameters(None, grads[2:3]), 1.0)
+    assert abs(norm.item() / (1e-30 * math.sqrt(1000)) - 1) < 2e-7
+    norm, _ = ops.grad_norm(ops.parameters(None, [grads[1], grads[3]]), 1.0)
+    assert abs(norm.item() - math.sqrt(9 * 4 + 77 * 9)) < 1e-5
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_grad_norm_not_finite(ops, bad):
+    g = torch.ones(5000, device="cuda")
+    g[4321] = bad
+    norm, factor = ops.grad_norm(ops.parameters(None, [torch.ones(3, device="cuda"), g]), 1.0)
+    assert not math.isfinite(norm.item()) and math.isnan(factor.item())
+
+
+def test_grad_norm_refusals(ops):
+    g = torch.ones(8, device="cuda")
+    group = ops.parameters(None, [g])
+    for kw, match in ((dict(max_norm=-1.0), "max_norm"), (dict(max_norm=math.nan), "max_norm"), (dict(scale=-1.0), "scale"),
+                      (dict(scale=math.inf), "scale"), (dict(out=(g, None)), "norm")):
+        with pytest.raises((ValueError, GwtfError), match=match):
+            ops.grad_norm(group, **kw)
+    for bad in ([g.double()], [g.cpu()], [g[::2]], [3.0]):
+        with pytest.raises((ValueError, TypeError)):
+            ops.parameters(None, bad)
+    with LearnOps() as other, pytest.raises(ValueError, match="Parameters"):
+        other.grad_norm(group)
+    with pytest.raises(ValueError, match="alone"):
+        ops.adamw(group, 1e-3, 1)
+
+
+# ---- AdamW ----
+
+SIZES = [1, 7, 128, 129, 0, 1000, 4096, 4097, 12345]
+
+
+def state(sizes, dtype, gtype, bits, master, seed, offset=0):
+    """Parameters, gradients and states in the middle of a run, as lists of tensors `offset` elements off their boundaries."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+
+    def new(std, dt):
+        out = []
+        for n in sizes:
+            out.append((torch.randn(n + offset, device="cuda", generator=gen) * std).to(dt)[offset:])
+        return out
+
+    s = dict(params=new(0.02, DT[dtype]), grads=new(1e-3, DT[gtype]))
+    m, v = new(3e-4, torch.float32), [t.square() for t in new(1e-3, torch.float32)]
+    s["master"] = [p.float() + 1e-6 for p in s["params"]] if master else None
+    s["scales"] = None
+    if bits == 8:
+        # as a former step leaves them: any 8-bit values, any powers of two
+        s["scales"] = tuple([torch.exp2(torch.randint(lo, lo + 4, (-(-n // 128),), device="cuda", generator=gen).float()) for n in sizes]
+                            for lo in (-21, -36))
+        spread = lambda t, z: z.repeat_interleave(128)[: t.numel()]  # noqa: E731
+        m = [(t / spread(t, z)).clamp(-448, 448).to(torch.float8_e4m3fn) for t, z in zip(m, s["scales"][0])]
+        v = [(t / spread(t, z)).clamp(0, 57344).to(torch.float8_e5m2) for t, z in zip(v, s["scales"][1])]
+    s["moments"] = (m, v)
+    return s
+
+
+def group_of(ops, s, **kw):
+    return ops.parameters(s["params"], s["grads"], moments=s["moments"], scales=s["scales"], master=s["master"], **kw)
+
+
+def wide(q, scale):
+    q = q.float()
+    return q if scale is None else q * scale.repeat_interleave(128)[: q.numel()]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype,gtype,master", [("f32", "f32", False), ("f16", "f16", False), ("bf16", "bf16", False), ("f16", "f32", True),
+                                                ("bf16", "f32", False), ("bf16", "bf16", True), ("f32", "f32", True)])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_adamw(ops, dtype, gtype, master, bits, offset):
+    lr, step, betas, eps, seed = 1e-2, 7, (0.9, 0.98), 1e-8, 0x1234567890ABCDEF
+    decay = [0.1 * (i % 3) for i in range(len(SIZES))]
+    s = state(SIZES, dtype, gtype, bits, master, 20, offset)
+    sites = [5 * i + 2 for i in range(len(SIZES))]
+    factor = torch.tensor([0.75], device="cuda")
+    group = group_of(ops, s, weight_decay=decay, sites=sites)
+    h = lambda t: t.double().cpu().numpy()  # noqa: E731
+    before = []
+    for i in range(len(SIZES)):
+        sc = (None, None) if bits == 32 else (s["scales"][0][i], s["scales"][1][i])
+        p = s["master"][i] if master else s["params"][i]
+        before.append((h(p), h(s["grads"][i]), h(wide(s["moments"][0][i], sc[0])), h(wide(s["moments"][1][i], sc[1]))))
+    ops.adamw(group, lr, step, betas, eps, factor=factor, seed=seed)
+    one = 2.0 ** -24
+    for i, (p0, g0, m0, v0) in enumerate(before):
+        if not len(p0):
+            continue
+        p, m, v = O.adamw(p0, g0, m0, v0, lr, step, betas, eps, decay[i], 0.75)
+        m32, v32 = O.moments32(g0, m0, v0, betas, 0.75)
+        if bits == 32:
+            assert np.array_equal(s["moments"][0][i].cpu().numpy(), m32) and np.array_equal(s["moments"][1][i].cpu().numpy(), v32)
+        else:
+            r = O.draws(len(p0), seed, sites[i], step)
+            for got, scale, x, kind in ((s["moments"][0][i], s["scales"][0][i], m32, "e4m3"), (s["moments"][1][i], s["scales"][1][i], v32, "e5m2")):
+                q, z = O.narrow(x, r, kind)
+                assert np.array_equal(scale.cpu().numpy(), z), (i, kind)
+                assert np.array_equal(h(got), q), (i, kind)
+        # the step in 32 bits: m is off by 4 roundings of its two terms (a beta, a factor, a product, the sum),
+        # v by 6; bias, root, eps and quotient add 9 (v's count half below the root); lr, the product and the sum with the
+        # decay's three add 6
+        den = np.sqrt(v / (1 - betas[1] ** step)) + eps
+        term = (np.abs(betas[0] * m0) + np.abs((1 - betas[0]) * 0.75 * g0)) / (1 - betas[0] ** step) / den
+        tol = lr * one * (4 * term + (9 + 3 + 6) * (np.abs(m / (1 - betas[0] ** step) / den) + decay[i] * np.abs(p0))) + 2 * one * np.abs(p)
+        if master:
+            got = h(s["master"][i])
+            assert (np.abs(got - p) <= tol).all(), i
+            assert np.array_equal(h(s["params"][i]), h(s["master"][i].to(DT[dtype])))
+        else:
+            low = 2.0 ** -25 if dtype == "f16" else 0.0  # half the smallest step of f16
+            assert (np.abs(h(s["params"][i]) - p) <= tol + HALF[dtype] * (np.abs(p) + tol) + low).all(), i
+
+
+def test_adamw_leaves_what_is_around(ops):
+    """Values before and behind a tensor, and scales behind its last block, stay."""
+    for bits in (32, 8):
+        n, kinds = 1000, (torch.float32,) * 2 if bits == 32 else (torch.float8_e4m3fn, torch.float8_e5m2)
+        full = [torch.full((n + 40,), 7.0, device="cuda").to(t) for t in (torch.bfloat16, *kinds)]
+        keep = [t.clone() for t in full]
+        p, m, v = (t[19:19 + n] for t in full)
+        scales = [torch.full((10,), 0.5, device="cuda") for _ in range(2)]
+        group = ops.parameters([p], [torch.ones(n, device="cuda")], moments=([m], [v]), scales=tuple([z[1:9]] for z in scales) if bits == 8 else None)
+        ops.adamw(group, 1e-2, 1, seed=3)
+        for i, (a, b) in enumerate(zip(full, keep)):
+            a, b = a.view(torch.uint8).view(n + 40, -1), b.view(torch.uint8).view(n + 40, -1)
+            assert torch.equal(a[:19], b[:19]) and torch.equal(a[19 + n:], b[19 + n:])
+            # the weights' step of less than 0.01 is below half a step of bf16 at 7 (2^-6) and leaves them; the states move
+            assert i == 0 or not torch.equal(a, b)
+        if bits == 8:
+            assert all(z[0] == 0.5 and z[9] == 0.5 and (z[1:9] != 0.5).all() for z in scales)
+
+
+def test_adamw_of_a_factor_that_is_not_finite_writes_nothing(ops):
+    for bits, bad in itertools.product((32, 8), (float("nan"), float("inf"))):
+        s = state([1000, 5], "bf16", "bf16", bits, True, 21)
+        group = group_of(ops, s)
+        before = [t.clone().view(torch.uint8) for t in group.tensors]
+        ops.adamw(group, 1e-2, 3, factor=torch.full((1,), bad, device="cuda"))
+        assert all(torch.equal(a.view(torch.uint8), b) for a, b in zip(group.tensors, before))
+
+
+def test_adamw_special_values_in_8_bits(ops):
+    n = 512
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    g[0], g[1], g[130], g[256] = 1.0, 1e-18, float("nan"), 1e-25
+    group = ops.parameters([p], [g], bits=8)
+    ops.adamw(group, 1e-3, 1, seed=1)
+    m, v, ms, vs = group.m[0].float(), group.v[0].float(), group.m_scales[0], group.v_scales[0]
+    assert m[0] * ms[0] == 0.1015625 or m[0] * ms[0] == 0.09375      # 0.1 is between these e4m3 values
+    assert v[1] == 2.0 ** -16 and (v[2:128] == 0).all()               # above 0 stays above 0
+    assert torch.isnan(ms[1]) and torch.isnan(vs[1]) and (group.m[0].view(torch.uint8)[128:256] == 0).all()
+    assert (m[257:] == 0).all() and vs[3] == 2.0 ** -126 and (v[257:] == 0).all()
+    # the step itself takes the values as they are: one of lr with the gradient's sign
+    assert abs(p[0].item() + 1e-3) < 1e-8 and abs(p[1].item() + 1e-3 / (1 + 1e-8 / 1e-18)) < 1e-10 and torch.isnan(p[130])
+
+
+def test_adamw_8_bits_follow_a_slow_average(ops):
+    """v of a constant gradient is 1 - beta2^t: it climbs by far less than a step of 8 bits at a time."""
+    n, steps = 4096, 400
+    p, g = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda")
+    group = ops.parameters([p], [g], bits=8)
+    for t in range(1, steps + 1):
+        ops.adamw(group, 0.0, t, betas=(0.9, 0.999), seed=9)
+    v = (group.v[0].float() * group.v_scales[0].repeat_interleave(128)).double()
+    want = 1 - 0.999 ** steps
+    # one rounding's variance is at most (step / 2)^2, e5m2's steps are at most v / 4: over 400 steps, with old ones
+    # fading, a deviation of at most sqrt(sum of change x step) per value; the mean over 4,096 values six of its own
+    dev_one = math.sqrt(sum(0.001 * (1 - 0.999 ** t) * 0.25 * (1 - 0.999 ** t) for t in range(1, steps + 1)) + steps * 0.001 * 0.25)
+    assert abs(v.mean().item() - want) <= 6 * dev_one / math.sqrt(n)
+
+
+def test_adamw_step_and_rate_on_the_device(ops):
+    for bits in (32, 8):
+        a, b = (state([3000, 70], "bf16", "f32", bits, True, 22) for _ in range(2))
+        ga, gb = group_of(ops, a, weight_decay=0.1), group_of(ops, b, weight_decay=0.1)
+        for t in (1, 2, 1000, 2 ** 33):
+            ops.adamw(ga, 3e-3, t, seed=5)
+            ops.adamw(gb, torch.tensor([3e-3], device="cuda"), torch.tensor([t], device="cuda"), seed=5)
+        for name in ("m", "v"):
+            assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(getattr(ga, name), getattr(gb, name)))
+        # 1 - beta^t from the host's and the device's functions may differ by a rounding
+        for x, y in zip(ga.master, gb.master):
+            assert ((x - y).abs() <= 4 * 4 * 2.0 ** -24 * (3e-3 * 30 + x.abs())).all()
+
+
+def test_adamw_of_many_tensors_is_that_of_each(ops):
+    """More tensors than a launch takes, of several types in one list."""
+    rng = np.random.default_rng(23)
+    sizes = [int(x) for x in rng.integers(0, 6000, 173)]
+    parts = [state([n], *[("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")][i // 9 % 4], 32, i % 5 == 0, i) for i, n in enumerate(sizes)]
+    again = [state([n], *[("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")][i // 9 % 4], 32, i % 5 == 0, i) for i, n in enumerate(sizes)]
+    for t in (1, 2):
+        for s in parts:
+            ops.adamw(group_of(ops, s, weight_decay=0.01), 1e-2, t)
+    none = [s for s in again if s["master"] is None]
+    some = [s for s in again if s["master"] is not None]
+    for one in (none, some):
+        group = ops.parameters([s["params"][0] for s in one], [s["grads"][0] for s in one],
+                               moments=([s["moments"][0][0] for s in one], [s["moments"][1][0] for s in one]),
+                               master=None if one is none else [s["master"][0] for s in one], weight_decay=0.01)
+        for t in (1, 2):
+            ops.adamw(group, 1e-2, t)
+    for a, b in zip(parts, again):
+        assert torch.equal(a["params"][0], b["params"][0]) and torch.equal(a["moments"][1][0], b["moments"][1][0])
+
+
+def test_adamw_refusals(ops):
+    s = state([64, 8], "bf16", "f32", 32, False, 24)
+    group = group_of(ops, s)
+    for kw, match in ((dict(step=0), "step"), (dict(lr=math.nan), "lr"), (dict(betas=(1.0, 0.9)), "beta"), (dict(betas=(0.9, -0.1)), "beta"),
+                      (dict(eps=-1.0), "eps"), (dict(eps=math.inf), "eps"), (dict(seed=-1), "seed"), (dict(seed=2 ** 64), "seed"),
+                      (dict(factor=0.5), "factor"), (dict(factor=torch.ones(2, device="cuda")), "factor"),
+                      (dict(step=torch.tensor([1], device="cuda", dtype=torch.int32)), "step"), (dict(lr=torch.tensor([1.0])), "lr")):
+        with pytest.raises((ValueError, TypeError, GwtfError), match=match):
+            ops.adamw(group, **{**dict(lr=1e-3, step=1), **kw})
+    p, g = s["params"], s["grads"]
+    m, v = s["moments"]
+    for args, match in ((dict(params=p, grads=g[:1]), "need 2"), (dict(params=p, grads=g, bits=16), "bits"),
+                        (dict(params=p, grads=[x.half() for x in g]), "grads"), (dict(params=p, grads=[g[0], g[1][:4]]), "values"),
+                        (dict(params=p, grads=g, moments=([x.half() for x in m], v)), "m"), (dict(params=p, grads=g, moments=(m, v), bits=8), "scales"),
+                        (dict(params=p, grads=g, master=p), "master"), (dict(params=p, grads=g, weight_decay=[0.1]), "weight_decay"),
+                        (dict(params=p, grads=g, sites=[0, -1]), "sites"), (dict(params=p, grads=g, moments=(m, m)), "shares memory"),
+                        (dict(params=[p[0], p[0][:8]], grads=g), "shares memory"), (dict(params=[g[0]], grads=[g[0]]), "shares memory"),
+                        (dict(params=[x.t() for x in (torch.ones(4, 8, device="cuda"),)], grads=g[:1]), "contiguous")):
+        with pytest.raises((ValueError, TypeError), match=match):
+            ops.parameters(**args)
+    bad = ops.parameters(p, g, weight_decay=math.inf)
+    with pytest.raises(GwtfError, match="tensor 0: weight_decay"):
+        ops.adamw(bad, 1e-3, 1)
+
+
+def test_closed(ops):
+    o = LearnOps()
+    group = o.parameters(None, [torch.ones(3, device="cuda")])
+    o.close()
+    with pytest.raises(RuntimeError, match="closed"):
+        o.grad_norm(group)
+
+
+# ---- together ----
+
+def test_a_step_from_answers_to_update():
+    """Drawn answers scored, their gradient taken through the norm and the factor into the update: as torch's arithmetic has it."""
+    from paper_2509_21221_amd.stage import StageOps
+
+    n, v, h = 48, 1500, 64
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(30)
+    x = torch.randn(n, h, device="cuda", generator=gen)
+    w = torch.randn(v, h, device="cuda", generator=gen) * 0.3
+    start = w.clone()
+    u = torch.rand(n, device="cuda", generator=gen, dtype=torch.float64)
+    reward = torch.randn(n, device="cuda", generator=gen)
+    grad = torch.empty_like(w)
+    with LearnOps() as learn, StageOps(n, h, v) as stage:
+        group = learn.parameters([w], [grad], weight_decay=0.01)
+        m, vv, p = np.zeros((v, h)), np.zeros((v, h)), start.double().cpu().numpy()
+        for t in (1, 2, 3):
+            logits_ = x @ w.t()
+            ids, drawn, _ = learn.sample(logits_, u)
+            logp, _, lse, _, _ = stage.logprob(logits_, ids)
+            assert ((logp - drawn).abs() <= 1e-5 * (1 + drawn.abs())).all()  # 32-bit sums of 1,500 terms and lse against 64-bit ones
+            d = stage.logprob_grad(logits_, ids, lse, dlogp=-reward / n)
+            torch.mm(d.t(), x, out=grad)
+            norm, factor = learn.grad_norm(group, max_norm=0.05)
+            g = grad.double().cpu().numpy()
+            want = O.grad_norm([g], 0.05)
+            assert abs(norm.item() - want[0]) <= 2e-7 * want[0] and abs(factor.item() - want[1]) <= 2e-7 * want[1]
+            learn.adamw(group, 1e-2, t, factor=factor)
+            p, m, vv = O.adamw(p, g, m, vv, 1e-2, t, (0.9, 0.999), 1e-8, 0.01, want[1])
+            big = np.abs(g) * want[1] > 1e-6  # where eps does not amplify what m and v are rounded by
+            assert np.abs(w.double().cpu().numpy() - p)[big].max() <= t * (1e-2 * 60 + 4) * 2.0 ** -24
+
+
+def test_captured_step_is_the_eager_one():
+    """Draw, norm and update replayed several times, with eager work between, against eager calls."""
+    side = torch.cuda.Stream()
+    x, u = logits(5, 40000, "bf16", 31), uniform(5, 31)
+    runs = {}
+    for how in ("eager", "graph"):
+        s = state([5000, 33], "bf16", "f32", 8, True, 32)
+        step, rate = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.full((1,), 1e-2, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side), LearnOps(stream=side) as o:
+            group = group_of(o, s)
+            out = o.sample(x, u, top_p=0.9)
+            norm = o.grad_norm(group, 0.1)
+
+            def one():
+                step.add_(1)
+                u.copy_(torch.frac(u + 0.37))
+                o.sample(x, u, top_p=0.9, out=out)
+                o.grad_norm(group, 0.1, out=norm)
+                o.adamw(group, rate, step, factor=norm[1], seed=77)
+
+            u0 = uniform(5, 31)
+            graph = None
+            if how == "graph":
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph, stream=side):
+                    one()
+            u.copy_(u0)
+            got = []
+            for k in range(4):
+                s["grads"][0].mul_(1.5)
+                rate.mul_(0.9)
+                graph.replay() if graph else one()
+                torch.cuda.synchronize()
+                got.append([t.clone() for t in (*out, *norm, *group.params, *group.master, *[t.view(torch.uint8) for t in (*group.m, *group.v)])])
+            runs[how] = got
+            del graph
+    for a, b in zip(runs["eager"], runs["graph"]):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+    assert len({tuple(r[0].tolist()) for r in runs["eager"]}) > 1
+
+
+def test_on_another_stream(ops):
+    """Called on another stream than its own, an operator waits for it and it for the operator."""
+    side = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device="cuda")
+    x0, u = logits(64, 20000, "f32", 33), uniform(64, 33)
+    want = ops.sample(x0, u, top_k=30)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(10):
+            big = big @ big * 1e-3
+        x = x0 + 0 * big[0, 0].nan_to_num(0.0, 0.0, 0.0)
+        got = ops.sample(x, u, top_k=30)
+        ids = got[0].clone()
+        g = torch.full((100_000,), 2.0, device="cuda")
+        norm, _ = ops.grad_norm(ops.parameters(None, [g]))
+        value = norm * 1
+    side.synchronize()
+    assert torch.equal(ids, want[0]) and abs(value.item() - 2 * math.sqrt(100_000)) < 1e-3
+
+
+def test_two_objects_at_once():
+    """Calls of two objects on two streams do not disturb each other."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    g = [torch.full((3_000_000,), float(k + 1), device="cuda") for k in range(2)]
+    torch.cuda.synchronize()
+    objects = [LearnOps(stream=s) for s in streams]
+    groups = [o.parameters(None, [t]) for o, t in zip(objects, g)]
+    found = [[], []]
+    for _ in range(20):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                found[k].append(objects[k].grad_norm(groups[k])[0])
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert {round(t.item(), 3) for t in found[k]} == {round(float(np.float32((k + 1) * math.sqrt(3_000_000))), 3)}
+        objects[k].close()
+
+
+def test_same_bits_again(ops):
+    x, u = logits(33, 50001, "f32", 34), uniform(33, 34)
+    first = ops.sample(x, u, top_p=0.95, temperature=0.9)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, ops.sample(x, u, top_p=0.95, temperature=0.9)))
+    group = ops.parameters(None, [torch.randn(1_000_003, device="cuda"), torch.randn(77, device="cuda")])
+    n0 = ops.grad_norm(group)[0]
+    assert all(torch.equal(n0, ops.grad_norm(group)[0]) for _ in range(3))
