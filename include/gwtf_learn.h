@@ -18,13 +18,12 @@
  *                          of its parameters, states in 32 bits or in 8
  *
  * Element types are GWTF_TYPE_* of gwtf_stage.h.  As there: pointers are
- * DEVICE pointers on the handle's GPU, owned by the caller (lists of tensors
- * are HOST arrays, read before the call returns); work is enqueued on the
- * handle's HIP stream and calls return after enqueueing; argument errors give
- * GWTF_ERR_INVALID_ARG with nothing enqueued; a handle serves one stream and is
- * not thread-safe.  No call allocates or synchronises, so all may be captured
- * into a HIP graph (one graph, or eager calls, at a time: they share the
- * handle's workspace).  Arrays need no more alignment than their element type.
+ * DEVICE pointers on the handle's GPU, owned by the caller; work is enqueued on
+ * the handle's HIP stream and calls return after enqueueing; argument errors
+ * give GWTF_ERR_INVALID_ARG with nothing enqueued; a handle serves one stream
+ * and is not thread-safe.  Of the calls only those that create or destroy
+ * allocate or synchronise, so the others may be captured into a HIP graph (one
+ * graph, or eager calls, at a time: they share the handle's workspace).  Arrays need no more alignment than their element type.
  * Outputs must not overlap inputs or each other, except where a call says so.
  * Results are deterministic: the same inputs give the same bits on every call.
  */
@@ -37,7 +36,8 @@
 extern "C" {
 #endif
 
-typedef struct gwtf_learn gwtf_learn_t; /* opaque; owns its device workspace */
+typedef struct gwtf_learn gwtf_learn_t;           /* opaque; owns its device workspace */
+typedef struct gwtf_learn_list gwtf_learn_list_t; /* opaque; a node's parameters, owns a table of them on the device */
 
 /* Types of given random numbers. */
 enum {
@@ -48,13 +48,14 @@ enum {
 /* Forms of the states of gwtf_learn_adamw. */
 enum {
     GWTF_STATE_F32 = 0, /* m and v in 32 bits */
-    GWTF_STATE_F8 = 1   /* m in OCP e4m3, v in OCP e5m2, a scale for each GWTF_STATE_BLOCK values */
+    GWTF_STATE_F8 = 1,  /* m in OCP e4m3, v in OCP e5m2, a scale for each GWTF_STATE_BLOCK values */
+    GWTF_STATE_NONE = 2 /* gradients alone, for gwtf_learn_grad_norm */
 };
 
 #define GWTF_STATE_BLOCK 128
 
 /* Creates a handle on `device` that enqueues on `hip_stream` (a hipStream_t;
- * NULL = the device's null stream) and allocates its workspace, 0.5 MB.  *out
+ * NULL = the device's null stream) and allocates its workspace, 50 KB.  *out
  * receives the handle, or NULL on failure. */
 gwtf_status_t gwtf_learn_create(int32_t device, void *hip_stream, gwtf_learn_t **out);
 
@@ -110,31 +111,40 @@ gwtf_status_t gwtf_learn_sample(gwtf_learn_t *h, const gwtf_learn_sample_t *a);
 
 /* ---- Parameters ----
  *
- * A tensor of a node's parameters: `size` adjacent values.  A call reads the
- * members that it names. */
+ * A tensor of a node's parameters: `size` adjacent values. */
 typedef struct {
     int64_t size;               /* 0 <= size < 2^35 */
     int32_t type, grad_type;    /* GWTF_TYPE_* of param; of grad: that type or GWTF_TYPE_F32 */
     const void *grad;           /* [size] */
     void *param;                /* [size] */
     float *master;              /* [size], the parameters in 32 bits, or NULL */
-    void *m, *v;                /* [size], in the form of the call */
+    void *m, *v;                /* [size], in the form of the list */
     float *m_scale, *v_scale;   /* [ceil(size / GWTF_STATE_BLOCK)]; with GWTF_STATE_F8 only */
     float weight_decay;         /* finite */
     uint32_t site;              /* number of the tensor; with GWTF_STATE_F8 only */
 } gwtf_learn_tensor_t;
 
+/* Makes a list of tensors, a HOST array, on the handle's GPU: a table of where
+ * they lie, 80 bytes a tensor and 4 for each 2048 of its values, which the calls that are given the list
+ * read.  All arrays have to stay where they are as long as the list is in use.  With
+ * GWTF_STATE_NONE of a tensor size, grad_type and grad count alone.  At
+ * most 2^42 values in all. */
+gwtf_status_t gwtf_learn_list_create(gwtf_learn_t *h, int64_t num_tensors, const gwtf_learn_tensor_t *tensors, int32_t form,
+                                     gwtf_learn_list_t **out);
+
+/* Frees the list, after the work of its device that may read it; NULL-safe. */
+void gwtf_learn_list_destroy(gwtf_learn_list_t *list);
+
 /* norm = scale * sqrt(sum of the squares of all gradients) and
  * factor = scale * min(1, max_norm / norm), NaN where norm is not a finite
  * number: what the gradients are to be multiplied with, for gwtf_learn_adamw.
- * Sums are held in 64 bits.  Of the tensors, size, grad_type and grad count. */
+ * Sums are held in 64 bits.  The list may have any form. */
 typedef struct {
-    int64_t num_tensors;                /* >= 0 */
-    const gwtf_learn_tensor_t *tensors; /* HOST array [num_tensors] */
-    double max_norm;                    /* >= 0; +infinity: no bound */
-    double scale;                       /* finite, >= 0 */
-    float *norm;                        /* [1], or NULL */
-    float *factor;                      /* [1], or NULL */
+    const gwtf_learn_list_t *list;
+    double max_norm; /* >= 0; +infinity: no bound */
+    double scale;    /* finite, >= 0 */
+    float *norm;     /* [1], or NULL */
+    float *factor;   /* [1], or NULL */
 } gwtf_learn_grad_norm_t;
 gwtf_status_t gwtf_learn_grad_norm(gwtf_learn_t *h, const gwtf_learn_grad_norm_t *a);
 
@@ -143,7 +153,9 @@ gwtf_status_t gwtf_learn_grad_norm(gwtf_learn_t *h, const gwtf_learn_grad_norm_t
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
  *   p = p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay p)
  * where p is master, rounded to param too, or param itself where master is
- * NULL.  With a factor that is not a finite number nothing is written.
+ * NULL, and a denominator below 2^-126 counts as 2^-126 (with eps 0, values whose
+ * gradients have all been 0 stay).  With a factor that is not a finite number
+ * nothing is written.
  *
  * GWTF_STATE_F8: m and v are values times the scale of their block, a power of
  * two that puts the block's largest magnitude into (224, 448] of m, (28672, 57344]
@@ -157,17 +169,15 @@ gwtf_status_t gwtf_learn_grad_norm(gwtf_learn_t *h, const gwtf_learn_grad_norm_t
  * whole number.  A v above 0 is kept above 0, so that m / sqrt(v) stays bounded.
  * A NaN or infinity among a block's new values makes its scale NaN. */
 typedef struct {
-    int64_t num_tensors;                /* >= 0 */
-    const gwtf_learn_tensor_t *tensors; /* HOST array [num_tensors] */
-    int32_t form;                       /* GWTF_STATE_* of all m and v */
-    int64_t step;                       /* >= 1, number of this step */
-    const int64_t *step_at;             /* DEVICE [1] to be read in its place, or NULL */
-    double lr;                          /* finite */
-    const float *lr_at;                 /* DEVICE [1] to be read in its place, or NULL */
-    double beta1, beta2;                /* within [0, 1) */
-    double eps;                         /* finite, >= 0 */
-    uint64_t seed;                      /* with GWTF_STATE_F8 only */
-    const float *factor;                /* DEVICE [1], or NULL = 1 */
+    const gwtf_learn_list_t *list; /* of GWTF_STATE_F32 or GWTF_STATE_F8 */
+    int64_t step;                  /* >= 1, number of this step */
+    const int64_t *step_at;        /* [1], to be read in its place, or NULL */
+    double lr;                     /* finite */
+    const float *lr_at;            /* [1], to be read in its place, or NULL */
+    double beta1, beta2;           /* within [0, 1), in 32 bits too */
+    double eps;                    /* finite, >= 0 */
+    uint64_t seed;                 /* with GWTF_STATE_F8 only */
+    const float *factor;           /* [1], or NULL = 1 */
 } gwtf_learn_adamw_t;
 gwtf_status_t gwtf_learn_adamw(gwtf_learn_t *h, const gwtf_learn_adamw_t *a);
 

@@ -16,6 +16,11 @@ struct gwtf_learn {
     char err[256];
 };
 
+struct gwtf_learn_list {
+    int32_t device;
+    LearnTable t;
+};
+
 namespace {
 
 thread_local char g_learn_err[256];
@@ -28,11 +33,6 @@ gwtf_status_t fail(gwtf_learn_t *h, gwtf_status_t code, const char *what, hipErr
     else snprintf(to, sizeof g_learn_err, "%s", what);
     return code;
 }
-gwtf_status_t fail_at(gwtf_learn_t *h, int64_t tensor, const char *what)
-{
-    snprintf(h->err, sizeof h->err, "tensor %lld: %s", static_cast<long long>(tensor), what);
-    return GWTF_ERR_INVALID_ARG;
-}
 
 #define LEARN_BEGIN(name)                                                               \
     if (!h) return fail(nullptr, GWTF_ERR_INVALID_ARG, name ": handle is NULL");        \
@@ -41,22 +41,32 @@ gwtf_status_t fail_at(gwtf_learn_t *h, int64_t tensor, const char *what)
     if (!(cond)) return fail(h, GWTF_ERR_INVALID_ARG, text);
 #define LEARN_CHECK(expr) \
     if (const char *bad = (expr)) return fail(h, GWTF_ERR_INVALID_ARG, bad);
-#define LEARN_CHECK_AT(i, expr) \
-    if (const char *bad = (expr)) return fail_at(h, i, bad);
 #define LEARN_LAUNCH(name, expr)                                                        \
     DeviceScope scope(h->device);                                                       \
     if (scope.e != hipSuccess) return fail(h, GWTF_ERR_DEVICE, "hipSetDevice", scope.e); \
     const hipError_t e = (expr);                                                        \
     return e == hipSuccess ? GWTF_OK : fail(h, GWTF_ERR_DEVICE, name " launch", e);
 
-constexpr int64_t kTensorSize = int64_t(1) << 35;
+constexpr int64_t kTensorSize = int64_t(1) << 35, kListSize = int64_t(1) << 42;
 
-// What every call asks of a tensor: its size, type and gradient.
-const char *bad_grad(const gwtf_learn_tensor_t &t)
+// What is wrong with a tensor of a list.
+const char *bad_tensor(const gwtf_learn_tensor_t &t, int32_t form)
 {
     if (t.size < 0 || t.size >= kTensorSize) return "size outside [0, 2^35)";
     if (!type_ok(t.grad_type)) return "unknown type of grad";
-    return bad_vector(t.grad, t.size, size_of(t.grad_type));
+    if (const char *bad = bad_vector(t.grad, t.size, size_of(t.grad_type))) return bad;
+    if (form == GWTF_STATE_NONE) return nullptr;
+    if (!type_ok(t.type)) return "unknown type";
+    if (t.grad_type != t.type && t.grad_type != GWTF_TYPE_F32) return "grad_type must be type or GWTF_TYPE_F32";
+    if (!std::isfinite(t.weight_decay)) return "weight_decay must be finite";
+    const bool f8 = form == GWTF_STATE_F8;
+    const char *bad = bad_vector(t.param, t.size, size_of(t.type));
+    if (!bad && t.master) bad = bad_vector(t.master, t.size, 4);
+    if (!bad) bad = bad_vector(t.m, t.size, f8 ? 1 : 4);
+    if (!bad) bad = bad_vector(t.v, t.size, f8 ? 1 : 4);
+    if (!bad && f8) bad = bad_vector(t.m_scale, t.size, 4);
+    if (!bad && f8) bad = bad_vector(t.v_scale, t.size, 4);
+    return bad;
 }
 
 } // namespace
@@ -125,47 +135,72 @@ extern "C" gwtf_status_t gwtf_learn_sample(gwtf_learn_t *h, const gwtf_learn_sam
     LEARN_LAUNCH("gwtf_learn_sample", launch_sample(*a, h->stream))
 }
 
+extern "C" gwtf_status_t gwtf_learn_list_create(gwtf_learn_t *h, int64_t num_tensors, const gwtf_learn_tensor_t *tensors, int32_t form,
+                                                gwtf_learn_list_t **out)
+{
+    if (out) *out = nullptr;
+    if (!h) return fail(nullptr, GWTF_ERR_INVALID_ARG, "gwtf_learn_list_create: handle is NULL");
+    LEARN_REQUIRE(out, "out is NULL")
+    LEARN_REQUIRE(num_tensors >= 0 && num_tensors <= (int64_t(1) << 30), "num_tensors outside [0, 2^30]")
+    LEARN_REQUIRE(num_tensors == 0 || tensors, "tensors is NULL")
+    LEARN_REQUIRE(form >= GWTF_STATE_F32 && form <= GWTF_STATE_NONE, "unknown form of the states")
+    int64_t values = 0;
+    for (int64_t i = 0; i < num_tensors; ++i) {
+        if (const char *bad = bad_tensor(tensors[i], form)) {
+            snprintf(h->err, sizeof h->err, "tensor %lld: %s", static_cast<long long>(i), bad);
+            return GWTF_ERR_INVALID_ARG;
+        }
+        values += tensors[i].size;
+        LEARN_REQUIRE(values <= kListSize, "more than 2^42 values")
+    }
+    gwtf_learn_list_t *list = new (std::nothrow) gwtf_learn_list_t();
+    if (!list) return fail(h, GWTF_ERR_OUT_OF_MEMORY, "host allocation failed");
+    list->device = h->device;
+    list->t.form = form;
+    DeviceScope scope(h->device);
+    hipError_t e = scope.e;
+    if (e == hipSuccess) e = build_table(num_tensors, tensors, list->t);
+    if (e != hipSuccess) {
+        delete list;
+        return fail(h, e == hipErrorOutOfMemory ? GWTF_ERR_OUT_OF_MEMORY : GWTF_ERR_DEVICE, "gwtf_learn_list_create", e);
+    }
+    *out = list;
+    return GWTF_OK;
+}
+
+extern "C" void gwtf_learn_list_destroy(gwtf_learn_list_t *list)
+{
+    if (!list) return;
+    DeviceScope scope(list->device);
+    if (list->t.base) (void)hipFree(list->t.base); // waits for the device
+    delete list;
+}
+
 extern "C" gwtf_status_t gwtf_learn_grad_norm(gwtf_learn_t *h, const gwtf_learn_grad_norm_t *a)
 {
     LEARN_BEGIN("gwtf_learn_grad_norm")
-    LEARN_REQUIRE(a->num_tensors >= 0, "num_tensors below 0")
-    LEARN_REQUIRE(a->num_tensors == 0 || a->tensors, "tensors is NULL")
+    LEARN_REQUIRE(a->list, "list is NULL")
+    LEARN_REQUIRE(a->list->device == h->device, "the list is on another device")
     LEARN_REQUIRE(a->max_norm >= 0, "max_norm must be >= 0")
     LEARN_REQUIRE(a->scale >= 0 && std::isfinite(a->scale), "scale must be finite and >= 0")
     LEARN_CHECK(a->norm ? bad_vector(a->norm, 1, 4) : nullptr)
     LEARN_CHECK(a->factor ? bad_vector(a->factor, 1, 4) : nullptr)
-    for (int64_t i = 0; i < a->num_tensors; ++i) LEARN_CHECK_AT(i, bad_grad(a->tensors[i]))
     if (!a->norm && !a->factor) return GWTF_OK;
-    LEARN_LAUNCH("gwtf_learn_grad_norm", launch_grad_norm(*a, h->ws, h->stream))
+    LEARN_LAUNCH("gwtf_learn_grad_norm", launch_grad_norm(*a, a->list->t, h->ws, h->stream))
 }
 
 extern "C" gwtf_status_t gwtf_learn_adamw(gwtf_learn_t *h, const gwtf_learn_adamw_t *a)
 {
     LEARN_BEGIN("gwtf_learn_adamw")
-    LEARN_REQUIRE(a->num_tensors >= 0, "num_tensors below 0")
-    LEARN_REQUIRE(a->num_tensors == 0 || a->tensors, "tensors is NULL")
-    LEARN_REQUIRE(a->form == GWTF_STATE_F32 || a->form == GWTF_STATE_F8, "unknown form of the states")
+    LEARN_REQUIRE(a->list, "list is NULL")
+    LEARN_REQUIRE(a->list->device == h->device, "the list is on another device")
+    LEARN_REQUIRE(a->list->t.form != GWTF_STATE_NONE, "the list has gradients alone")
     LEARN_REQUIRE(a->step_at || a->step >= 1, "step below 1")
     LEARN_REQUIRE(a->lr_at || std::isfinite(a->lr), "lr must be finite")
-    LEARN_REQUIRE(a->beta1 >= 0 && a->beta1 < 1 && a->beta2 >= 0 && a->beta2 < 1, "beta1 or beta2 outside [0, 1)")
+    LEARN_REQUIRE(a->beta1 >= 0 && float(a->beta1) < 1 && a->beta2 >= 0 && float(a->beta2) < 1, "beta1 or beta2 outside [0, 1)")
     LEARN_REQUIRE(a->eps >= 0 && std::isfinite(a->eps), "eps must be finite and >= 0")
     LEARN_CHECK(a->step_at ? bad_vector(a->step_at, 1, 8) : nullptr)
     LEARN_CHECK(a->lr_at ? bad_vector(a->lr_at, 1, 4) : nullptr)
     LEARN_CHECK(a->factor ? bad_vector(a->factor, 1, 4) : nullptr)
-    const bool f8 = a->form == GWTF_STATE_F8;
-    for (int64_t i = 0; i < a->num_tensors; ++i) {
-        const gwtf_learn_tensor_t &t = a->tensors[i];
-        LEARN_CHECK_AT(i, bad_grad(t))
-        LEARN_CHECK_AT(i, type_ok(t.type) ? nullptr : "unknown type")
-        LEARN_CHECK_AT(i, t.grad_type == t.type || t.grad_type == GWTF_TYPE_F32 ? nullptr : "grad_type must be type or GWTF_TYPE_F32")
-        LEARN_CHECK_AT(i, std::isfinite(t.weight_decay) ? nullptr : "weight_decay must be finite")
-        LEARN_CHECK_AT(i, bad_vector(t.param, t.size, size_of(t.type)))
-        LEARN_CHECK_AT(i, t.master ? bad_vector(t.master, t.size, 4) : nullptr)
-        LEARN_CHECK_AT(i, bad_vector(t.m, t.size, f8 ? 1 : 4))
-        LEARN_CHECK_AT(i, bad_vector(t.v, t.size, f8 ? 1 : 4))
-        LEARN_CHECK_AT(i, f8 ? bad_vector(t.m_scale, t.size, 4) : nullptr)
-        LEARN_CHECK_AT(i, f8 ? bad_vector(t.v_scale, t.size, 4) : nullptr)
-    }
-    if (a->num_tensors == 0) return GWTF_OK;
-    LEARN_LAUNCH("gwtf_learn_adamw", launch_adamw(*a, h->stream))
+    LEARN_LAUNCH("gwtf_learn_adamw", launch_adamw(*a, a->list->t, h->stream))
 }

@@ -1,49 +1,18 @@
 // Update phase of a node: the norm of its gradients (gwtf_learn_grad_norm) and
 // the AdamW step over its parameters (gwtf_learn_adamw).
 //
-// Tensors come as a list whose entries travel in the kernel's arguments, as many
-// as fit in 4 KB, so that no call copies a table or keeps one between calls; a
-// workgroup finds its tensor by a ballot over the entries' first chunks.
+// Tensors come as a table on the device.  A workgroup takes chunks of 2048 values and
+// finds a chunk's tensor in two reads that are the same for all its lanes.
 #include "learn_internal.h"
 #include "stage_device.h"
 
 #include <cmath>
+#include <new>
 
 namespace gwtf {
 namespace {
 
-// A launch takes fewer chunks than this: below 2^32 threads.
-constexpr int64_t kMostChunks = int64_t(1) << 23;
-
-// Which of `count` entries, in order of their first chunks, `chunk` belongs to.
-template <int K>
-__device__ __forceinline__ int entry_of(const uint32_t (&first)[K], int count, uint32_t chunk)
-{
-    const int lane = threadIdx.x & 63;
-    int at = -1;
-#pragma unroll
-    for (int base = 0; base < K; base += 64) {
-        const int i = base + lane;
-        at += __popcll(__ballot(i < count && first[i < K ? i : 0] <= chunk));
-    }
-    return __builtin_amdgcn_readfirstlane(at);
-}
-
 // ---- Norm ----
-
-constexpr int kNormEntries = 160;
-constexpr int kNormChunk = 256 * kVec; // values of a workgroup's step
-
-struct NormEntry {
-    const void *grad;
-    int64_t size;
-};
-struct NormArgs {
-    NormEntry e[kNormEntries];
-    uint32_t first[kNormEntries];
-    int32_t count;
-    uint32_t chunks;
-};
 
 __device__ __forceinline__ double wave_sum64(double v)
 {
@@ -52,18 +21,17 @@ __device__ __forceinline__ double wave_sum64(double v)
     return v;
 }
 
-// partial[workgroup] = sum of squares of the chunks blockIdx.x, blockIdx.x + gridDim.x, ..
+// partial[workgroup] = sum of squares of the chunks begin + blockIdx.x, begin + blockIdx.x + gridDim.x, ..
 template <class T>
-__global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double *partial)
+__global__ __launch_bounds__(256) void norm_kernel(const LearnEntry *entry, const uint32_t *owner, int64_t begin, int64_t end, double *partial)
 {
     __shared__ double red[4];
     double sum = 0.0;
-    for (uint32_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-        const int at = entry_of(a.first, a.count, chunk);
-        const T *g = static_cast<const T *>(a.e[at].grad);
-        const int64_t i = int64_t(chunk - a.first[at]) * kNormChunk + threadIdx.x * kVec;
+    for (int64_t chunk = begin + blockIdx.x; chunk < end; chunk += gridDim.x) {
+        const LearnEntry &t = entry[owner[chunk]];
+        const int64_t i = (chunk - t.first) * kChunk + threadIdx.x * kVec;
         float v[8];
-        load8(g + i, a.e[at].size - i, v);
+        load8(static_cast<const T *>(t.grad) + i, t.size - i, v);
 #pragma unroll
         for (int q = 0; q < kVec; ++q) sum = fma(double(v[q]), double(v[q]), sum);
     }
@@ -73,9 +41,8 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs a, double *partial)
     if (threadIdx.x == 0) partial[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// The sum of `count` partial sums, in a fixed order: to *sum, or as the results.
-__global__ __launch_bounds__(256) void norm_join_kernel(const double *partial, int count, double *sum, double max_norm, double scale,
-                                                        float *norm, float *factor)
+// The sum of `count` partial sums, in a fixed order, and the results.
+__global__ __launch_bounds__(256) void norm_join_kernel(const double *partial, int count, double max_norm, double scale, float *norm, float *factor)
 {
     __shared__ double red[4];
     double v = 0.0;
@@ -84,35 +51,17 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const double *partial, i
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     if (threadIdx.x) return;
-    v = (red[0] + red[1]) + (red[2] + red[3]);
-    if (sum) {
-        *sum = v;
-        return;
-    }
-    const double n = scale * sqrt(v);
+    const double n = scale * sqrt((red[0] + red[1]) + (red[2] + red[3]));
     if (norm) *norm = float(n);
     if (factor) *factor = n < __builtin_inf() ? float(n > max_norm ? scale * (max_norm / n) : scale) : __builtin_nanf("");
 }
 
 // ---- AdamW ----
 
-constexpr int kAdamEntries = 50;
-constexpr int kAdamChunk = 256 * kVec * 2;
-
-struct AdamEntry {
-    int64_t size;
-    const void *grad;
-    void *param;
-    float *master;
-    void *m, *v;
-    float *m_scale, *v_scale;
-    float decay;
-    uint32_t site;
-};
 struct AdamArgs {
-    AdamEntry e[kAdamEntries];
-    uint32_t first[kAdamEntries];
-    int32_t count;
+    const LearnEntry *entry;
+    const uint32_t *owner;
+    int64_t begin; // chunk of the first workgroup
     float lr, beta1, rest1, beta2, rest2, eps, unbias1, unbias2;
     uint32_t k0, k1;
     double log_beta1, log_beta2;
@@ -120,7 +69,6 @@ struct AdamArgs {
     const int64_t *step_at;
     const float *lr_at, *factor;
 };
-static_assert(sizeof(NormArgs) + 8 <= 4096 && sizeof(AdamArgs) <= 4096, "kernel arguments");
 
 __device__ __forceinline__ void philox4x32(uint32_t k0, uint32_t k1, uint32_t c[4])
 {
@@ -209,143 +157,162 @@ __device__ __forceinline__ u32x2 narrow_f8(const float x[8], const uint32_t r[8]
     return w;
 }
 
+// The root, to its last bit or so; the hardware's knows no values below 2^-126.
+__device__ __forceinline__ float root(float x)
+{
+    const bool small = x < 0x1p-96f;
+    const float r = __builtin_amdgcn_sqrtf(small ? x * 0x1p64f : x);
+    return small ? r * 0x1p-32f : r;
+}
+
 template <class T, class G, bool F8>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a)
 {
+    // m and v follow the formula one rounding an operation, so that 8-bit states
+    // are the same wherever the step is repeated
 #pragma clang fp contract(off)
-    const int at = entry_of(a.first, a.count, blockIdx.x);
-    const AdamEntry t = a.e[at];
+    const int64_t chunk = a.begin + blockIdx.x;
+    const LearnEntry t = a.entry[a.owner[chunk]];
     const float factor = a.factor ? *a.factor : 1.f;
     if (!(__builtin_fabsf(factor) < __builtin_inff())) return;
     const float lr = a.lr_at ? *a.lr_at : a.lr;
     int64_t step = a.step;
-    float unbias1 = a.unbias1, unbias2 = a.unbias2;
+    float unbias1 = a.unbias1, unbias2 = a.unbias2; // 1 / (1 - beta^step)
     if (a.step_at) {
         step = *a.step_at;
-        unbias1 = float(-expm1(double(step) * a.log_beta1));
-        unbias2 = float(-expm1(double(step) * a.log_beta2));
+        unbias1 = float(-1.0 / expm1(double(step) * a.log_beta1));
+        unbias2 = float(-1.0 / expm1(double(step) * a.log_beta2));
     }
-    const int64_t begin = int64_t(blockIdx.x - a.first[at]) * kAdamChunk;
+    const int64_t i = (chunk - t.first) * kChunk + threadIdx.x * kVec, n = t.size - i;
+    float g[8], p[8], m[8], v[8];
+    load8(static_cast<const G *>(t.grad) + i, n, g);
+    if (t.master) load8(t.master + i, n, p);
+    else load8(static_cast<const T *>(t.param) + i, n, p);
+    if constexpr (F8) {
+        const bool in = n > 0;
+        widen_f8<false>(load_f8(static_cast<const uint8_t *>(t.m) + i, n), in ? t.m_scale[i / GWTF_STATE_BLOCK] : 0.f, m);
+        widen_f8<true>(load_f8(static_cast<const uint8_t *>(t.v) + i, n), in ? t.v_scale[i / GWTF_STATE_BLOCK] : 0.f, v);
+    } else {
+        load8(static_cast<const float *>(t.m) + i, n, m);
+        load8(static_cast<const float *>(t.v) + i, n, v);
+    }
 #pragma unroll
-    for (int q = 0; q < kAdamChunk / (256 * kVec); ++q) {
-        const int64_t i = begin + (q * 256 + threadIdx.x) * kVec, n = t.size - i;
-        float g[8], p[8], m[8], v[8];
-        load8(static_cast<const G *>(t.grad) + i, n, g);
-        if (t.master) load8(t.master + i, n, p);
-        else load8(static_cast<const T *>(t.param) + i, n, p);
-        if constexpr (F8) {
-            const bool in = n > 0;
-            widen_f8<false>(load_f8(static_cast<const uint8_t *>(t.m) + i, n), in ? t.m_scale[i / GWTF_STATE_BLOCK] : 0.f, m);
-            widen_f8<true>(load_f8(static_cast<const uint8_t *>(t.v) + i, n), in ? t.v_scale[i / GWTF_STATE_BLOCK] : 0.f, v);
-        } else {
-            load8(static_cast<const float *>(t.m) + i, n, m);
-            load8(static_cast<const float *>(t.v) + i, n, v);
-        }
+    for (int k = 0; k < kVec; ++k) {
+        g[k] = g[k] * factor;
+        m[k] = m[k] * a.beta1 + g[k] * a.rest1;
+        v[k] = v[k] * a.beta2 + g[k] * g[k] * a.rest2;
+        const float den = root(v[k] * unbias2) + a.eps;
+        const float d = m[k] * unbias1 * __builtin_amdgcn_rcpf(den < 0x1p-126f ? 0x1p-126f : den);
+        p[k] = p[k] - lr * (d + t.decay * p[k]);
+    }
+    store8(static_cast<T *>(t.param) + i, n, p);
+    if (t.master) store8(t.master + i, n, p);
+    if constexpr (F8) {
+        // values past the end have no part in the scale of the last block
 #pragma unroll
         for (int k = 0; k < kVec; ++k) {
-            g[k] = g[k] * factor;
-            m[k] = m[k] * a.beta1 + g[k] * a.rest1;
-            v[k] = v[k] * a.beta2 + g[k] * g[k] * a.rest2;
-            const float d = (m[k] / unbias1) / (sqrtf(v[k] / unbias2) + a.eps);
-            p[k] = p[k] - lr * (d + t.decay * p[k]);
+            m[k] = k < n ? m[k] : 0.f;
+            v[k] = k < n ? v[k] : 0.f;
         }
-        store8(static_cast<T *>(t.param) + i, n, p);
-        if (t.master) store8(t.master + i, n, p);
-        if constexpr (F8) {
-            // values past the end have no part in the scale of the last block
+        uint32_t c[4] = {uint32_t(i / kVec), t.site, uint32_t(step), uint32_t(uint64_t(step) >> 32)}, r[8];
+        philox4x32(a.k0, a.k1, c);
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                m[k] = k < n ? m[k] : 0.f;
-                v[k] = k < n ? v[k] : 0.f;
-            }
-            uint32_t c[4] = {uint32_t(i / kVec), t.site, uint32_t(step), uint32_t(uint64_t(step) >> 32)}, r[8];
-            philox4x32(a.k0, a.k1, c);
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) r[k] = (k & 1) ? c[k / 2] >> 16 : c[k / 2] & 0xffffu;
-            float sm, sv;
-            const u32x2 wm = narrow_f8<false>(m, r, sm), wv = narrow_f8<true>(v, r, sv);
-            store_f8(static_cast<uint8_t *>(t.m) + i, n, wm);
-            store_f8(static_cast<uint8_t *>(t.v) + i, n, wv);
-            if (n > 0 && i % GWTF_STATE_BLOCK == 0) {
-                t.m_scale[i / GWTF_STATE_BLOCK] = sm;
-                t.v_scale[i / GWTF_STATE_BLOCK] = sv;
-            }
-        } else {
-            store8(static_cast<float *>(t.m) + i, n, m);
-            store8(static_cast<float *>(t.v) + i, n, v);
+        for (int k = 0; k < kVec; ++k) r[k] = (k & 1) ? c[k / 2] >> 16 : c[k / 2] & 0xffffu;
+        float sm, sv;
+        const u32x2 wm = narrow_f8<false>(m, r, sm), wv = narrow_f8<true>(v, r, sv);
+        store_f8(static_cast<uint8_t *>(t.m) + i, n, wm);
+        store_f8(static_cast<uint8_t *>(t.v) + i, n, wv);
+        if (n > 0 && i % GWTF_STATE_BLOCK == 0) {
+            t.m_scale[i / GWTF_STATE_BLOCK] = sm;
+            t.v_scale[i / GWTF_STATE_BLOCK] = sv;
         }
+    } else {
+        store8(static_cast<float *>(t.m) + i, n, m);
+        store8(static_cast<float *>(t.v) + i, n, v);
     }
 }
 
-template <class T, class G>
-hipError_t run_adamw(const AdamArgs &a, int64_t chunks, bool f8, hipStream_t s)
-{
-    return launch(f8 ? adamw_kernel<T, G, true> : adamw_kernel<T, G, false>, chunks, 256, s, a);
-}
-
-hipError_t flush_adamw(AdamArgs &a, int64_t chunks, int type, int grad_type, bool f8, hipStream_t s)
+using AdamKernel = void (*)(AdamArgs);
+template <bool F8>
+AdamKernel adamw_of(int type, int grad_type)
 {
     const bool wide = grad_type == GWTF_TYPE_F32;
     switch (type) {
-    case GWTF_TYPE_F32: return run_adamw<float, float>(a, chunks, f8, s);
-    case GWTF_TYPE_F16: return wide ? run_adamw<f16_t, float>(a, chunks, f8, s) : run_adamw<f16_t, f16_t>(a, chunks, f8, s);
-    default: return wide ? run_adamw<bf16_t, float>(a, chunks, f8, s) : run_adamw<bf16_t, bf16_t>(a, chunks, f8, s);
-    }
-}
-
-hipError_t flush_norm(const NormArgs &a, int type, int64_t groups, double *partial, hipStream_t s)
-{
-    switch (type) {
-    case GWTF_TYPE_F32: return launch(norm_kernel<float>, groups, 256, s, a, partial);
-    case GWTF_TYPE_F16: return launch(norm_kernel<f16_t>, groups, 256, s, a, partial);
-    default: return launch(norm_kernel<bf16_t>, groups, 256, s, a, partial);
+    case GWTF_TYPE_F32: return adamw_kernel<float, float, F8>;
+    case GWTF_TYPE_F16: return wide ? adamw_kernel<f16_t, float, F8> : adamw_kernel<f16_t, f16_t, F8>;
+    default: return wide ? adamw_kernel<bf16_t, float, F8> : adamw_kernel<bf16_t, bf16_t, F8>;
     }
 }
 
 } // namespace
 
-hipError_t launch_grad_norm(const gwtf_learn_grad_norm_t &a, const LearnWorkspace &w, hipStream_t s)
+hipError_t build_table(int64_t num, const gwtf_learn_tensor_t *tensors, LearnTable &t)
 {
-    const int64_t most = 8 * int64_t(w.cus);
-    NormArgs args;
+    // classes of types, then the tensors of each in the order of the list
+    const int kinds = 9;
+    auto kind_of = [&](const gwtf_learn_tensor_t &x) { return t.form == GWTF_STATE_NONE ? x.grad_type : 3 * x.grad_type + x.type; };
     int64_t chunks = 0, used = 0;
-    args.count = 0;
-    int type = 0;
-    hipError_t e = hipSuccess;
-    auto flush = [&]() {
-        if (!args.count) return hipSuccess;
-        const int64_t groups = chunks < most ? chunks : most;
-        if (used + groups > kNormSlots) { // the sums so far become the first one
-            const hipError_t j = launch(norm_join_kernel, 1, 256, s, w.partial, int(used), w.partial, 0.0, 0.0, nullptr, nullptr);
-            if (j != hipSuccess) return j;
-            used = 1;
-        }
-        args.chunks = uint32_t(chunks);
-        const hipError_t k = flush_norm(args, type, groups, w.partial + used, s);
-        used += groups;
-        args.count = 0;
-        chunks = 0;
-        return k;
-    };
-    for (int64_t i = 0; i < a.num_tensors; ++i) {
-        const gwtf_learn_tensor_t &t = a.tensors[i];
-        if (!t.size) continue;
-        const int64_t more = (t.size + kNormChunk - 1) / kNormChunk;
-        if (args.count == kNormEntries || (args.count && (t.grad_type != type || chunks + more > int64_t(1) << 31)))
-            if ((e = flush()) != hipSuccess) return e;
-        type = t.grad_type;
-        args.e[args.count] = {t.grad, t.size};
-        args.first[args.count++] = uint32_t(chunks);
-        chunks += more;
+    for (int64_t i = 0; i < num; ++i) {
+        chunks += (tensors[i].size + kChunk - 1) / kChunk;
+        used += tensors[i].size != 0;
     }
-    if ((e = flush()) != hipSuccess) return e;
-    return launch(norm_join_kernel, 1, 256, s, w.partial, int(used), nullptr, a.max_norm, a.scale, a.norm, a.factor);
+    const size_t entries = sizeof(LearnEntry) * size_t(used), bytes = entries + sizeof(uint32_t) * size_t(chunks);
+    if (!bytes) return hipSuccess;
+    unsigned char *host = new (std::nothrow) unsigned char[bytes];
+    if (!host) return hipErrorOutOfMemory;
+    LearnEntry *entry = reinterpret_cast<LearnEntry *>(host);
+    uint32_t *owner = reinterpret_cast<uint32_t *>(host + entries);
+    int64_t at = 0, chunk = 0;
+    for (int kind = 0; kind < kinds; ++kind) {
+        const int64_t begin = chunk;
+        for (int64_t i = 0; i < num; ++i) {
+            const gwtf_learn_tensor_t &x = tensors[i];
+            if (!x.size || kind_of(x) != kind) continue;
+            entry[at] = {x.size, x.grad, x.param, x.master, x.m, x.v, x.m_scale, x.v_scale, chunk, x.weight_decay, x.site};
+            for (int64_t q = (x.size + kChunk - 1) / kChunk; q > 0; --q) owner[chunk++] = uint32_t(at);
+            ++at;
+            t.cls[t.classes] = {x.type, x.grad_type, begin, chunk};
+        }
+        if (chunk > begin) ++t.classes;
+    }
+    hipError_t e = hipMalloc(&t.base, bytes);
+    if (e == hipSuccess) {
+        e = hipMemcpy(t.base, host, bytes, hipMemcpyHostToDevice);
+        if (e != hipSuccess) {
+            (void)hipFree(t.base);
+            t.base = nullptr;
+        }
+    }
+    delete[] host;
+    t.entry = static_cast<const LearnEntry *>(t.base);
+    t.owner = reinterpret_cast<const uint32_t *>(static_cast<const unsigned char *>(t.base) + entries);
+    return e;
 }
 
-hipError_t launch_adamw(const gwtf_learn_adamw_t &a, hipStream_t s)
+hipError_t launch_grad_norm(const gwtf_learn_grad_norm_t &a, const LearnTable &t, const LearnWorkspace &w, hipStream_t s)
 {
-    const bool f8 = a.form == GWTF_STATE_F8;
+    int64_t used = 0;
+    for (int c = 0; c < t.classes;) {
+        // classes that differ in the parameters' type alone are one here
+        int next = c + 1;
+        while (next < t.classes && t.cls[next].grad_type == t.cls[c].grad_type) ++next;
+        const int64_t begin = t.cls[c].begin, end = t.cls[next - 1].end;
+        const int64_t groups = end - begin < kNormGroups ? end - begin : kNormGroups;
+        const int type = t.cls[c].grad_type;
+        auto kernel = type == GWTF_TYPE_F32 ? norm_kernel<float> : type == GWTF_TYPE_F16 ? norm_kernel<f16_t> : norm_kernel<bf16_t>;
+        const hipError_t e = launch(kernel, groups, 256, s, t.entry, t.owner, begin, end, w.partial + used);
+        if (e != hipSuccess) return e;
+        used += groups;
+        c = next;
+    }
+    return launch(norm_join_kernel, 1, 256, s, w.partial, int(used), a.max_norm, a.scale, a.norm, a.factor);
+}
+
+hipError_t launch_adamw(const gwtf_learn_adamw_t &a, const LearnTable &t, hipStream_t s)
+{
     AdamArgs args;
+    args.entry = t.entry;
+    args.owner = t.owner;
     args.lr = float(a.lr);
     args.beta1 = float(a.beta1);
     args.rest1 = float(1.0 - a.beta1);
@@ -354,35 +321,26 @@ hipError_t launch_adamw(const gwtf_learn_adamw_t &a, hipStream_t s)
     args.eps = float(a.eps);
     args.log_beta1 = std::log(a.beta1); // -infinity for 0: then expm1 gives -1
     args.log_beta2 = std::log(a.beta2);
-    args.unbias1 = a.step_at ? 1.f : float(-std::expm1(double(a.step) * args.log_beta1));
-    args.unbias2 = a.step_at ? 1.f : float(-std::expm1(double(a.step) * args.log_beta2));
+    args.unbias1 = a.step_at ? 1.f : float(-1.0 / std::expm1(double(a.step) * args.log_beta1));
+    args.unbias2 = a.step_at ? 1.f : float(-1.0 / std::expm1(double(a.step) * args.log_beta2));
     args.k0 = uint32_t(a.seed);
     args.k1 = uint32_t(a.seed >> 32);
     args.step = a.step;
     args.step_at = a.step_at;
     args.lr_at = a.lr_at;
     args.factor = a.factor;
-    args.count = 0;
-    int64_t chunks = 0;
-    int type = 0, grad_type = 0;
-    hipError_t e = hipSuccess;
-    for (int64_t i = 0; i < a.num_tensors; ++i) {
-        const gwtf_learn_tensor_t &t = a.tensors[i];
-        if (!t.size) continue;
-        const int64_t more = (t.size + kAdamChunk - 1) / kAdamChunk;
-        if (args.count == kAdamEntries ||
-            (args.count && (t.type != type || t.grad_type != grad_type || chunks + more > kMostChunks))) {
-            if ((e = flush_adamw(args, chunks, type, grad_type, f8, s)) != hipSuccess) return e;
-            args.count = 0;
-            chunks = 0;
+    const int64_t slab = kLaunchThreads / 256;
+    for (int c = 0; c < t.classes; ++c) {
+        const AdamKernel kernel = t.form == GWTF_STATE_F8 ? adamw_of<true>(t.cls[c].type, t.cls[c].grad_type)
+                                                          : adamw_of<false>(t.cls[c].type, t.cls[c].grad_type);
+        for (int64_t b = t.cls[c].begin; b < t.cls[c].end; b += slab) {
+            args.begin = b;
+            const int64_t n = t.cls[c].end - b < slab ? t.cls[c].end - b : slab;
+            const hipError_t e = launch(kernel, n, 256, s, args);
+            if (e != hipSuccess) return e;
         }
-        type = t.type;
-        grad_type = t.grad_type;
-        args.e[args.count] = {t.size, t.grad, t.param, t.master, t.m, t.v, t.m_scale, t.v_scale, t.weight_decay, t.site};
-        args.first[args.count++] = uint32_t(chunks);
-        chunks += more;
     }
-    return args.count ? flush_adamw(args, chunks, type, grad_type, f8, s) : hipSuccess;
+    return hipSuccess;
 }
 
 } // namespace gwtf

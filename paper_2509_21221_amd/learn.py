@@ -2,6 +2,7 @@
 marshalling only -- the operators run in the HIP library).
 
 The functions carry the C names (``gwtf_learn_create``, ``gwtf_learn_sample``,
+``gwtf_learn_list_create``, ``gwtf_learn_list_destroy``,
 ``gwtf_learn_grad_norm``, ``gwtf_learn_adamw``, ``gwtf_learn_destroy``,
 ``gwtf_learn_last_error``); ``LearnOps`` wraps them for torch device tensors.
 PyTorch only provides device memory and the HIP stream.
@@ -21,6 +22,7 @@ GWTF_UNIFORM_F32 = 0
 GWTF_UNIFORM_F64 = 1
 GWTF_STATE_F32 = 0
 GWTF_STATE_F8 = 1
+GWTF_STATE_NONE = 2
 GWTF_STATE_BLOCK = 128
 
 _i32, _i64, _u32, _u64, _vp, _f32, _f64 = (ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64,
@@ -40,14 +42,12 @@ class gwtf_learn_tensor_t(ctypes.Structure):
 
 
 class gwtf_learn_grad_norm_t(ctypes.Structure):
-    _fields_ = [("num_tensors", _i64), ("tensors", ctypes.POINTER(gwtf_learn_tensor_t)), ("max_norm", _f64),
-                ("scale", _f64), ("norm", _vp), ("factor", _vp)]
+    _fields_ = [("list", _vp), ("max_norm", _f64), ("scale", _f64), ("norm", _vp), ("factor", _vp)]
 
 
 class gwtf_learn_adamw_t(ctypes.Structure):
-    _fields_ = [("num_tensors", _i64), ("tensors", ctypes.POINTER(gwtf_learn_tensor_t)), ("form", _i32), ("step", _i64),
-                ("step_at", _vp), ("lr", _f64), ("lr_at", _vp), ("beta1", _f64), ("beta2", _f64), ("eps", _f64),
-                ("seed", _u64), ("factor", _vp)]
+    _fields_ = [("list", _vp), ("step", _i64), ("step_at", _vp), ("lr", _f64), ("lr_at", _vp), ("beta1", _f64),
+                ("beta2", _f64), ("eps", _f64), ("seed", _u64), ("factor", _vp)]
 
 
 _CALLS = {"sample": gwtf_learn_sample_t, "grad_norm": gwtf_learn_grad_norm_t, "adamw": gwtf_learn_adamw_t}
@@ -66,6 +66,10 @@ def _library():
         lib.gwtf_learn_destroy.restype = None
         lib.gwtf_learn_last_error.argtypes = [_vp]
         lib.gwtf_learn_last_error.restype = ctypes.c_char_p
+        lib.gwtf_learn_list_create.argtypes = [_vp, _i64, ctypes.POINTER(gwtf_learn_tensor_t), _i32, ctypes.POINTER(_vp)]
+        lib.gwtf_learn_list_create.restype = ctypes.c_int
+        lib.gwtf_learn_list_destroy.argtypes = [_vp]
+        lib.gwtf_learn_list_destroy.restype = None
         for name, args in _CALLS.items():
             fn = getattr(lib, "gwtf_learn_" + name)
             fn.argtypes = [_vp, ctypes.POINTER(args)]
@@ -94,6 +98,17 @@ def gwtf_learn_destroy(handle) -> None:
     _library().gwtf_learn_destroy(handle)
 
 
+def gwtf_learn_list_create(handle, tensors, form: int):
+    """Create a list of an array of gwtf_learn_tensor_t; returns an opaque pointer."""
+    out = _vp()
+    _check(_library().gwtf_learn_list_create(handle, len(tensors), tensors, form, ctypes.byref(out)), handle)
+    return out
+
+
+def gwtf_learn_list_destroy(list_) -> None:
+    _library().gwtf_learn_list_destroy(list_)
+
+
 def gwtf_learn_sample(handle, args: gwtf_learn_sample_t) -> None:
     _check(_library().gwtf_learn_sample(handle, args), handle)
 
@@ -116,11 +131,20 @@ class Parameters:
     (accumulated, or copied), and a parameter that is to live elsewhere needs a new list."""
 
     def __init__(self, owner, lists, form, array):
+        self.list = None
         self.owner = owner
         self.params, self.grads, self.m, self.v, self.m_scales, self.v_scales, self.master = lists
         self.form = form
-        self.array = array
         self.tensors = [t for one in lists if one for t in one]
+        self.list = gwtf_learn_list_create(owner.handle, array, form)
+
+    def __del__(self):
+        try:
+            if self.list is not None:
+                gwtf_learn_list_destroy(self.list)
+                self.list = None
+        except Exception:
+            pass
 
 
 class LearnOps:
@@ -275,6 +299,8 @@ class LearnOps:
         True to make them.  ``weight_decay``: a number or one for each tensor;
         ``sites``: numbers of the tensors for 8-bit rounding, their places in the list by
         default.  With ``params`` None the list is for ``grad_norm`` alone."""
+        if self.handle is None:
+            raise RuntimeError("LearnOps: closed")
         torch, types = self.torch, tuple(self._types)
         f32 = torch.float32
         if params is None:
@@ -282,7 +308,7 @@ class LearnOps:
             array = (gwtf_learn_tensor_t * len(grads))()
             for a, g in zip(array, grads):
                 a.size, a.grad_type, a.grad = g.numel(), self._types[g.dtype], g.data_ptr()
-            return Parameters(self, (None, grads, None, None, None, None, None), None, array)
+            return Parameters(self, (None, grads, None, None, None, None, None), GWTF_STATE_NONE, array)
         if bits not in (8, 32):
             raise ValueError("bits: 8 or 32")
         params = self._list(params, None, types, "params")
@@ -336,9 +362,11 @@ class LearnOps:
         return Parameters(self, (params, grads, m, v, ms, vs, master), GWTF_STATE_F8 if bits == 8 else GWTF_STATE_F32, array)
 
     def _group(self, group):
+        if self.handle is None:
+            raise RuntimeError("LearnOps: closed")
         if not isinstance(group, Parameters) or group.owner is not self:
             raise ValueError("need the Parameters of this object's parameters()")
-        return len(group.array), group.array
+        return group.list
 
     def grad_norm(self, group, max_norm: float = math.inf, scale: float = 1.0, out=None):
         """(norm, factor), float32 tensors of one: ``scale`` times the norm of
@@ -348,7 +376,7 @@ class LearnOps:
             out = self._f32.new_empty(1), self._f32.new_empty(1)
         norm, factor = out
         f32 = self.torch.float32
-        a = gwtf_learn_grad_norm_t(*self._group(group), max_norm, scale, None if norm is None else self._vec(norm, 1, f32, "norm"),
+        a = gwtf_learn_grad_norm_t(self._group(group), max_norm, scale, None if norm is None else self._vec(norm, 1, f32, "norm"),
                                    None if factor is None else self._vec(factor, 1, f32, "factor"))
         self._run("grad_norm", a, (*group.tensors, norm, factor) if self._current(self.device) != self._raw else ())
         return out
@@ -358,16 +386,14 @@ class LearnOps:
         ``step`` (1 for the first) are numbers or device tensors of one (float32, int64);
         ``factor``: ``grad_norm``'s, one that is not finite leaves everything
         as it was; ``seed``: of 8-bit states' rounding."""
-        count, array = self._group(group)
-        if group.form is None:
-            raise ValueError("the list has gradients alone")
+        table = self._group(group)
         if not 0 <= seed < 1 << 64:
             raise ValueError("seed must fit in 64 bits and be >= 0")
         if factor is not None and not isinstance(factor, self.torch.Tensor):
             raise TypeError("factor: need a device tensor, as grad_norm gives it")
         lr_, lr_at = self._one(lr, self.torch.float32, "lr")
         step_, step_at = self._one(step, self.torch.int64, "step")
-        a = gwtf_learn_adamw_t(count, array, group.form, step_, step_at, lr_, lr_at, betas[0], betas[1], eps, seed,
+        a = gwtf_learn_adamw_t(table, step_, step_at, lr_, lr_at, betas[0], betas[1], eps, seed,
                                None if factor is None else self._one(factor, self.torch.float32, "factor")[1])
         self._run("adamw", a, (*group.tensors, lr, step, factor) if self._current(self.device) != self._raw else ())
 

@@ -261,7 +261,7 @@ def test_grad_norm_refusals(ops):
             ops.parameters(None, bad)
     with LearnOps() as other, pytest.raises(ValueError, match="Parameters"):
         other.grad_norm(group)
-    with pytest.raises(ValueError, match="alone"):
+    with pytest.raises(GwtfError, match="alone"):
         ops.adamw(group, 1e-3, 1)
 
 
@@ -465,9 +465,8 @@ def test_adamw_refusals(ops):
                         (dict(params=[x.t() for x in (torch.ones(4, 8, device="cuda"),)], grads=g[:1]), "contiguous")):
         with pytest.raises((ValueError, TypeError), match=match):
             ops.parameters(**args)
-    bad = ops.parameters(p, g, weight_decay=math.inf)
     with pytest.raises(GwtfError, match="tensor 0: weight_decay"):
-        ops.adamw(bad, 1e-3, 1)
+        ops.parameters(p, g, weight_decay=math.inf)
 
 
 def test_closed(ops):

@@ -21,7 +21,7 @@ def text():
 def test_every_declared_function_is_exported_and_bound():
     lib = mcf.load_library()
     names = sorted(set(re.findall(r"\b(gwtf_learn_\w+)\s*\(", text())))
-    assert len(names) == 6
+    assert len(names) == 8
     for name in names:
         assert hasattr(lib, name), name
         assert callable(getattr(learn, name)), name
@@ -30,7 +30,7 @@ def test_every_declared_function_is_exported_and_bound():
 def test_constants_match_the_header():
     found = dict(re.findall(r"\b(GWTF_(?:UNIFORM|STATE)_\w+)\s*=\s*(\d+)", text()))
     found.update(re.findall(r"#define (GWTF_\w+) (\d+)", text()))
-    assert len(found) == 5
+    assert len(found) == 6
     for name, value in found.items():
         assert getattr(learn, name) == int(value), name
 
@@ -64,6 +64,10 @@ def test_null_arguments_fail_cleanly():
     assert lib.gwtf_learn_create(-1, None, ctypes.byref(out)) == mcf.GWTF_ERR_INVALID_ARG
     assert out.value is None
     assert lib.gwtf_learn_create(0, None, None) == mcf.GWTF_ERR_INVALID_ARG
+    out = ctypes.c_void_p(1)
+    assert lib.gwtf_learn_list_create(None, 0, None, 0, ctypes.byref(out)) == mcf.GWTF_ERR_INVALID_ARG
+    assert out.value is None
+    lib.gwtf_learn_list_destroy(None)
 
 
 def test_parts_of_one_memory_are_refused():
