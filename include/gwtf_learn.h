@@ -82,7 +82,8 @@ const char *gwtf_learn_last_error(const gwtf_learn_t *h);
  * and of those before it, is above u times that of all:
  *   ids = its index, logp = ln of its share of the sum, kept = how many stay.
  * Sums, w and their products with u and p are held in 64 bits, so that a draw is
- * that of exact arithmetic unless u or p falls within some 1e-13 of a border.  u counts as within [0, 1)
+ * that of exact arithmetic unless u or p falls within some 1e-13 of a border; a w
+ * below 2^-600 may count as 0.  u counts as within [0, 1)
  * (a NaN as 0).  An entry of -infinity is masked; a row of nothing else gives
  * ids -1, logp -infinity, kept 0.  A row with a NaN or +infinity, and one
  * whose settings are out of range (below), gives ids -1, logp NaN, kept 0.

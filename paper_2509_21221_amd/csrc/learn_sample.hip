@@ -2,15 +2,22 @@
 //
 //   w_j = 2^y_j,  y_j = (x_j - max x) log2 e / T,  in 64 bits
 //
-// A workgroup takes a row.  The tokens that stay are the first n in the order of
-// descending logits, so all three filters are cuts in that order: a key (the
-// logit's bits in an order of unsigned words) and how many of the entries with
-// that key stay, by ascending index.  A cut by number or by sum is found by
-// counting keys in equal bins between two bounds (and adding up w, as whole
-// numbers, so that the order of the additions does not matter), and again within
-// the bin that the cut falls into, until a bin is one key.  The draw needs no
-// order: sums of what stays over segments of the row, then a prefix within the
-// segment that u falls into.
+// A workgroup takes a row and keeps it in registers, up to 131,072 columns of 16
+// bits or 65,536 of 32, since every filter needs another look at it; a lane also
+// keeps the largest of each of its eights, so that looks at few entries pass
+// over the others.
+//
+// The tokens that stay are the first n in the order of descending logits, so all
+// three filters are cuts in that order: a key (the logit's bits in an order of
+// unsigned words) and how many of the entries with that key stay, by ascending
+// index.  A cut by number or by sum is found by counting keys in equal bins
+// between two bounds (and adding up w, as whole numbers, so that the order of the
+// additions does not matter), and again within the bin that the cut falls into,
+// until a bin is one key.  The draw needs no order: sums of what stays over
+// segments of the row, then a prefix within the segment that u falls into.
+//
+// With top_k up to kFew the k-th largest of the eights' largest entries is a bound
+// that about k entries reach; they are ranked by comparison, and one wave does the rest.
 #include "learn_internal.h"
 #include "stage_device.h"
 
@@ -32,7 +39,7 @@ __device__ __forceinline__ float value_of(uint32_t k)
     return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
 }
 
-// 2^y, y <= 0, to about 1e-15: 2^f by the exponential's series in f ln 2, |f| <= 1/2.
+// 2^y by the exponential's series in f ln 2, |f| <= 1/2, to about 1e-15.
 __device__ __forceinline__ double exp2_64(double y)
 {
     y = fmax(y, -1100.0);
@@ -60,6 +67,24 @@ __device__ __forceinline__ double wave_sum64(double v)
     for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
     return v;
 }
+__device__ __forceinline__ uint32_t scan_up(uint32_t v, int lane) // sums over lanes 0 .. lane
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(v, d);
+        v += lane >= d ? o : 0u;
+    }
+    return v;
+}
+__device__ __forceinline__ double scan_up(double v, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const double o = __shfl_up(v, d);
+        v += lane >= d ? o : 0.0;
+    }
+    return v;
+}
 __device__ __forceinline__ uint32_t wave_add(uint32_t v)
 {
 #pragma unroll
@@ -73,17 +98,27 @@ struct Cut {
     uint32_t key, ties, n;
 };
 
-constexpr int kBins = 2048, kSegs = 1024;
+constexpr int kBins = 2048;
+constexpr int kFew = 256;  // top_k up to which the entries are ranked
+constexpr int kList = 512; // entries that can be ranked
 
-template <int WAVES>
+// SEGS: segments of a row
+template <int WAVES, int SEGS>
 struct Shared {
     uint32_t count[kBins];
-    uint64_t mass[kBins];
-    double sum[kSegs];    // of a segment's w whose keys are above the cut's
-    uint32_t tied[kSegs]; // its entries with the cut's key
+    union {
+        uint64_t mass[kBins];
+        struct {
+            uint64_t list[kList], order[kList];
+            double w[kFew];
+        } few;
+    };
+    double sum[SEGS];    // of a segment's w whose keys are above the cut's
+    uint32_t tied[SEGS]; // its entries with the cut's key
     double wsum[WAVES];
-    uint32_t wcount[WAVES];
+    uint32_t wcount[WAVES], wmost[WAVES], wleast[WAVES];
     uint32_t at; // first bin from the top that reaches a target
+    uint32_t listed;
     struct {
         uint32_t count, above;
         double above_mass;
@@ -94,34 +129,80 @@ struct Shared {
     } draw;
 };
 
-template <class T, int WAVES>
+// S: eights that a lane keeps in registers; 0: the row is read at every look.
+template <class T, int WAVES, int S>
 struct Row {
     static constexpr int kThreads = WAVES * 64;
+    static constexpr int kSegs = S ? S * WAVES : 1024;
     // keys of a type differ above this bit only
     static constexpr int kRes = sizeof(T) == 4 ? 0 : __is_same(T, bf16_t) ? 16 : 13;
-    Shared<WAVES> &sh;
+    Shared<WAVES, kSegs> &sh;
     const T *x;
-    int64_t V, steps;
+    int64_t V;
     int lane, wave;
     int per, segs; // steps of a segment, segments
-    double top, c; // the largest entry, log2 e / T
     int unit;      // the whole numbers that stand for w are w 2^unit
+    float top;     // the largest entry
+    double c;      // log2 e / T
+    float zero;    // entries from here down have a w of 0 (2^-1000, but for the rounding of this bound: 2^-600 at most)
+    typename Vec8<T>::type raw[S ? S : 1];
+    float largest[S ? S : 1]; // of each eight
 
-    // f(first column of this lane's eight, their values) for every step of a segment, done(segment) after them
-    template <class F, class D>
-    __device__ __forceinline__ void scan(F f, D done)
+    // first column of this lane's eight
+    __device__ __forceinline__ int64_t column(int seg, int q) const { return (int64_t(seg) * per + q) * kStepCols + lane * kVec; }
+    __device__ __forceinline__ void read()
     {
-        for (int seg = wave; seg < segs; seg += WAVES) {
-            for (int q = 0; q < per; ++q) {
-                const int64_t col = (int64_t(seg) * per + q) * kStepCols + lane * kVec;
-                float v[8];
-                load8(x + col, V - col, v, -__builtin_inff());
-                f(v);
+        if constexpr (S > 0) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const int64_t col = column(s * WAVES + wave, 0);
+                raw[s] = load8_raw(x + col, V - col, T(-__builtin_inff()));
             }
-            done(seg);
         }
     }
-    __device__ __forceinline__ double weight(float v) const { return exp2_64((double(v) - top) * c); }
+    // What is worked out of a row's eights at one look is not kept for the next (the
+    // compiler would, in memory).
+    __device__ __forceinline__ void forget(typename Vec8<T>::type &r)
+    {
+        typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * 2)));
+        words w = __builtin_bit_cast(words, r);
+        asm volatile("" : "+v"(w));
+        r = __builtin_bit_cast(typename Vec8<T>::type, w);
+    }
+    // f(eight's number s, first column, eight values) for every eight of this lane, done(segment) at a segment's
+    // end.  With `bound` eights are left out where all of a wave's are below.
+    template <class F, class D>
+    __device__ __forceinline__ void scan(float bound, F f, D done)
+    {
+        if constexpr (S > 0) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const int seg = s * WAVES + wave;
+                if (__ballot(largest[s] >= bound)) {
+                    float v[8];
+                    forget(raw[s]);
+                    widen<T>(raw[s], v);
+                    f(s, column(seg, 0), v);
+                }
+                done(seg);
+            }
+        } else {
+            for (int seg = wave; seg < segs; seg += WAVES) {
+                for (int q = 0; q < per; ++q) {
+                    const int64_t col = column(seg, q);
+                    float v[8], most;
+                    load8(x + col, V - col, v, -__builtin_inff());
+                    most = v[0];
+#pragma unroll
+                    for (int i = 1; i < kVec; ++i) most = fmaxf(most, v[i]);
+                    if (__ballot(most >= bound)) f(0, col, v);
+                }
+                done(seg);
+            }
+        }
+    }
+    // entries from `zero` up
+    __device__ __forceinline__ double weight(float v) const { return exp2_64((double(v) - double(top)) * c); }
 
     __device__ __forceinline__ uint32_t block_add(uint32_t v)
     {
@@ -130,26 +211,17 @@ struct Row {
         if (lane == 0) sh.wcount[wave] = v;
         __syncthreads();
         uint32_t s = 0;
+#pragma unroll
         for (int i = 0; i < WAVES; ++i) s += sh.wcount[i];
         return s;
     }
-    __device__ __forceinline__ uint32_t block_umax(uint32_t v)
-    {
-        v = wave_umax(v);
-        __syncthreads();
-        if (lane == 0) sh.wcount[wave] = v;
-        __syncthreads();
-        uint32_t s = 0;
-        for (int i = 0; i < WAVES; ++i) s = umax(s, sh.wcount[i]);
-        return s;
-    }
 
-    __device__ __forceinline__ void clear_bins()
+    __device__ __forceinline__ void clear_bins(bool masses)
     {
         __syncthreads();
         for (int b = threadIdx.x; b < kBins; b += kThreads) {
             sh.count[b] = 0;
-            sh.mass[b] = 0;
+            if (masses) sh.mass[b] = 0;
         }
         if (threadIdx.x == 0) sh.at = kBins;
         __syncthreads();
@@ -178,13 +250,8 @@ struct Row {
             before += n[q];
             before_mass += m[q];
         }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(before, d);
-            const double om = __shfl_up(before_mass, d);
-            before += lane >= d ? o : 0u;
-            before_mass += lane >= d ? om : 0.0;
-        }
+        before = scan_up(before, lane);
+        if (by_mass) before_mass = scan_up(before_mass, lane);
         if (lane == 63) {
             sh.wcount[wave] = before;
             sh.wsum[wave] = before_mass;
@@ -229,16 +296,18 @@ struct Row {
     // what holds where rounding lets no sum reach the target.
     __device__ __forceinline__ Cut select(bool by_mass, uint32_t target, double target_mass, uint32_t lo, Cut none)
     {
-        uint32_t hi = key_of(float(top)), above = 0;
+        uint32_t hi = key_of(top), above = 0;
         double above_mass = 0.0;
         for (;;) {
             lo = lo >> kRes << kRes;
             int shift = kRes;
             while (((hi - lo) >> shift) >= uint32_t(kBins)) ++shift;
             const bool one = shift == kRes, add = by_mass && !one;
-            clear_bins();
+            clear_bins(add);
+            const float bound = value_of(umax(lo, kNoneKey + 1));
             scan(
-                [&](const float *v) {
+                bound,
+                [&](int, int64_t, const float *v) {
 #pragma unroll
                     for (int i = 0; i < kVec; ++i) {
                         const uint32_t k = key_of(v[i]);
@@ -281,31 +350,36 @@ struct Row {
     // then the segment in which the sum passes u times the row's (sh.draw).
     __device__ __forceinline__ void sums(const Cut &cut, double u)
     {
-        const float least = value_of(cut.key);
+        const float least = value_of(cut.key), from = fmaxf(least, zero);
         double s = 0.0;
         uint32_t e = 0;
+        bool some = false;
         __syncthreads();
         scan(
-            [&](const float *v) {
-                bool any = false;
+            cut.ties ? least : from,
+            [&](int, int64_t, const float *v) {
+                some = true;
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) any = any || v[i] >= least;
-                if (!__ballot(any)) return;
+                for (int i = 0; i < kVec; ++i) s += v[i] > from ? weight(v[i]) : 0.0;
+                if (cut.ties) {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    s += v[i] > least ? weight(v[i]) : 0.0;
-                    e += v[i] == least ? 1u : 0u;
+                    for (int i = 0; i < kVec; ++i) e += v[i] == least ? 1u : 0u;
                 }
             },
             [&](int seg) {
-                const double all = wave_sum64(s);
-                const uint32_t tied = wave_add(e);
+                double all = 0.0;
+                uint32_t tied = 0;
+                if (some) {
+                    all = wave_sum64(s);
+                    if (cut.ties) tied = wave_add(e);
+                }
                 if (lane == 0) {
                     sh.sum[seg] = all;
                     sh.tied[seg] = tied;
                 }
                 s = 0.0;
                 e = 0;
+                some = false;
             });
         __syncthreads();
         if (wave == 0) {
@@ -313,25 +387,14 @@ struct Row {
             const int each = (segs + 63) / 64, j0 = lane * each, j1 = j0 + each < segs ? j0 + each : segs;
             uint32_t tied = 0;
             for (int j = j0; j < j1; ++j) tied += sh.tied[j];
-            uint32_t before = tied;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t o = __shfl_up(before, d);
-                before += lane >= d ? o : 0u;
-            }
-            before -= tied;
+            uint32_t before = scan_up(tied, lane) - tied;
             const uint32_t first_tied = before;
             double mass = 0.0;
             for (int j = j0; j < j1; ++j) {
                 mass += sh.sum[j] + double(stay(sh.tied[j], before, cut.ties)) * wc;
                 before += sh.tied[j];
             }
-            double after = mass;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double o = __shfl_up(after, d);
-                after += lane >= d ? o : 0.0;
-            }
+            const double after = scan_up(mass, lane);
             const double up = __shfl_up(after, 1), total = __shfl(after, 63), target = u * total;
             double at = lane ? up : 0.0;
             // the first lane whose segments pass the target; where rounding lets none, the last that has a token
@@ -368,7 +431,7 @@ struct Row {
         return tied < left ? tied : left;
     }
 
-    // The token within the segment of sh.draw; by one wave.
+    // The token within the segment of sh.draw; by the wave that has the segment.
     __device__ __forceinline__ void draw(const Cut &cut, int32_t *id, float *logp)
     {
         const float least = value_of(cut.key);
@@ -377,19 +440,22 @@ struct Row {
         uint32_t tied = sh.draw.tied;
         int64_t found = -1;
         double w_found = 0.0;
+        const int seg = __builtin_amdgcn_readfirstlane(int(sh.draw.seg));
+        typename Vec8<T>::type mine_raw;
+        if constexpr (S > 0) {
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (seg / WAVES == s) mine_raw = raw[s];
+        }
         for (int q = 0; q < per; ++q) {
-            const int64_t col = (int64_t(sh.draw.seg) * per + q) * kStepCols + lane * kVec;
+            const int64_t col = column(seg, q);
+            if constexpr (S == 0) mine_raw = load8_raw(x + col, V - col, T(-__builtin_inff()));
             float v[8];
-            load8(x + col, V - col, v, -__builtin_inff());
+            widen<T>(mine_raw, v);
             uint32_t e = 0;
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) e += v[i] == least && least > -__builtin_inff() ? 1u : 0u;
-            uint32_t before = e;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t o = __shfl_up(before, d);
-                before += lane >= d ? o : 0u;
-            }
+            for (int i = 0; i < kVec; ++i) e += cut.ties && v[i] == least ? 1u : 0u;
+            uint32_t before = scan_up(e, lane);
             const uint32_t step_tied = __shfl(before, 63);
             before += tied - e;
             tied += step_tied;
@@ -397,16 +463,11 @@ struct Row {
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
                 bool in = v[i] > least;
-                if (v[i] == least && least > -__builtin_inff()) in = before++ < cut.ties;
-                w[i] = in ? weight(v[i]) : 0.0;
+                if (cut.ties && v[i] == least) in = before++ < cut.ties;
+                w[i] = in && v[i] > zero ? weight(v[i]) : 0.0;
                 mine += w[i];
             }
-            double after = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double o = __shfl_up(after, d);
-                after += lane >= d ? o : 0.0;
-            }
+            const double after = scan_up(mine, lane);
             const double up = __shfl_up(after, 1), end = __shfl(after, 63);
             const uint64_t pass = __ballot(run + after > target && mine > 0.0), some = __ballot(mine > 0.0);
             if (some) { // without a lane that passes, the last token so far is the one if none follows
@@ -436,22 +497,161 @@ struct Row {
             if (logp) *logp = float(log(w_found / sh.draw.total));
         }
     }
+
+    // A key that at least `target` entries reach and not many more: the lower end of
+    // the bin of the target-th largest of the eights' largest.
+    __device__ __forceinline__ uint32_t bound_of(uint32_t target)
+    {
+        if constexpr (S == 0) return kNoneKey + 1;
+        float mine = -__builtin_inff();
+#pragma unroll
+        for (int s = 0; s < S; ++s) mine = fmaxf(mine, largest[s]);
+        // no lane's largest is below lo, so that the bins are as narrow as can be
+        uint32_t low = key_of(mine);
+        low = low <= kNoneKey ? ~0u : low;
+        low = ~wave_umax(~low);
+        __syncthreads();
+        if (lane == 0) sh.wleast[wave] = low;
+        clear_bins(false);
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) low = low < sh.wleast[i] ? low : sh.wleast[i];
+        const uint32_t lo = low >> kRes << kRes, hi = key_of(top);
+        int shift = kRes;
+        while (((hi - lo) >> shift) >= uint32_t(kBins)) ++shift;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const uint32_t k = key_of(largest[s]);
+            if (k >= lo && k > kNoneKey) atomicAdd(&sh.count[(k - lo) >> shift], 1u);
+        }
+        find_bin(false, target, 0.0, 0, 0.0, lo, false);
+        const uint32_t at = sh.at;
+        return at == kBins ? kNoneKey + 1 : umax(lo + ((kBins - 1 - at) << shift), kNoneKey + 1);
+    }
+
+    // top_k = K <= kFew: the whole rest of the row, if the entries that reach `bound` fit in the list.
+    __device__ __forceinline__ bool few(uint32_t K, uint32_t bound, double top_p, double min_p, double u, int32_t *id, float *logp, int32_t *kept)
+    {
+        __syncthreads();
+        if (threadIdx.x == 0) sh.listed = 0;
+        __syncthreads();
+        const float least = value_of(bound);
+        scan(
+            least,
+            [&](int, int64_t col, const float *v) {
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    if (v[i] >= least) {
+                        const uint32_t at = atomicAdd(&sh.listed, 1u);
+                        // descending: larger keys first, then smaller indices
+                        if (at < kList) sh.few.list[at] = uint64_t(key_of(v[i])) << 32 | uint32_t(~uint32_t(col + i));
+                    }
+                }
+            },
+            [](int) {});
+        __syncthreads();
+        const uint32_t L = sh.listed;
+        if (L > kList || L < K) return false; // uniform
+        for (uint32_t j = threadIdx.x; j < L; j += kThreads) {
+            const uint64_t mine = sh.few.list[j];
+            uint32_t rank = 0;
+            for (uint32_t i = 0; i < L; ++i) rank += sh.few.list[i] > mine ? 1u : 0u;
+            if (rank < kFew) sh.few.order[rank] = mine;
+        }
+        __syncthreads();
+        if (wave) return true;
+        constexpr int kEach = kFew / 64;
+        const uint32_t j0 = lane * kEach;
+        uint64_t e[kEach];
+        double w[kEach], mass = 0.0;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            const bool in = j0 + q < K;
+            e[q] = in ? sh.few.order[j0 + q] : 0;
+            const float v = value_of(uint32_t(e[q] >> 32));
+            w[q] = in && v > zero ? weight(v) : 0.0;
+            mass += w[q];
+        }
+        double at = scan_up(mass, lane);
+        const double all = __shfl(at, 63);
+        const double before = __shfl_up(at, 1);
+        at = lane ? before : 0.0;
+        uint32_t n_p = 0, n_q = 0;
+        const double target = top_p * all;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            at += w[q];
+            const bool in = j0 + q < K;
+            n_p += in && at < target ? 1u : 0u;
+            n_q += in && w[q] >= min_p ? 1u : 0u;
+        }
+        n_p = top_p < 1.0 ? wave_add(n_p) + 1u : K;
+        n_q = wave_add(n_q);
+        uint32_t n = n_p < n_q ? n_p : n_q;
+        n = n < K ? n : K;
+        // by index: a rank among the n, then sums in that order
+        uint32_t rank[kEach];
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) rank[q] = 0;
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t other = uint32_t(sh.few.order[i]); // ~index
+#pragma unroll
+            for (int q = 0; q < kEach; ++q) rank[q] += other > uint32_t(e[q]) ? 1u : 0u;
+        }
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            if (j0 + q < n) {
+                sh.few.w[rank[q]] = w[q];
+                sh.few.list[rank[q]] = e[q];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        mass = 0.0;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            w[q] = j0 + q < n ? sh.few.w[j0 + q] : 0.0;
+            mass += w[q];
+        }
+        const double after = scan_up(mass, lane), up = __shfl_up(after, 1), total = __shfl(after, 63), goal = u * total;
+        const uint64_t pass = __ballot(after > goal && mass > 0.0), some = __ballot(mass > 0.0);
+        const int who = pass ? __builtin_ctzll(pass) : 63 - __builtin_clzll(some);
+        at = lane ? up : 0.0;
+        uint32_t which = 0;
+        double w_which = 0.0;
+        bool over = false;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            at += w[q];
+            if (w[q] > 0.0 && !over) {
+                which = j0 + q;
+                w_which = w[q];
+                over = at > goal;
+            }
+        }
+        if (lane == who) {
+            *id = int32_t(~uint32_t(sh.few.list[which]));
+            if (logp) *logp = float(log(w_which / total));
+            if (kept) *kept = int32_t(n);
+        }
+        return true;
+    }
 };
 
 struct SampleArgs {
     gwtf_learn_sample_t a;
     int64_t row0;
-    int32_t steps, per, segs, unit;
+    int32_t per, segs, unit;
 };
 
-template <class T, int WAVES>
+template <class T, int WAVES, int S>
 __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
 {
-    __shared__ Shared<WAVES> sh;
+    using R = Row<T, WAVES, S>;
+    __shared__ Shared<WAVES, R::kSegs> sh;
     const gwtf_learn_sample_t &a = p.a;
     const int64_t i = p.row0 + blockIdx.x;
-    Row<T, WAVES> row{sh, static_cast<const T *>(a.logits) + i * a.logits_stride, a.vocab, p.steps, int(threadIdx.x & 63),
-                      __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p.per, p.segs, 0.0, 0.0, p.unit};
+    R row{sh, static_cast<const T *>(a.logits) + i * a.logits_stride, a.vocab, int(threadIdx.x & 63),
+          __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p.per, S ? R::kSegs : p.segs, p.unit};
+    row.read();
     const double T_ = a.temperatures ? double(a.temperatures[i]) : a.temperature;
     const double top_p = a.top_ps ? double(a.top_ps[i]) : a.top_p;
     const double min_p = a.min_ps ? double(a.min_ps[i]) : a.min_p;
@@ -463,19 +663,42 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
     float most = -__builtin_inff();
     uint32_t there = 0;
     bool bad = !(T_ >= 0.0 && T_ < __builtin_inf()) || !(top_p >= 0.0) || !(min_p >= 0.0 && min_p <= 1.0);
-    row.scan(
-        [&](const float *v) {
+    if constexpr (S > 0) {
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                bad = bad || !(v[k] < __builtin_inff());
-                most = fmaxf(most, v[k]);
-                there += v[k] > -__builtin_inff() ? 1u : 0u;
-            }
+        for (int s = 0; s < S; ++s) row.largest[s] = __builtin_inff(); // all are looked at
+    }
+    row.scan(
+        -__builtin_inff(),
+        [&](int s, int64_t, const float *v) {
+            float m = v[0];
+#pragma unroll
+            for (int k = 1; k < kVec; ++k) m = fmaxf(m, v[k]);
+#pragma unroll
+            for (int k = 0; k < kVec; k += 2) bad = bad || __builtin_isunordered(v[k], v[k + 1]);
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) there += v[k] > -__builtin_inff() ? 1u : 0u;
+            row.largest[s] = m;
+            most = fmaxf(most, m);
         },
         [](int) {});
-    row.top = double(value_of(row.block_umax(key_of(most))));
-    const uint32_t F = row.block_add(there);
-    const bool wrong = row.block_add(bad ? 1u : 0u) != 0;
+    {
+        const uint32_t key = wave_umax(key_of(most)), n = wave_add(there), wrong = __ballot(bad) != 0;
+        if (row.lane == 0) {
+            sh.wmost[row.wave] = key;
+            sh.wcount[row.wave] = n;
+            sh.wleast[row.wave] = wrong;
+        }
+    }
+    __syncthreads();
+    uint32_t key = 0, F = 0, wrong = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        key = umax(key, sh.wmost[w]);
+        F += sh.wcount[w];
+        wrong |= sh.wleast[w];
+    }
+    row.top = value_of(key);
+    wrong |= row.top == __builtin_inff();
     if (wrong || F == 0) {
         if (threadIdx.x == 0) {
             a.ids[i] = -1;
@@ -488,17 +711,23 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
     Cut cut = {kNoneKey, 0, F};
     bool summed = false;
     row.c = kLog2e64 / (T_ > 1e-300 ? T_ : 1e-300);
+    row.zero = fminf(float(double(row.top) - 1000.0 / row.c), value_of(key - 1));
     if (T_ == 0.0 || top_k == 1 || top_p == 0.0) {
-        cut = {key_of(float(row.top)), 1, 1};
+        cut = {key, 1, 1};
     } else {
-        if (top_k > 0 && uint32_t(top_k) < F) cut = row.select(false, uint32_t(top_k), 0.0, kNoneKey + 1, cut);
+        if (top_k > 0 && uint32_t(top_k) < F) {
+            const uint32_t lo = row.bound_of(uint32_t(top_k));
+            if (top_k <= kFew && row.few(uint32_t(top_k), lo, top_p, min_p, u, a.ids + i, a.logp ? a.logp + i : nullptr, a.kept ? a.kept + i : nullptr))
+                return;
+            cut = row.select(false, uint32_t(top_k), 0.0, lo, cut);
+        }
         if (top_p < 1.0) {
             row.sums(cut, u);
             summed = true;
             // The entry that the sum ends with and those after it are worth more than
             // (1 - p) of the sum: it is above that over their number.
             const double all = sh.draw.total, least = 0.99 * (1.0 - top_p) * all / double(cut.n);
-            const uint32_t k = key_of(float(row.top + log2(least) / row.c)), lo = k > kNoneKey + 3 ? k - 2 : kNoneKey + 1;
+            const uint32_t k = key_of(float(double(row.top) + log2(least) / row.c)), lo = k > kNoneKey + 3 ? k - 2 : kNoneKey + 1;
             const Cut by_mass = row.select(true, 0, top_p * all, lo, cut);
             if (by_mass.n < cut.n) {
                 cut = by_mass;
@@ -507,12 +736,13 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
         }
         if (min_p > 0.0) {
             // the smallest 32-bit number whose w reaches min_p
-            const double at = row.top + log2(min_p) / row.c;
+            const double at = double(row.top) + log2(min_p) / row.c;
             float least = float(at);
             if (double(least) < at) least = value_of(key_of(least) + 1);
             uint32_t n = 0;
             row.scan(
-                [&](const float *v) {
+                least,
+                [&](int, int64_t, const float *v) {
 #pragma unroll
                     for (int k = 0; k < kVec; ++k) n += v[k] >= least ? 1u : 0u;
                 },
@@ -525,30 +755,41 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
         }
     }
     if (!summed) row.sums(cut, u);
-    if (row.wave == 0) row.draw(cut, a.ids + i, a.logp ? a.logp + i : nullptr);
+    if (row.wave == int(sh.draw.seg % WAVES)) row.draw(cut, a.ids + i, a.logp ? a.logp + i : nullptr);
     if (threadIdx.x == 0 && a.kept) a.kept[i] = int32_t(cut.n);
 }
 
-template <class T>
+template <class T, int WAVES, int S>
 hipError_t run(const gwtf_learn_sample_t &a, hipStream_t s)
 {
     SampleArgs p;
     p.a = a;
-    p.steps = int32_t((a.vocab + kStepCols - 1) / kStepCols);
-    p.per = (p.steps + kSegs - 1) / kSegs;
-    p.segs = (p.steps + p.per - 1) / p.per;
+    const int64_t steps = (a.vocab + kStepCols - 1) / kStepCols, most = Row<T, WAVES, S>::kSegs;
+    p.per = int32_t((steps + most - 1) / most);
+    p.segs = int32_t((steps + p.per - 1) / p.per);
     p.unit = 62;
     while ((int64_t(1) << (62 - p.unit)) < a.vocab) --p.unit;
-    const bool wide = a.vocab > 16384;
-    const int threads = wide ? 1024 : 256;
-    const int64_t slab = kLaunchThreads / threads;
+    const int64_t slab = kLaunchThreads / (WAVES * 64);
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         p.row0 = r;
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
-        const hipError_t e = launch(wide ? sample_kernel<T, 16> : sample_kernel<T, 4>, n, threads, s, p);
+        const hipError_t e = launch(sample_kernel<T, WAVES, S>, n, WAVES * 64, s, p);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+template <class T>
+hipError_t by_width(const gwtf_learn_sample_t &a, hipStream_t s)
+{
+    const int64_t V = a.vocab;
+    if (V <= 2048) return run<T, 4, 1>(a, s);
+    if (V <= 8192) return run<T, 4, 4>(a, s);
+    if (V <= 32768) return run<T, 16, 4>(a, s);
+    if (V <= 65536) return run<T, 16, 8>(a, s);
+    if constexpr (sizeof(T) == 2)
+        if (V <= 131072) return run<T, 16, 16>(a, s);
+    return run<T, 16, 0>(a, s);
 }
 
 } // namespace
@@ -556,9 +797,9 @@ hipError_t run(const gwtf_learn_sample_t &a, hipStream_t s)
 hipError_t launch_sample(const gwtf_learn_sample_t &a, hipStream_t s)
 {
     switch (a.type) {
-    case GWTF_TYPE_F32: return run<float>(a, s);
-    case GWTF_TYPE_F16: return run<f16_t>(a, s);
-    default: return run<bf16_t>(a, s);
+    case GWTF_TYPE_F32: return by_width<float>(a, s);
+    case GWTF_TYPE_F16: return by_width<f16_t>(a, s);
+    default: return by_width<bf16_t>(a, s);
     }
 }
 
