@@ -39,11 +39,10 @@ __device__ __forceinline__ float value_of(uint32_t k)
     return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
 }
 
-// 2^y by the exponential's series in f ln 2, |f| <= 1/2, to about 1e-15.
-__device__ __forceinline__ double exp2_64(double y)
+// 2^y, 0 <= y < 1, by the exponential's series, to about 1e-15.
+__device__ __forceinline__ double exp2_series(double y)
 {
-    y = fmax(y, -1100.0);
-    const double n = rint(y), z = (y - n) * kLn264;
+    const double z = (y - 0.5) * kLn264;
     double s = 1.0 / 6227020800.0;
     s = fma(s, z, 1.0 / 479001600.0);
     s = fma(s, z, 1.0 / 39916800.0);
@@ -58,8 +57,19 @@ __device__ __forceinline__ double exp2_64(double y)
     s = fma(s, z, 0.5);
     s = fma(s, z, 1.0);
     s = fma(s, z, 1.0);
-    return ldexp(s, int(n));
+    return s * 1.4142135623730950488;
 }
+
+// The exponential between two entries of a table of 2^(j / kTable): the series up
+// to the fourth power, |f| <= 1 / 2, is off by 4e-14 at most.  The coefficients
+// come as arguments of the kernel, to be operands that are the same for all lanes
+// (as literals they cost two instructions each).
+constexpr int kTable = 64;
+struct Series {
+    double a1, a2, a3, a4;
+};
+constexpr double kZ = kLn264 / kTable;
+constexpr Series kSeries = {kZ, kZ * kZ / 2, kZ * kZ * kZ / 6, kZ * kZ * kZ * kZ / 24};
 
 __device__ __forceinline__ double wave_sum64(double v)
 {
@@ -105,6 +115,7 @@ constexpr int kList = 512; // entries that can be ranked
 // SEGS: segments of a row
 template <int WAVES, int SEGS>
 struct Shared {
+    double table[kTable]; // 2^(j / kTable)
     uint32_t count[kBins];
     union {
         uint64_t mass[kBins];
@@ -142,8 +153,9 @@ struct Row {
     int lane, wave;
     int per, segs; // steps of a segment, segments
     int unit;      // the whole numbers that stand for w are w 2^unit
-    float top;     // the largest entry
-    double c;      // log2 e / T
+    Series a;
+    float top; // the largest entry
+    double c;  // kTable log2 e / T
     float zero;    // entries from here down have a w of 0 (2^-1000, but for the rounding of this bound: 2^-600 at most)
     typename Vec8<T>::type raw[S ? S : 1];
     float largest[S ? S : 1]; // of each eight
@@ -201,8 +213,18 @@ struct Row {
             }
         }
     }
-    // entries from `zero` up
-    __device__ __forceinline__ double weight(float v) const { return exp2_64((double(v) - double(top)) * c); }
+    // Of entries above `zero`.
+    __device__ __forceinline__ double weight(float v) const
+    {
+        constexpr double kMagic = 0x1.8p52; // added, it leaves the nearest whole number in the low bits
+        const double y = (double(v) - double(top)) * c, k = y + kMagic, f = y - (k - kMagic);
+        const double r = fma(fma(fma(fma(f, a.a4, a.a3), f, a.a2), f, a.a1), f, 1.0);
+        const uint32_t n = uint32_t(__builtin_bit_cast(uint64_t, k));
+        const uint64_t t = __builtin_bit_cast(uint64_t, sh.table[n % kTable]);
+        const uint32_t high = uint32_t(t >> 32) + ((n & ~uint32_t(kTable - 1)) << 14); // n / kTable in units of the exponent
+        return __builtin_bit_cast(double, uint64_t(high) << 32 | uint32_t(t)) * r;
+    }
+    __device__ __forceinline__ double weight_or_0(float v) const { return v > zero ? weight(v) : 0.0; }
 
     __device__ __forceinline__ uint32_t block_add(uint32_t v)
     {
@@ -246,7 +268,7 @@ struct Row {
             const int b = kBins - 1 - (int(threadIdx.x) * kEach + q);
             n[q] = sh.count[b];
             m[q] = 0.0;
-            if (by_mass && n[q]) m[q] = one ? double(n[q]) * weight(value_of(bin_key(lo, b))) : ldexp(double(sh.mass[b]), -unit);
+            if (by_mass && n[q]) m[q] = one ? double(n[q]) * weight_or_0(value_of(bin_key(lo, b))) : ldexp(double(sh.mass[b]), -unit);
             before += n[q];
             before_mass += m[q];
         }
@@ -315,7 +337,7 @@ struct Row {
                         const uint32_t b = (k - lo) >> shift;
                         atomicAdd(&sh.count[b], 1u);
                         if (add)
-                            atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[b]), (unsigned long long)(ldexp(weight(v[i]), unit)));
+                            atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[b]), (unsigned long long)(ldexp(weight_or_0(v[i]), unit)));
                     }
                 },
                 [](int) {});
@@ -328,8 +350,8 @@ struct Row {
                 Cut cut;
                 cut.key = bin_key(lo, b);
                 if (by_mass) {
-                    const double w = weight(value_of(cut.key)), most = double(sh.bin.count);
-                    double t = fmin(fmax(ceil((target_mass - above_mass) / w), 1.0), most);
+                    const double w = weight_or_0(value_of(cut.key)), most = double(sh.bin.count);
+                    double t = w > 0.0 ? fmin(fmax(ceil((target_mass - above_mass) / w), 1.0), most) : 1.0;
                     // the division may be off by its last bit
                     if (t > 1.0 && above_mass + (t - 1.0) * w >= target_mass) t -= 1.0;
                     if (t < most && above_mass + t * w < target_mass) t += 1.0;
@@ -383,7 +405,7 @@ struct Row {
             });
         __syncthreads();
         if (wave == 0) {
-            const double wc = cut.ties ? weight(least) : 0.0;
+            const double wc = cut.ties ? weight_or_0(least) : 0.0;
             const int each = (segs + 63) / 64, j0 = lane * each, j1 = j0 + each < segs ? j0 + each : segs;
             uint32_t tied = 0;
             for (int j = j0; j < j1; ++j) tied += sh.tied[j];
@@ -640,6 +662,7 @@ struct SampleArgs {
     gwtf_learn_sample_t a;
     int64_t row0;
     int32_t per, segs, unit;
+    Series series;
 };
 
 template <class T, int WAVES, int S>
@@ -650,8 +673,9 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
     const gwtf_learn_sample_t &a = p.a;
     const int64_t i = p.row0 + blockIdx.x;
     R row{sh, static_cast<const T *>(a.logits) + i * a.logits_stride, a.vocab, int(threadIdx.x & 63),
-          __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p.per, S ? R::kSegs : p.segs, p.unit};
+          __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p.per, S ? R::kSegs : p.segs, p.unit, p.series};
     row.read();
+    if (threadIdx.x < kTable) sh.table[threadIdx.x] = threadIdx.x ? exp2_series(double(threadIdx.x) / kTable) : 1.0;
     const double T_ = a.temperatures ? double(a.temperatures[i]) : a.temperature;
     const double top_p = a.top_ps ? double(a.top_ps[i]) : a.top_p;
     const double min_p = a.min_ps ? double(a.min_ps[i]) : a.min_p;
@@ -676,13 +700,13 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
 #pragma unroll
             for (int k = 0; k < kVec; k += 2) bad = bad || __builtin_isunordered(v[k], v[k + 1]);
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) there += v[k] > -__builtin_inff() ? 1u : 0u;
+            for (int k = 0; k < kVec; ++k) there += __popcll(__ballot(v[k] > -__builtin_inff()));
             row.largest[s] = m;
             most = fmaxf(most, m);
         },
         [](int) {});
     {
-        const uint32_t key = wave_umax(key_of(most)), n = wave_add(there), wrong = __ballot(bad) != 0;
+        const uint32_t key = wave_umax(key_of(most)), n = there, wrong = __ballot(bad) != 0;
         if (row.lane == 0) {
             sh.wmost[row.wave] = key;
             sh.wcount[row.wave] = n;
@@ -710,8 +734,8 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
 
     Cut cut = {kNoneKey, 0, F};
     bool summed = false;
-    row.c = kLog2e64 / (T_ > 1e-300 ? T_ : 1e-300);
-    row.zero = fminf(float(double(row.top) - 1000.0 / row.c), value_of(key - 1));
+    row.c = kTable * kLog2e64 / (T_ > 1e-300 ? T_ : 1e-300);
+    row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), value_of(key - 1));
     if (T_ == 0.0 || top_k == 1 || top_p == 0.0) {
         cut = {key, 1, 1};
     } else {
@@ -727,7 +751,7 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
             // The entry that the sum ends with and those after it are worth more than
             // (1 - p) of the sum: it is above that over their number.
             const double all = sh.draw.total, least = 0.99 * (1.0 - top_p) * all / double(cut.n);
-            const uint32_t k = key_of(float(double(row.top) + log2(least) / row.c)), lo = k > kNoneKey + 3 ? k - 2 : kNoneKey + 1;
+            const uint32_t k = key_of(float(double(row.top) + kTable * log2(least) / row.c)), lo = k > kNoneKey + 3 ? k - 2 : kNoneKey + 1;
             const Cut by_mass = row.select(true, 0, top_p * all, lo, cut);
             if (by_mass.n < cut.n) {
                 cut = by_mass;
@@ -736,7 +760,7 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
         }
         if (min_p > 0.0) {
             // the smallest 32-bit number whose w reaches min_p
-            const double at = double(row.top) + log2(min_p) / row.c;
+            const double at = double(row.top) + kTable * log2(min_p) / row.c;
             float least = float(at);
             if (double(least) < at) least = value_of(key_of(least) + 1);
             uint32_t n = 0;
@@ -764,6 +788,7 @@ hipError_t run(const gwtf_learn_sample_t &a, hipStream_t s)
 {
     SampleArgs p;
     p.a = a;
+    p.series = kSeries;
     const int64_t steps = (a.vocab + kStepCols - 1) / kStepCols, most = Row<T, WAVES, S>::kSegs;
     p.per = int32_t((steps + most - 1) / most);
     p.segs = int32_t((steps + p.per - 1) / p.per);
