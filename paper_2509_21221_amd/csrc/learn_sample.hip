@@ -67,15 +67,40 @@ __device__ __forceinline__ double exp2_series(double y)
 constexpr int kTable = 64;
 struct Series {
     double a1, a2, a3, a4;
+    double magic; // added to a number, it leaves the nearest whole one in the low bits
 };
 constexpr double kZ = kLn264 / kTable;
-constexpr Series kSeries = {kZ, kZ * kZ / 2, kZ * kZ * kZ / 6, kZ * kZ * kZ * kZ / 24};
+constexpr Series kSeries = {kZ, kZ * kZ / 2, kZ * kZ * kZ / 6, kZ * kZ * kZ * kZ / 24, 0x1.8p52};
 
+// Sums over the wave, uniform, without a way through LDS.
+template <int n>
+__device__ __forceinline__ double row_ror64(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = uint32_t(row_ror<n>(int(uint32_t(b)))), hi = uint32_t(row_ror<n>(int(uint32_t(b >> 32))));
+    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+__device__ __forceinline__ double lane_value64(double v, int lane)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane(uint32_t(b), lane), hi = __builtin_amdgcn_readlane(uint32_t(b >> 32), lane);
+    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum64(double v)
 {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+    v += row_ror64<8>(v);
+    v += row_ror64<4>(v);
+    v += row_ror64<2>(v);
+    v += row_ror64<1>(v);
+    return (lane_value64(v, 0) + lane_value64(v, 16)) + (lane_value64(v, 32) + lane_value64(v, 48));
+}
+__device__ __forceinline__ uint32_t wave_add(uint32_t v)
+{
+    v += uint32_t(row_ror<8>(int(v)));
+    v += uint32_t(row_ror<4>(int(v)));
+    v += uint32_t(row_ror<2>(int(v)));
+    v += uint32_t(row_ror<1>(int(v)));
+    return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) + (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
 }
 __device__ __forceinline__ uint32_t scan_up(uint32_t v, int lane) // sums over lanes 0 .. lane
 {
@@ -95,13 +120,6 @@ __device__ __forceinline__ double scan_up(double v, int lane)
     }
     return v;
 }
-__device__ __forceinline__ uint32_t wave_add(uint32_t v)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
-
 // Entries of the order that stay: those with larger keys, and `ties` with this
 // one, by ascending index; n of them in all.
 struct Cut {
@@ -216,13 +234,24 @@ struct Row {
     // Of entries above `zero`.
     __device__ __forceinline__ double weight(float v) const
     {
-        constexpr double kMagic = 0x1.8p52; // added, it leaves the nearest whole number in the low bits
-        const double y = (double(v) - double(top)) * c, k = y + kMagic, f = y - (k - kMagic);
-        const double r = fma(fma(fma(fma(f, a.a4, a.a3), f, a.a2), f, a.a1), f, 1.0);
-        const uint32_t n = uint32_t(__builtin_bit_cast(uint64_t, k));
+        const double d = double(v) - double(top), k = fma(d, c, a.magic), f = fma(d, c, a.magic - k);
+        const uint32_t n = uint32_t(__builtin_bit_cast(uint64_t, k)); // the nearest whole number to d c
         const uint64_t t = __builtin_bit_cast(uint64_t, sh.table[n % kTable]);
-        const uint32_t high = uint32_t(t >> 32) + ((n & ~uint32_t(kTable - 1)) << 14); // n / kTable in units of the exponent
+        const double r = fma(fma(fma(fma(f, a.a4, a.a3), f, a.a2), f, a.a1), f, 1.0);
+        uint32_t high = uint32_t(t >> 32) + ((n & ~uint32_t(kTable - 1)) << 14); // n / kTable in units of the exponent
+        asm volatile("" : "+v"(high)); // else the sum is a 64-bit one
         return __builtin_bit_cast(double, uint64_t(high) << 32 | uint32_t(t)) * r;
+    }
+    // w, or 0 for what is not above `from`; all eight are worked out, side by side.
+    __device__ __forceinline__ void weights(const float v[8], float from, double w[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) w[i] = weight(v[i]);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            asm volatile("" : "+v"(w[i])); // else each becomes a branch, with a wait for its own table entry
+            w[i] = v[i] > from ? w[i] : 0.0;
+        }
     }
     __device__ __forceinline__ double weight_or_0(float v) const { return v > zero ? weight(v) : 0.0; }
 
@@ -381,8 +410,9 @@ struct Row {
             cut.ties ? least : from,
             [&](int, int64_t, const float *v) {
                 some = true;
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) s += v[i] > from ? weight(v[i]) : 0.0;
+                double w[8];
+                weights(v, from, w);
+                s += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
                 if (cut.ties) {
 #pragma unroll
                     for (int i = 0; i < kVec; ++i) e += v[i] == least ? 1u : 0u;
