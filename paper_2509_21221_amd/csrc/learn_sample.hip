@@ -127,19 +127,20 @@ struct Cut {
 };
 
 constexpr int kBins = 2048;
+constexpr int kAhead = 4;  // steps that a wave has in flight
 constexpr int kFew = 256;  // top_k up to which the entries are ranked
 constexpr int kList = 512; // entries that can be ranked
 
-// SEGS: segments of a row
-template <int WAVES, int SEGS>
+// SEGS: segments of a row; BINS: kBins, or 1 where nothing is counted or listed.
+template <int WAVES, int SEGS, int BINS>
 struct Shared {
     double table[kTable]; // 2^(j / kTable)
-    uint32_t count[kBins];
+    uint32_t count[BINS];
     union {
-        uint64_t mass[kBins];
+        uint64_t mass[BINS];
         struct {
-            uint64_t list[kList], order[kList];
-            double w[kFew];
+            uint64_t list[BINS > 1 ? kList : 1], order[BINS > 1 ? kFew : 1];
+            double w[BINS > 1 ? kFew : 1];
         } few;
     };
     double sum[SEGS];    // of a segment's w whose keys are above the cut's
@@ -156,16 +157,17 @@ struct Shared {
         uint32_t seg, tied;
         double total, before, target;
     } draw;
+    bool certain;
 };
 
 // S: eights that a lane keeps in registers; 0: the row is read at every look.
-template <class T, int WAVES, int S>
+template <class T, int WAVES, int S, int BINS = kBins>
 struct Row {
     static constexpr int kThreads = WAVES * 64;
     static constexpr int kSegs = S ? S * WAVES : 1024;
     // keys of a type differ above this bit only
     static constexpr int kRes = sizeof(T) == 4 ? 0 : __is_same(T, bf16_t) ? 16 : 13;
-    Shared<WAVES, kSegs> &sh;
+    Shared<WAVES, kSegs, BINS> &sh;
     const T *x;
     int64_t V;
     int lane, wave;
@@ -217,17 +219,39 @@ struct Row {
                 done(seg);
             }
         } else {
-            for (int seg = wave; seg < segs; seg += WAVES) {
-                for (int q = 0; q < per; ++q) {
+            // steps of this wave's segments, kAhead of them in flight
+            const int mine = wave < segs ? (segs - wave + WAVES - 1) / WAVES : 0;
+            const int64_t all = int64_t(mine) * per;
+            int seg = wave, q = 0, next_seg = wave, next_q = 0;
+            typename Vec8<T>::type next[kAhead];
+            auto fetch = [&](int slot) {
+                const int64_t col = column(next_seg, next_q);
+                next[slot] = load8_raw(x + col, next_seg < segs ? V - col : 0, T(-__builtin_inff()));
+                if (++next_q == per) {
+                    next_q = 0;
+                    next_seg += WAVES;
+                }
+            };
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) fetch(k);
+            for (int64_t n = 0; n < all; n += kAhead) {
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    if (n + k >= all) break; // uniform
                     const int64_t col = column(seg, q);
                     float v[8], most;
-                    load8(x + col, V - col, v, -__builtin_inff());
+                    widen<T>(next[k], v);
+                    fetch(k);
                     most = v[0];
 #pragma unroll
                     for (int i = 1; i < kVec; ++i) most = fmaxf(most, v[i]);
                     if (__ballot(most >= bound)) f(0, col, v);
+                    if (++q == per) {
+                        done(seg);
+                        q = 0;
+                        seg += WAVES;
+                    }
                 }
-                done(seg);
             }
         }
     }
@@ -434,47 +458,50 @@ struct Row {
                 some = false;
             });
         __syncthreads();
-        if (wave == 0) {
-            const double wc = cut.ties ? weight_or_0(least) : 0.0;
-            const int each = (segs + 63) / 64, j0 = lane * each, j1 = j0 + each < segs ? j0 + each : segs;
-            uint32_t tied = 0;
-            for (int j = j0; j < j1; ++j) tied += sh.tied[j];
-            uint32_t before = scan_up(tied, lane) - tied;
-            const uint32_t first_tied = before;
-            double mass = 0.0;
+        if (wave == 0) pick(cut, u);
+        __syncthreads();
+    }
+    // The segment in which the sum over the segments passes u times the row's; by one wave.
+    __device__ __forceinline__ void pick(const Cut &cut, double u)
+    {
+        const double wc = cut.ties ? weight_or_0(value_of(cut.key)) : 0.0;
+        const int each = (segs + 63) / 64, j0 = lane * each, j1 = j0 + each < segs ? j0 + each : segs;
+        uint32_t tied = 0;
+        for (int j = j0; j < j1; ++j) tied += sh.tied[j];
+        uint32_t before = scan_up(tied, lane) - tied;
+        const uint32_t first_tied = before;
+        double mass = 0.0;
+        for (int j = j0; j < j1; ++j) {
+            mass += sh.sum[j] + double(stay(sh.tied[j], before, cut.ties)) * wc;
+            before += sh.tied[j];
+        }
+        const double after = scan_up(mass, lane);
+        const double up = __shfl_up(after, 1), total = __shfl(after, 63), target = u * total;
+        double at = lane ? up : 0.0;
+        // the first lane whose segments pass the target; where rounding lets none, the last that has a token
+        const uint64_t pass = __ballot(after > target && mass > 0.0), some = __ballot(mass > 0.0);
+        const int who = pass ? __builtin_ctzll(pass) : 63 - __builtin_clzll(some ? some : 1ull);
+        if (lane == who) {
+            uint32_t seg = uint32_t(j0), seg_tied = first_tied;
+            double seg_at = at;
+            before = first_tied;
             for (int j = j0; j < j1; ++j) {
-                mass += sh.sum[j] + double(stay(sh.tied[j], before, cut.ties)) * wc;
+                const double add = sh.sum[j] + double(stay(sh.tied[j], before, cut.ties)) * wc;
+                if (add > 0.0) {
+                    seg = uint32_t(j);
+                    seg_tied = before;
+                    seg_at = at;
+                    if (at + add > target) break;
+                }
+                at += add;
                 before += sh.tied[j];
             }
-            const double after = scan_up(mass, lane);
-            const double up = __shfl_up(after, 1), total = __shfl(after, 63), target = u * total;
-            double at = lane ? up : 0.0;
-            // the first lane whose segments pass the target; where rounding lets none, the last that has a token
-            const uint64_t pass = __ballot(after > target && mass > 0.0), some = __ballot(mass > 0.0);
-            const int who = pass ? __builtin_ctzll(pass) : 63 - __builtin_clzll(some ? some : 1ull);
-            if (lane == who) {
-                uint32_t seg = uint32_t(j0), seg_tied = first_tied;
-                double seg_at = at;
-                before = first_tied;
-                for (int j = j0; j < j1; ++j) {
-                    const double add = sh.sum[j] + double(stay(sh.tied[j], before, cut.ties)) * wc;
-                    if (add > 0.0) {
-                        seg = uint32_t(j);
-                        seg_tied = before;
-                        seg_at = at;
-                        if (at + add > target) break;
-                    }
-                    at += add;
-                    before += sh.tied[j];
-                }
-                sh.draw.seg = seg;
-                sh.draw.tied = seg_tied;
-                sh.draw.before = seg_at;
-                sh.draw.target = target;
-                sh.draw.total = total;
-            }
+            sh.draw.seg = seg;
+            sh.draw.tied = seg_tied;
+            sh.draw.before = seg_at;
+            sh.draw.target = target;
+            sh.draw.total = total;
         }
-        __syncthreads();
     }
     // How many of `tied` entries stay, with `before` of them before.
     static __device__ __forceinline__ uint32_t stay(uint32_t tied, uint32_t before, uint32_t ties)
@@ -484,8 +511,11 @@ struct Row {
     }
 
     // The token within the segment of sh.draw; by the wave that has the segment.
-    __device__ __forceinline__ void draw(const Cut &cut, int32_t *id, float *logp)
+    // Returns how far the target is from the sums before and after the token (infinitely
+    // far from a sum of nothing), 0 where rounding let none pass it.
+    __device__ __forceinline__ double draw(const Cut &cut, int32_t *id, float *logp)
     {
+        double gap = 0.0;
         const float least = value_of(cut.key);
         const double target = sh.draw.target;
         double run = sh.draw.before;
@@ -535,9 +565,14 @@ struct Row {
                         over = at > target;
                     }
                 }
-                double w_which = 0.0;
+                double w_which = 0.0, after_which = run + (lane ? up : 0.0);
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) w_which = i == which ? w[i] : w_which;
+                for (int i = 0; i < kVec; ++i) {
+                    after_which += i <= which ? w[i] : 0.0;
+                    w_which = i == which ? w[i] : w_which;
+                }
+                const double over_by = after_which - target, left = after_which - w_which;
+                gap = __shfl(fmin(over_by, left > 0.0 ? target - left : over_by), who);
                 found = __shfl(col + which, who);
                 w_found = __shfl(w_which, who);
             }
@@ -548,6 +583,7 @@ struct Row {
             *id = int32_t(found);
             if (logp) *logp = float(log(w_found / sh.draw.total));
         }
+        return gap;
     }
 
     // A key that at least `target` entries reach and not many more: the lower end of
@@ -699,7 +735,7 @@ template <class T, int WAVES, int S>
 __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
 {
     using R = Row<T, WAVES, S>;
-    __shared__ Shared<WAVES, R::kSegs> sh;
+    __shared__ Shared<WAVES, R::kSegs, kBins> sh;
     const gwtf_learn_sample_t &a = p.a;
     const int64_t i = p.row0 + blockIdx.x;
     R row{sh, static_cast<const T *>(a.logits) + i * a.logits_stride, a.vocab, int(threadIdx.x & 63),
@@ -813,6 +849,152 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
     if (threadIdx.x == 0 && a.kept) a.kept[i] = int32_t(cut.n);
 }
 
+// The largest and the least of eight numbers.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float r;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// Rows of which everything stays (no top_k, top_p or min_p): one reading, with the
+// sums of segments in 32 bits under a reference R that is an entry of the segment's
+// wave, at most kAbove bits below any of the segment's; then the one segment that the
+// target falls into in 64 bits.
+//
+// The token is that of 64-bit sums if the target is further from the borders of
+// the token than the 32-bit sums can be off.  With A the sum up to a border, B the sum
+// after it and W = A + B, the border lies at (1 - u) A - u B from the target.  Of
+// A's terms w = 2^y each is off by its y's two roundings (of x - R and of the
+// product with log2 e / T, which is held in two parts), the exponential's 2^-23 and
+// the nine additions': 2^-24 (2 ln 2 |y| + 11) relatively.  |y| is at most kAbove +
+// |log2 w|, and the mean of -log2 w under the shares w / A is their entropy less log2
+// A, log2 V - log2 A at most.  So A is off by at most A 2^-24 (2 ln 2 (log2 V - log2 A +
+// kAbove) + 11), B likewise, and near a border A = u W, B = (1 - u) W.
+// Otherwise (one row in fifteen of normal logits of deviation 2.5 and 131,072 columns) the
+// sums are taken again in 64 bits.
+constexpr float kAbove = 4.f;
+constexpr int64_t kOpenMost = 1024 * kStepCols; // columns
+
+template <class T, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void sample_open_kernel(SampleArgs p)
+{
+    using R = Row<T, WAVES, 0, 1>;
+    __shared__ Shared<WAVES, R::kSegs, 1> sh;
+    __shared__ float ref[R::kSegs];
+    const gwtf_learn_sample_t &a = p.a;
+    const int64_t i = p.row0 + blockIdx.x;
+    R row{sh, static_cast<const T *>(a.logits) + i * a.logits_stride, a.vocab, int(threadIdx.x & 63),
+          __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 1, p.segs, p.unit, p.series};
+    const int each = (p.segs + WAVES - 1) / WAVES, first = row.wave * each;
+    const int end = first + each < p.segs ? first + each : p.segs;
+    const int64_t at = int64_t(first) * kStepCols + row.lane * kVec;
+    typename Vec8<T>::type raw[kAhead];
+    auto fetch = [&](int seg, int slot) {
+        const int64_t col = at + int64_t(seg - first) * kStepCols;
+        raw[slot] = load8_raw(row.x + col, seg < end ? a.vocab - col : 0, T(-__builtin_inff()));
+    };
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) fetch(first + q, q);
+    if (threadIdx.x < kTable) sh.table[threadIdx.x] = threadIdx.x ? exp2_series(double(threadIdx.x) / kTable) : 1.0;
+    double u = a.uniform_type == GWTF_UNIFORM_F64 ? static_cast<const double *>(a.u)[i] : double(static_cast<const float *>(a.u)[i]);
+    u = u >= 0.0 ? u : 0.0;
+    row.c = kTable * kLog2e64 / a.temperature;
+    const double c = kLog2e64 / a.temperature;
+    // c in two parts, both above 0, so that a masked entry's y is -infinity
+    float ch = float(c);
+    if (double(ch) > c) ch = __uint_as_float(__float_as_uint(ch) - 1);
+    const float cl = fmaxf(float(c - double(ch)), 0x1p-126f), limit = kAbove / ch;
+
+    float most = -__builtin_inff(), reference = -0x1.fffffep127f;
+    uint32_t there = 0;
+    bool bad = false;
+    for (int seg = first; seg < end; seg += kAhead) {
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            if (seg + q >= end) break; // uniform
+            float v[8];
+            widen<T>(raw[q], v);
+            fetch(seg + q + kAhead, q);
+            const float m = max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), fmaxf(v[6], v[7]));
+            const float l = min3(min3(v[0], v[1], v[2]), min3(v[3], v[4], v[5]), fminf(v[6], v[7]));
+            most = fmaxf(most, m);
+            if (__ballot(m > reference + limit)) reference = wave_fmax(m);
+            if (__ballot(l == -__builtin_inff())) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) there += __popcll(__ballot(v[k] > -__builtin_inff()));
+            } else {
+                there += kStepCols;
+            }
+            float e[8];
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const float d = v[k] - reference;
+                e[k] = exp2_(fmaf(d, ch, d * cl));
+            }
+            const float s = wave_sum(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+            bad = bad || s != s; // a NaN, or +infinity less itself
+            if (row.lane == 0) {
+                sh.sum[seg + q] = double(s);
+                sh.tied[seg + q] = 0;
+                ref[seg + q] = reference;
+            }
+        }
+    }
+    {
+        const uint32_t key = wave_umax(key_of(most));
+        if (row.lane == 0) {
+            sh.wmost[row.wave] = key;
+            sh.wcount[row.wave] = there;
+            sh.wleast[row.wave] = bad;
+        }
+    }
+    __syncthreads();
+    uint32_t key = 0, F = 0, wrong = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        key = umax(key, sh.wmost[w]);
+        F += sh.wcount[w];
+        wrong |= sh.wleast[w];
+    }
+    row.top = value_of(key);
+    wrong |= row.top == __builtin_inff();
+    if (wrong || F == 0) {
+        if (threadIdx.x == 0) {
+            a.ids[i] = -1;
+            if (a.logp) a.logp[i] = wrong ? __builtin_nanf("") : -__builtin_inff();
+            if (a.kept) a.kept[i] = 0;
+        }
+        return;
+    }
+    row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), value_of(key - 1));
+    const Cut cut = {kNoneKey, 0, F};
+    if (threadIdx.x == 0 && a.kept) a.kept[i] = int32_t(F);
+    for (int seg = threadIdx.x; seg < p.segs; seg += WAVES * 64) sh.sum[seg] *= row.weight_or_0(ref[seg]);
+    __syncthreads();
+    if (row.wave == 0) {
+        row.pick(cut, u);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        const double gap = row.draw(cut, a.ids + i, a.logp ? a.logp + i : nullptr);
+        if (row.lane == 0) {
+            const double W = sh.draw.total, v = fmin(u, 1.0), A = v * W, B = W - A, span = log2(double(a.vocab)) + kAbove;
+            // (the sums in A and B are themselves off by their 1e-5th at most)
+            const double off_a = A > 0.0 ? 2 * kLn264 * (span - log2(A)) + 11 : 0.0, off_b = B > 0.0 ? 2 * kLn264 * (span - log2(B)) + 11 : 0.0;
+            sh.certain = gap > 0x1.02p-24 * (1.0 - v) * A * off_a + 0x1.02p-24 * v * B * off_b + 1e-13 * W;
+        }
+    }
+    __syncthreads();
+    if (sh.certain) return;
+    row.sums(cut, u);
+    if (row.wave == 0) row.draw(cut, a.ids + i, a.logp ? a.logp + i : nullptr);
+}
+
 template <class T, int WAVES, int S>
 hipError_t run(const gwtf_learn_sample_t &a, hipStream_t s)
 {
@@ -834,10 +1016,33 @@ hipError_t run(const gwtf_learn_sample_t &a, hipStream_t s)
     return hipSuccess;
 }
 
+template <class T, int WAVES>
+hipError_t run_open(const gwtf_learn_sample_t &a, hipStream_t s)
+{
+    SampleArgs p;
+    p.a = a;
+    p.series = kSeries;
+    p.per = 1;
+    p.segs = int32_t((a.vocab + kStepCols - 1) / kStepCols);
+    p.unit = 0;
+    const int64_t slab = kLaunchThreads / (WAVES * 64);
+    for (int64_t r = 0; r < a.num_tokens; r += slab) {
+        p.row0 = r;
+        const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
+        const hipError_t e = launch(sample_open_kernel<T, WAVES>, n, WAVES * 64, s, p);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <class T>
 hipError_t by_width(const gwtf_learn_sample_t &a, hipStream_t s)
 {
     const int64_t V = a.vocab;
+    // 32-bit sums need a temperature whose quotients stay within 32 bits
+    const bool open = !a.temperatures && !a.top_ks && !a.top_ps && !a.min_ps && a.top_k <= 0 && a.top_p >= 1.0 && a.min_p == 0.0 &&
+                      a.temperature > 1e-30 && a.temperature < 1e30;
+    if (open && V <= kOpenMost) return V > 16384 ? run_open<T, 16>(a, s) : run_open<T, 4>(a, s);
     if (V <= 2048) return run<T, 4, 1>(a, s);
     if (V <= 8192) return run<T, 4, 4>(a, s);
     if (V <= 32768) return run<T, 16, 4>(a, s);

@@ -45,8 +45,16 @@ def logits(n, v, dtype, seed, pad=0, offset=0, std=2.5):
     return x
 
 
+def open_error(v):
+    """Where nothing is filtered logp's sum W is of 32-bit terms: of a term 2^y two roundings of y, the exponential's
+    2^-23, nine of additions, so that with |y| <= 4 + |log2 w| and the mean of |log2 w| <= log2 V - log2 W <= log2 V
+    the sum, and with it the logarithm, is off by 2^-24 (2 ln 2 (log2 V + 4) + 11) at most."""
+    return 2.0 ** -24 * (2 * math.log(2) * (math.log2(v) + 4) + 11)
+
+
 def check_rows(ops, x, u, **kw):
     """ids and kept are the oracle's; logp is rounded once from 64 bits."""
+    free = not any(isinstance(v, np.ndarray) for v in kw.values()) and kw.get("top_k", 0) == 0 and kw.get("top_p", 1) >= 1 and kw.get("min_p", 0) == 0
     ids, logp, kept = ops.sample(x, u, **{k: dev(v) if isinstance(v, np.ndarray) else v for k, v in kw.items()})
     host, us = x.double().cpu().numpy(), u.double().cpu().numpy()
     for i in range(len(host)):
@@ -59,7 +67,7 @@ def check_rows(ops, x, u, **kw):
             assert got[1] == want[1] or (math.isnan(got[1]) and math.isnan(want[1])), what
         else:
             # sums, weights and the logarithm in 64 bits (1e-12 covers them amply), then one rounding
-            assert abs(got[1] - want[1]) <= HALF["f32"] * abs(want[1]) + 1e-12, what
+            assert abs(got[1] - want[1]) <= HALF["f32"] * abs(want[1]) + (open_error(host.shape[1]) if free else 1e-12), what
     return ids, logp, kept
 
 
