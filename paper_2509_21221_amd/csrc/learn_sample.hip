@@ -256,9 +256,13 @@ struct Row {
         }
     }
     // Of entries above `zero`.
-    __device__ __forceinline__ double weight(float v) const
+    __device__ __forceinline__ double weight(float v) const { return power(double(v) - double(top), c); }
+    // 2^y, -1020 < y < 1020.
+    __device__ __forceinline__ double power(double y) const { return power(y, kTable); }
+    // 2^(d c / kTable)
+    __device__ __forceinline__ double power(double d, double c) const
     {
-        const double d = double(v) - double(top), k = fma(d, c, a.magic), f = fma(d, c, a.magic - k);
+        const double k = fma(d, c, a.magic), f = fma(d, c, a.magic - k);
         const uint32_t n = uint32_t(__builtin_bit_cast(uint64_t, k)); // the nearest whole number to d c
         const uint64_t t = __builtin_bit_cast(uint64_t, sh.table[n % kTable]);
         const double r = fma(fma(fma(fma(f, a.a4, a.a3), f, a.a2), f, a.a1), f, 1.0);
@@ -466,15 +470,22 @@ struct Row {
     {
         const double wc = cut.ties ? weight_or_0(value_of(cut.key)) : 0.0;
         const int each = (segs + 63) / 64, j0 = lane * each, j1 = j0 + each < segs ? j0 + each : segs;
-        uint32_t tied = 0;
-        for (int j = j0; j < j1; ++j) tied += sh.tied[j];
-        uint32_t before = scan_up(tied, lane) - tied;
-        const uint32_t first_tied = before;
-        double mass = 0.0;
-        for (int j = j0; j < j1; ++j) {
-            mass += sh.sum[j] + double(stay(sh.tied[j], before, cut.ties)) * wc;
-            before += sh.tied[j];
+        uint32_t before = 0;
+        if (cut.ties) {
+            uint32_t tied = 0;
+            for (int j = j0; j < j1; ++j) tied += sh.tied[j];
+            before = scan_up(tied, lane) - tied;
         }
+        const uint32_t first_tied = before;
+        // what stays of a segment's tied entries counts too
+        auto mass_of = [&](int j) {
+            if (!cut.ties) return sh.sum[j];
+            const double m = sh.sum[j] + double(stay(sh.tied[j], before, cut.ties)) * wc;
+            before += sh.tied[j];
+            return m;
+        };
+        double mass = 0.0;
+        for (int j = j0; j < j1; ++j) mass += mass_of(j);
         const double after = scan_up(mass, lane);
         const double up = __shfl_up(after, 1), total = __shfl(after, 63), target = u * total;
         double at = lane ? up : 0.0;
@@ -486,15 +497,15 @@ struct Row {
             double seg_at = at;
             before = first_tied;
             for (int j = j0; j < j1; ++j) {
-                const double add = sh.sum[j] + double(stay(sh.tied[j], before, cut.ties)) * wc;
+                const uint32_t tied = before;
+                const double add = mass_of(j);
                 if (add > 0.0) {
                     seg = uint32_t(j);
-                    seg_tied = before;
+                    seg_tied = tied;
                     seg_at = at;
                     if (at + add > target) break;
                 }
                 at += add;
-                before += sh.tied[j];
             }
             sh.draw.seg = seg;
             sh.draw.tied = seg_tied;
@@ -511,11 +522,8 @@ struct Row {
     }
 
     // The token within the segment of sh.draw; by the wave that has the segment.
-    // Returns how far the target is from the sums before and after the token (infinitely
-    // far from a sum of nothing), 0 where rounding let none pass it.
-    __device__ __forceinline__ double draw(const Cut &cut, int32_t *id, float *logp)
+    __device__ __forceinline__ void draw(const Cut &cut, int32_t *id, float *logp)
     {
-        double gap = 0.0;
         const float least = value_of(cut.key);
         const double target = sh.draw.target;
         double run = sh.draw.before;
@@ -565,14 +573,9 @@ struct Row {
                         over = at > target;
                     }
                 }
-                double w_which = 0.0, after_which = run + (lane ? up : 0.0);
+                double w_which = 0.0;
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    after_which += i <= which ? w[i] : 0.0;
-                    w_which = i == which ? w[i] : w_which;
-                }
-                const double over_by = after_which - target, left = after_which - w_which;
-                gap = __shfl(fmin(over_by, left > 0.0 ? target - left : over_by), who);
+                for (int i = 0; i < kVec; ++i) w_which = i == which ? w[i] : w_which;
                 found = __shfl(col + which, who);
                 w_found = __shfl(w_which, who);
             }
@@ -583,7 +586,6 @@ struct Row {
             *id = int32_t(found);
             if (logp) *logp = float(log(w_found / sh.draw.total));
         }
-        return gap;
     }
 
     // A key that at least `target` entries reach and not many more: the lower end of
@@ -849,7 +851,6 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
     if (threadIdx.x == 0 && a.kept) a.kept[i] = int32_t(cut.n);
 }
 
-// The largest and the least of eight numbers.
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float r;
@@ -864,87 +865,156 @@ __device__ __forceinline__ float min3(float a, float b, float c)
 }
 
 // Rows of which everything stays (no top_k, top_p or min_p): one reading, with the
-// sums of segments in 32 bits under a reference R that is an entry of the segment's
-// wave, at most kAbove bits below any of the segment's; then the one segment that the
-// target falls into in 64 bits.
+// sums of segments in 32 bits, of 2^y, y = x c - r in one fused operation, c = log2 e /
+// T in 32 bits and r the product of c and the largest entry that the segment's wave has
+// met, or a little less: no y is above kAbove + 1.  Then the one segment that the target
+// falls into in 64 bits.
 //
 // The token is that of 64-bit sums if the target is further from the borders of
 // the token than the 32-bit sums can be off.  With A the sum up to a border, B the sum
 // after it and W = A + B, the border lies at (1 - u) A - u B from the target.  Of
-// A's terms w = 2^y each is off by its y's two roundings (of x - R and of the
-// product with log2 e / T, which is held in two parts), the exponential's 2^-23 and
-// the nine additions': 2^-24 (2 ln 2 |y| + 11) relatively.  |y| is at most kAbove +
-// |log2 w|, and the mean of -log2 w under the shares w / A is their entropy less log2
-// A, log2 V - log2 A at most.  So A is off by at most A 2^-24 (2 ln 2 (log2 V - log2 A +
-// kAbove) + 11), B likewise, and near a border A = u W, B = (1 - u) W.
-// Otherwise (one row in fifteen of normal logits of deviation 2.5 and 131,072 columns) the
-// sums are taken again in 64 bits.
+// A's terms each is off by its y's two roundings (of y, and of c, whose effect at y = 0
+// is in the segment's factor), the exponential's 2^-23 and the ten additions': 2^-24 (2 ln
+// 2 |y| + 12) relatively.  |y| is at most kAbove + 1 + |log2 w|, w = 2^((x - max x) log2 e /
+// T), and the mean of -log2 w under the shares w / A is their entropy less log2 A, log2
+// V - log2 A at most.  So A is off by at most A 2^-24 (2 ln 2 (log2 V - log2 A + kAbove +
+// 1) + 12), B likewise, and near a border A = u W, B = (1 - u) W.
+// Otherwise (one row in fifteen of normal logits of deviation 2.5 and 131,072 columns),
+// and where the largest x c is beyond kRange, the sums are taken again in 64 bits.  r is
+// never below -kRange, so that entries further down, masks of -1e30 among them, add
+// nothing.
+constexpr float kRange = 0x1p17f;
 constexpr float kAbove = 4.f;
-constexpr int64_t kOpenMost = 1024 * kStepCols; // columns
+constexpr int kOpenPer = 2;                              // steps of a segment
+constexpr int64_t kOpenMost = 1024 * kOpenPer * kStepCols; // columns
+
+// The token within the segment of sh.draw, whose sum in 64 bits takes the place of that
+// in 32 (by one wave).  Returns whether the token is certain.
+template <class R>
+__device__ __forceinline__ bool draw_open(const R &row, double u, int32_t *id, float *logp)
+{
+    const auto &sh = row.sh;
+    const int seg = __builtin_amdgcn_readfirstlane(int(sh.draw.seg)), lane = row.lane;
+    const double begin = sh.draw.before;
+    double w[kOpenPer][8], after[kOpenPer], sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < kOpenPer; ++k) {
+        const int64_t col = row.column(seg, k);
+        float v[8];
+        load8(row.x + col, row.V - col, v, -__builtin_inff());
+        row.weights(v, row.zero, w[k]);
+        after[k] = scan_up(((w[k][0] + w[k][1]) + (w[k][2] + w[k][3])) + ((w[k][4] + w[k][5]) + (w[k][6] + w[k][7])), lane) + sum;
+        sum = __shfl(after[k], 63); // of the segment so far
+    }
+    const double W = sh.draw.total - sh.sum[seg] + sum, target = u * W;
+    double gap = 0.0, w_found = 0.0;
+    int64_t found = -1;
+#pragma unroll
+    for (int k = 0; k < kOpenPer; ++k) {
+        const uint64_t pass = __ballot(begin + after[k] > target);
+        if (!pass || found >= 0) continue;
+        const int who = __builtin_ctzll(pass);
+        const double up = __shfl_up(after[k], 1), before = k ? __shfl(after[k ? k - 1 : 0], 63) : 0.0;
+        double at = begin + (lane ? up : before), left = at, right = at, mine = 0.0;
+        int which = -1;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const double next = at + w[k][i];
+            if (which < 0 && next > target) {
+                which = i;
+                left = at;
+                right = next;
+                mine = w[k][i];
+            }
+            at = next;
+        }
+        // a sum of nothing is no border
+        const double g = which < 0 ? 0.0 : fmin(right - target, left > 0.0 ? target - left : right - target);
+        gap = __shfl(g, who);
+        w_found = __shfl(mine, who);
+        found = __shfl(row.column(seg, k) + which, who);
+    }
+    if (lane == 0 && found >= 0) {
+        *id = int32_t(found);
+        if (logp) *logp = float(log(w_found / W));
+    }
+    const double v = fmin(u, 1.0), A = v * W, B = W - A, span = log2(double(row.V)) + kAbove + 1;
+    // (A and B themselves are known to a hundred thousandth)
+    const double off_a = A > 0.0 ? 2 * kLn264 * (span - log2(A)) + 12 : 0.0, off_b = B > 0.0 ? 2 * kLn264 * (span - log2(B)) + 12 : 0.0;
+    return found >= 0 && gap > 0x1.02p-24 * ((1.0 - v) * A * off_a + v * B * off_b) + 1e-13 * W;
+}
 
 template <class T, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void sample_open_kernel(SampleArgs p)
 {
     using R = Row<T, WAVES, 0, 1>;
+    constexpr int kCols = kOpenPer * kStepCols;
     __shared__ Shared<WAVES, R::kSegs, 1> sh;
-    __shared__ float ref[R::kSegs];
+    __shared__ float2 part[R::kSegs]; // a segment's sum and its r
     const gwtf_learn_sample_t &a = p.a;
     const int64_t i = p.row0 + blockIdx.x;
     R row{sh, static_cast<const T *>(a.logits) + i * a.logits_stride, a.vocab, int(threadIdx.x & 63),
-          __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 1, p.segs, p.unit, p.series};
+          __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kOpenPer, p.segs, p.unit, p.series};
     const int each = (p.segs + WAVES - 1) / WAVES, first = row.wave * each;
-    const int end = first + each < p.segs ? first + each : p.segs;
-    const int64_t at = int64_t(first) * kStepCols + row.lane * kVec;
-    typename Vec8<T>::type raw[kAhead];
+    const int end = first + each < p.segs ? first + each : p.segs, whole = int(a.vocab / kCols); // segments without an end of the row
+    typename Vec8<T>::type raw[2][kOpenPer];
     auto fetch = [&](int seg, int slot) {
-        const int64_t col = at + int64_t(seg - first) * kStepCols;
-        raw[slot] = load8_raw(row.x + col, seg < end ? a.vocab - col : 0, T(-__builtin_inff()));
-    };
+        if (seg >= end) return;
+        const T *from = row.x + int64_t(seg) * kCols + row.lane * kVec;
 #pragma unroll
-    for (int q = 0; q < kAhead; ++q) fetch(first + q, q);
+        for (int k = 0; k < kOpenPer; ++k) {
+            if (seg < whole) raw[slot][k] = *reinterpret_cast<const typename Vec8<T>::type *>(from + k * kStepCols);
+            else raw[slot][k] = load8_raw(from + k * kStepCols, a.vocab - int64_t(seg) * kCols - k * kStepCols - row.lane * kVec, T(-__builtin_inff()));
+        }
+    };
+    fetch(first, 0);
+    fetch(first + 1, 1);
     if (threadIdx.x < kTable) sh.table[threadIdx.x] = threadIdx.x ? exp2_series(double(threadIdx.x) / kTable) : 1.0;
     double u = a.uniform_type == GWTF_UNIFORM_F64 ? static_cast<const double *>(a.u)[i] : double(static_cast<const float *>(a.u)[i]);
     u = u >= 0.0 ? u : 0.0;
     row.c = kTable * kLog2e64 / a.temperature;
     const double c = kLog2e64 / a.temperature;
-    // c in two parts, both above 0, so that a masked entry's y is -infinity
-    float ch = float(c);
-    if (double(ch) > c) ch = __uint_as_float(__float_as_uint(ch) - 1);
-    const float cl = fmaxf(float(c - double(ch)), 0x1p-126f), limit = kAbove / ch;
+    const float c32 = float(c);
 
-    float most = -__builtin_inff(), reference = -0x1.fffffep127f;
+    float most = -__builtin_inff(), ref = -kRange;
     uint32_t there = 0;
     bool bad = false;
-    for (int seg = first; seg < end; seg += kAhead) {
+    for (int seg = first; seg < end; seg += 2) {
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            if (seg + q >= end) break; // uniform
-            float v[8];
-            widen<T>(raw[q], v);
-            fetch(seg + q + kAhead, q);
-            const float m = max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), fmaxf(v[6], v[7]));
-            const float l = min3(min3(v[0], v[1], v[2]), min3(v[3], v[4], v[5]), fminf(v[6], v[7]));
+        for (int slot = 0; slot < 2; ++slot) {
+            if (seg + slot >= end) break; // uniform
+            float v[kOpenPer][8], m = -__builtin_inff(), l = __builtin_inff();
+#pragma unroll
+            for (int k = 0; k < kOpenPer; ++k) {
+                widen<T>(raw[slot][k], v[k]);
+#pragma unroll
+                for (int q = 0; q < kVec; q += 2) {
+                    m = max3(m, v[k][q], v[k][q + 1]);
+                    l = min3(l, v[k][q], v[k][q + 1]);
+                }
+            }
+            fetch(seg + slot + 2, slot);
             most = fmaxf(most, m);
-            if (__ballot(m > reference + limit)) reference = wave_fmax(m);
+            if (__ballot(fmaf(m, c32, -ref) > kAbove)) ref = wave_fmax(m) * c32;
             if (__ballot(l == -__builtin_inff())) {
 #pragma unroll
-                for (int k = 0; k < kVec; ++k) there += __popcll(__ballot(v[k] > -__builtin_inff()));
-            } else {
-                there += kStepCols;
-            }
-            float e[8];
+                for (int k = 0; k < kOpenPer; ++k) {
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                const float d = v[k] - reference;
-                e[k] = exp2_(fmaf(d, ch, d * cl));
+                    for (int q = 0; q < kVec; ++q) there += __popcll(__ballot(v[k][q] > -__builtin_inff()));
+                }
+            } else {
+                there += kCols;
             }
-            const float s = wave_sum(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < kOpenPer; ++k) {
+#pragma unroll
+                for (int q = 0; q < kVec; ++q) v[k][q] = exp2_(fmaf(v[k][q], c32, -ref));
+                s += ((v[k][0] + v[k][1]) + (v[k][2] + v[k][3])) + ((v[k][4] + v[k][5]) + (v[k][6] + v[k][7]));
+            }
+            s = wave_sum(s);
             bad = bad || s != s; // a NaN, or +infinity less itself
-            if (row.lane == 0) {
-                sh.sum[seg + q] = double(s);
-                sh.tied[seg + q] = 0;
-                ref[seg + q] = reference;
-            }
+            if (row.lane == 0) part[seg + slot] = {s, ref};
         }
     }
     {
@@ -976,18 +1046,17 @@ __global__ __launch_bounds__(WAVES * 64) void sample_open_kernel(SampleArgs p)
     row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), value_of(key - 1));
     const Cut cut = {kNoneKey, 0, F};
     if (threadIdx.x == 0 && a.kept) a.kept[i] = int32_t(F);
-    for (int seg = threadIdx.x; seg < p.segs; seg += WAVES * 64) sh.sum[seg] *= row.weight_or_0(ref[seg]);
-    __syncthreads();
     if (row.wave == 0) {
+        const double per32 = c / double(c32), highest = double(row.top) * c;
+        for (int seg = row.lane; seg < p.segs; seg += 64) {
+            const double y = double(part[seg].y) * per32 - highest;
+            sh.sum[seg] = y > -1000.0 ? double(part[seg].x) * row.power(y) : 0.0;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
         row.pick(cut, u);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-        const double gap = row.draw(cut, a.ids + i, a.logp ? a.logp + i : nullptr);
-        if (row.lane == 0) {
-            const double W = sh.draw.total, v = fmin(u, 1.0), A = v * W, B = W - A, span = log2(double(a.vocab)) + kAbove;
-            // (the sums in A and B are themselves off by their 1e-5th at most)
-            const double off_a = A > 0.0 ? 2 * kLn264 * (span - log2(A)) + 11 : 0.0, off_b = B > 0.0 ? 2 * kLn264 * (span - log2(B)) + 11 : 0.0;
-            sh.certain = gap > 0x1.02p-24 * (1.0 - v) * A * off_a + 0x1.02p-24 * v * B * off_b + 1e-13 * W;
-        }
+        const bool certain = draw_open(row, u, a.ids + i, a.logp ? a.logp + i : nullptr);
+        if (row.lane == 0) sh.certain = certain && fabs(highest) < kRange;
     }
     __syncthreads();
     if (sh.certain) return;
@@ -1022,8 +1091,8 @@ hipError_t run_open(const gwtf_learn_sample_t &a, hipStream_t s)
     SampleArgs p;
     p.a = a;
     p.series = kSeries;
-    p.per = 1;
-    p.segs = int32_t((a.vocab + kStepCols - 1) / kStepCols);
+    p.per = kOpenPer;
+    p.segs = int32_t((a.vocab + kOpenPer * kStepCols - 1) / (kOpenPer * kStepCols));
     p.unit = 0;
     const int64_t slab = kLaunchThreads / (WAVES * 64);
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
@@ -1042,7 +1111,7 @@ hipError_t by_width(const gwtf_learn_sample_t &a, hipStream_t s)
     // 32-bit sums need a temperature whose quotients stay within 32 bits
     const bool open = !a.temperatures && !a.top_ks && !a.top_ps && !a.min_ps && a.top_k <= 0 && a.top_p >= 1.0 && a.min_p == 0.0 &&
                       a.temperature > 1e-30 && a.temperature < 1e30;
-    if (open && V <= kOpenMost) return V > 16384 ? run_open<T, 16>(a, s) : run_open<T, 4>(a, s);
+    if (open && V <= kOpenMost) return V > 16384 ? (a.num_tokens <= 256 ? run_open<T, 16>(a, s) : run_open<T, 8>(a, s)) : run_open<T, 4>(a, s);
     if (V <= 2048) return run<T, 4, 1>(a, s);
     if (V <= 8192) return run<T, 4, 4>(a, s);
     if (V <= 32768) return run<T, 16, 4>(a, s);
