@@ -91,11 +91,17 @@ extern "C" gwtf_status_t gwtf_learn_create(int32_t device, void *hip_stream, gwt
         return fail(nullptr, GWTF_ERR_DEVICE, "hipDeviceGetAttribute", e);
     }
     void *partial = nullptr;
-    if ((e = hipMalloc(&partial, sizeof(double) * kNormSlots)) != hipSuccess) {
+    if ((e = hipMalloc(&partial, sizeof(double) * (kNormSlots + 1))) != hipSuccess) {
         delete h;
         return fail(nullptr, GWTF_ERR_OUT_OF_MEMORY, "hipMalloc workspace", e);
     }
     h->ws.partial = static_cast<double *>(partial);
+    h->ws.arrived = reinterpret_cast<uint32_t *>(h->ws.partial + kNormSlots);
+    if ((e = hipMemsetAsync(h->ws.arrived, 0, sizeof(double), h->stream)) != hipSuccess) {
+        (void)hipFree(partial);
+        delete h;
+        return fail(nullptr, GWTF_ERR_DEVICE, "hipMemsetAsync", e);
+    }
     *out = h;
     return GWTF_OK;
 }

@@ -9,12 +9,13 @@ namespace gwtf {
 
 // Device workspace of a handle, used in the order of its stream.
 struct LearnWorkspace {
-    double *partial = nullptr; // gradient norm: [kNormSlots] sums of workgroups
+    double *partial = nullptr;   // gradient norm: [kNormSlots] sums of workgroups
+    uint32_t *arrived = nullptr; // and how many have arrived, 0 between calls
     int cus = 0;
 };
 
 constexpr int kNormGroups = 2048; // most workgroups that sum squares of one type
-constexpr int kNormSlots = 3 * kNormGroups;
+constexpr int kNormSlots = 3 * kNormGroups + 1;
 
 // A list's tensors on the device, those of the same types side by side, and for
 // each chunk of values the tensor that it belongs to.

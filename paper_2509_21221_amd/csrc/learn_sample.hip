@@ -139,7 +139,7 @@ struct Shared {
     union {
         uint64_t mass[BINS];
         struct {
-            uint64_t list[BINS > 1 ? kList : 1], order[BINS > 1 ? kFew : 1];
+            uint64_t list[BINS > 1 ? kList : 1], order[BINS > 1 ? kList : 1];
             double w[BINS > 1 ? kFew : 1];
         } few;
     };
@@ -423,6 +423,118 @@ struct Row {
             const uint32_t end = lo + ((1u << shift) - 1u);
             hi = end < hi ? end : hi;
         }
+    }
+
+    // The bin of an entry by its distance from the largest: kBins - 1 at the top, 0 at
+    // kSpan bits of w and further down.
+    static constexpr float kSpan = 48.f;
+    __device__ __forceinline__ uint32_t bin_of(float v, float scale) const
+    {
+        return uint32_t(kBins - 1) - uint32_t(fminf((top - v) * scale, float(kBins - 1)));
+    }
+    // The cut after the least number of entries whose sum of w reaches top_p times the row's: w
+    // added up in bins of equal widths, then the entries of the bin that the sum is
+    // reached in ranked by comparison.  False where those are too many.
+    __device__ __forceinline__ bool nucleus(double top_p, Cut &cut)
+    {
+        const float scale = float(c * (double(kBins) / (kTable * double(kSpan))));
+        // w + magic has w in units of 2^-unit in its low bits
+        const double magic = __builtin_bit_cast(double, uint64_t(1023 + 52 - unit) << 52 | uint64_t(1) << 51);
+        double rest = 0.0;
+        uint32_t further = 0;
+        clear_bins(true);
+        scan(
+            value_of(kNoneKey + 1),
+            [&](int, int64_t, const float *v) {
+                double w[8];
+                weights(v, zero, w);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    const uint32_t b = bin_of(v[i], scale);
+                    if (b) {
+                        atomicAdd(&sh.count[b], 1u);
+                        atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[b]),
+                                  (unsigned long long)(__builtin_bit_cast(uint64_t, w[i] + magic) - __builtin_bit_cast(uint64_t, magic)));
+                    } else {
+                        rest += w[i];
+                        further += v[i] > -__builtin_inff() ? 1u : 0u;
+                    }
+                }
+            },
+            [](int) {});
+        const uint32_t some = wave_add(further);
+        rest = wave_sum64(rest);
+        if (lane == 0 && some) {
+            atomicAdd(&sh.count[0], some);
+            atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[0]), (unsigned long long)(ldexp(rest, unit)));
+        }
+        // the row's sum, in an order of its own
+        __syncthreads();
+        uint64_t mine = 0;
+        for (int b = threadIdx.x; b < kBins; b += kThreads) mine += sh.mass[b];
+        double all = wave_sum64(double(mine));
+        if (lane == 0) sh.wsum[wave] = all;
+        __syncthreads();
+        all = 0.0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) all += sh.wsum[i];
+        const double target = top_p * ldexp(all, -unit);
+        find_bin(true, 0, target, 0, 0.0, 0, false);
+        if (sh.at == kBins) return true; // nothing is cut off
+        const uint32_t bin = kBins - 1 - sh.at, L = sh.bin.count, above = sh.bin.above;
+        const double above_mass = sh.bin.above_mass;
+        if (L > kList) return false;
+        __syncthreads();
+        if (threadIdx.x == 0) sh.listed = 0;
+        __syncthreads();
+        // nothing of the bin is below this
+        const float low = bin ? top - (float(kBins - bin) * 1.0001f + 1.f) / scale : -__builtin_inff();
+        scan(
+            fmaxf(low, value_of(kNoneKey + 1)),
+            [&](int, int64_t col, const float *v) {
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    if (v[i] > -__builtin_inff() && bin_of(v[i], scale) == bin) {
+                        const uint32_t at = atomicAdd(&sh.listed, 1u);
+                        if (at < kList) sh.few.list[at] = uint64_t(key_of(v[i])) << 32 | uint32_t(~uint32_t(col + i));
+                    }
+                }
+            },
+            [](int) {});
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < L; j += kThreads) {
+            const uint64_t mine = sh.few.list[j];
+            uint32_t rank = 0;
+            for (uint32_t i = 0; i < L; ++i) rank += sh.few.list[i] > mine ? 1u : 0u;
+            sh.few.order[rank] = mine;
+        }
+        __syncthreads();
+        // in every wave alike
+        constexpr int kEach = kList / 64;
+        const uint32_t j0 = lane * kEach;
+        double w[kEach], mass = 0.0;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            w[q] = j0 + q < L ? weight_or_0(value_of(uint32_t(sh.few.order[j0 + q] >> 32))) : 0.0;
+            mass += w[q];
+        }
+        double at = scan_up(mass, lane);
+        const double up = __shfl_up(at, 1);
+        at = above_mass + (lane ? up : 0.0);
+        uint32_t under = 0;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            at += w[q];
+            under += j0 + q < L && at < target ? 1u : 0u;
+        }
+        under = wave_add(under);
+        under = under < L ? under : L - 1;
+        const uint32_t key = uint32_t(sh.few.order[under] >> 32);
+        uint32_t ties = 0;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) ties += j0 + q <= under && uint32_t(sh.few.order[j0 + q] >> 32) == key ? 1u : 0u;
+        cut = {key, wave_add(ties), above + under + 1};
+        return true;
     }
 
     // Sums of w over what stays, by segment, and over the row (sh.draw.total);
@@ -813,7 +925,7 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
                 return;
             cut = row.select(false, uint32_t(top_k), 0.0, lo, cut);
         }
-        if (top_p < 1.0) {
+        if (top_p < 1.0 && !(cut.n == F && row.nucleus(top_p, cut))) {
             row.sums(cut, u);
             summed = true;
             // The entry that the sum ends with and those after it are worth more than
@@ -1075,6 +1187,7 @@ hipError_t run(const gwtf_learn_sample_t &a, hipStream_t s)
     p.segs = int32_t((steps + p.per - 1) / p.per);
     p.unit = 62;
     while ((int64_t(1) << (62 - p.unit)) < a.vocab) --p.unit;
+    p.unit = p.unit < 50 ? p.unit : 50;
     const int64_t slab = kLaunchThreads / (WAVES * 64);
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         p.row0 = r;
