@@ -55,7 +55,7 @@ enum {
 #define GWTF_STATE_BLOCK 128
 
 /* Creates a handle on `device` that enqueues on `hip_stream` (a hipStream_t;
- * NULL = the device's null stream) and allocates its workspace, 50 KB.  *out
+ * NULL = the device's null stream) and allocates its workspace, 2.2 MB.  *out
  * receives the handle, or NULL on failure. */
 gwtf_status_t gwtf_learn_create(int32_t device, void *hip_stream, gwtf_learn_t **out);
 

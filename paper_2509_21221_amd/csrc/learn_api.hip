@@ -86,19 +86,29 @@ extern "C" gwtf_status_t gwtf_learn_create(int32_t device, void *hip_stream, gwt
     if (!h) return fail(nullptr, GWTF_ERR_OUT_OF_MEMORY, "host allocation failed");
     h->device = device;
     h->stream = static_cast<hipStream_t>(hip_stream);
-    if ((e = hipDeviceGetAttribute(&h->ws.cus, hipDeviceAttributeMultiprocessorCount, device)) != hipSuccess) {
-        delete h;
-        return fail(nullptr, GWTF_ERR_DEVICE, "hipDeviceGetAttribute", e);
-    }
-    void *partial = nullptr;
-    if ((e = hipMalloc(&partial, sizeof(double) * (kNormSlots + 1))) != hipSuccess) {
+    // one allocation, its parts on 256-byte boundaries, the counters first
+    LearnWorkspace &w = h->ws;
+    size_t total = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = total;
+        total += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    const size_t arrived = take(sizeof(uint32_t)), rows = take(sizeof(uint32_t) * kRecheckSlots), zeros = total;
+    const size_t partial = take(sizeof(double) * kNormSlots), key = take(sizeof(uint32_t) * kRecheckRows);
+    const size_t sum = take(sizeof(uint64_t) * kRecheckSlots * kRecheckSegs);
+    if ((e = hipMalloc(&w.base, total)) != hipSuccess) {
         delete h;
         return fail(nullptr, GWTF_ERR_OUT_OF_MEMORY, "hipMalloc workspace", e);
     }
-    h->ws.partial = static_cast<double *>(partial);
-    h->ws.arrived = reinterpret_cast<uint32_t *>(h->ws.partial + kNormSlots);
-    if ((e = hipMemsetAsync(h->ws.arrived, 0, sizeof(double), h->stream)) != hipSuccess) {
-        (void)hipFree(partial);
+    unsigned char *const base = static_cast<unsigned char *>(w.base);
+    w.arrived = reinterpret_cast<uint32_t *>(base + arrived);
+    w.recheck.arrived = reinterpret_cast<uint32_t *>(base + rows);
+    w.partial = reinterpret_cast<double *>(base + partial);
+    w.recheck.key = reinterpret_cast<uint32_t *>(base + key);
+    w.recheck.sum = reinterpret_cast<uint64_t *>(base + sum);
+    if ((e = hipMemsetAsync(base, 0, zeros, h->stream)) != hipSuccess) {
+        (void)hipFree(w.base);
         delete h;
         return fail(nullptr, GWTF_ERR_DEVICE, "hipMemsetAsync", e);
     }
@@ -111,7 +121,7 @@ extern "C" void gwtf_learn_destroy(gwtf_learn_t *h)
     if (!h) return;
     DeviceScope scope(h->device);
     if (scope.e == hipSuccess) (void)hipStreamSynchronize(h->stream);
-    (void)hipFree(h->ws.partial);
+    (void)hipFree(h->ws.base);
     delete h;
 }
 
@@ -138,7 +148,7 @@ extern "C" gwtf_status_t gwtf_learn_sample(gwtf_learn_t *h, const gwtf_learn_sam
     LEARN_CHECK(bad_vector(a->ids, N, 4))
     LEARN_CHECK(a->logp ? bad_vector(a->logp, N, 4) : nullptr)
     LEARN_CHECK(a->kept ? bad_vector(a->kept, N, 4) : nullptr)
-    LEARN_LAUNCH("gwtf_learn_sample", launch_sample(*a, h->stream))
+    LEARN_LAUNCH("gwtf_learn_sample", launch_sample(*a, h->ws, h->stream))
 }
 
 extern "C" gwtf_status_t gwtf_learn_list_create(gwtf_learn_t *h, int64_t num_tensors, const gwtf_learn_tensor_t *tensors, int32_t form,

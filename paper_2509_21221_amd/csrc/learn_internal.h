@@ -7,11 +7,23 @@
 
 namespace gwtf {
 
+// Draws of many rows: the rows that are uncertain after 32-bit sums.
+constexpr int kRecheckRows = 4096;  // most rows of such a call
+constexpr int kRecheckSlots = 256;  // of them shared by workgroups
+constexpr int kRecheckSegs = 1024;
+constexpr int kRecheckGroups = 512; // workgroups that share them
+struct RecheckWorkspace {
+    uint32_t *key = nullptr;     // [kRecheckRows] of an uncertain row's largest entry, 0 of others
+    uint32_t *arrived = nullptr; // [kRecheckSlots] 0 between calls
+    uint64_t *sum = nullptr;     // [kRecheckSlots][kRecheckSegs] sums of segments
+};
+
 // Device workspace of a handle, used in the order of its stream.
 struct LearnWorkspace {
+    void *base = nullptr; // the allocation that holds the parts
     double *partial = nullptr;   // gradient norm: [kNormSlots] sums of workgroups
     uint32_t *arrived = nullptr; // and how many have arrived, 0 between calls
-    int cus = 0;
+    RecheckWorkspace recheck;
 };
 
 constexpr int kNormGroups = 2048; // most workgroups that sum squares of one type
@@ -45,7 +57,7 @@ struct LearnTable {
 };
 hipError_t build_table(int64_t num, const gwtf_learn_tensor_t *tensors, LearnTable &t);
 
-hipError_t launch_sample(const gwtf_learn_sample_t &a, hipStream_t s);
+hipError_t launch_sample(const gwtf_learn_sample_t &a, const LearnWorkspace &w, hipStream_t s);
 hipError_t launch_grad_norm(const gwtf_learn_grad_norm_t &a, const LearnTable &t, const LearnWorkspace &w, hipStream_t s);
 hipError_t launch_adamw(const gwtf_learn_adamw_t &a, const LearnTable &t, hipStream_t s);
 

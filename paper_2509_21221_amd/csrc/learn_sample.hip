@@ -843,6 +843,7 @@ struct SampleArgs {
     int64_t row0;
     int32_t per, segs, unit;
     Series series;
+    RecheckWorkspace ws; // of sample_open_kernel: where ws.key is not NULL uncertain rows are left to another launch
 };
 
 template <class T, int WAVES, int S>
@@ -1152,6 +1153,7 @@ __global__ __launch_bounds__(WAVES * 64) void sample_open_kernel(SampleArgs p)
             a.ids[i] = -1;
             if (a.logp) a.logp[i] = wrong ? __builtin_nanf("") : -__builtin_inff();
             if (a.kept) a.kept[i] = 0;
+            if (p.ws.key) p.ws.key[i] = 0;
         }
         return;
     }
@@ -1168,12 +1170,108 @@ __global__ __launch_bounds__(WAVES * 64) void sample_open_kernel(SampleArgs p)
         row.pick(cut, u);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
         const bool certain = draw_open(row, u, a.ids + i, a.logp ? a.logp + i : nullptr);
-        if (row.lane == 0) sh.certain = certain && fabs(highest) < kRange;
+        if (row.lane == 0) {
+            sh.certain = certain && fabs(highest) < kRange;
+            if (p.ws.key) p.ws.key[i] = sh.certain ? 0u : key;
+        }
     }
+    if (p.ws.key) return;
     __syncthreads();
     if (sh.certain) return;
     row.sums(cut, u);
     if (row.wave == 0) row.draw(cut, a.ids + i, a.logp ? a.logp + i : nullptr);
+}
+
+// The rows that sample_open_kernel has left, in 64 bits: each shared by kParts workgroups,
+// of which the last to arrive draws.  (By the workgroup that finds its row uncertain,
+// 20 us after all others have ended: 1,024 rows of 131,072 109 us.)
+constexpr int kParts = 8;
+
+template <class T, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void sample_recheck_kernel(SampleArgs p)
+{
+    using R = Row<T, WAVES, 0, 1>;
+    __shared__ Shared<WAVES, R::kSegs, 1> sh;
+    __shared__ uint16_t rows[kRecheckRows];
+    const gwtf_learn_sample_t &a = p.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // the rows that are left, in their order
+    constexpr int kEach = kRecheckRows / (WAVES * 64);
+    const int r0 = threadIdx.x * kEach, N = int(a.num_tokens);
+    uint32_t mine = 0;
+    for (int r = r0; r < r0 + kEach && r < N; ++r) mine += p.ws.key[r] != 0;
+    const uint32_t upto = scan_up(mine, lane);
+    if (lane == 63) sh.wcount[wave] = upto;
+    if (threadIdx.x < kTable) sh.table[threadIdx.x] = threadIdx.x ? exp2_series(double(threadIdx.x) / kTable) : 1.0;
+    __syncthreads();
+    uint32_t at = upto - mine, left = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        at += w < wave ? sh.wcount[w] : 0u;
+        left += sh.wcount[w];
+    }
+    if (mine)
+        for (int r = r0; r < r0 + kEach && r < N; ++r)
+            if (p.ws.key[r] != 0) rows[at++] = uint16_t(r);
+    __syncthreads();
+    // the first kRecheckSlots in parts, others whole
+    const uint32_t shared = left < uint32_t(kRecheckSlots) ? left : uint32_t(kRecheckSlots), items = shared * kParts + (left - shared);
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const bool whole = item >= shared * kParts;
+        const uint32_t slot = whole ? shared + (item - shared * kParts) : item / kParts;
+        const int part = whole ? 0 : int(item % kParts);
+        const int64_t i = rows[slot];
+        R row{sh, static_cast<const T *>(a.logits) + i * a.logits_stride, a.vocab, lane, wave, p.per, p.segs, p.unit, p.series};
+        const uint32_t key = p.ws.key[i];
+        row.top = value_of(key);
+        row.c = kTable * kLog2e64 / a.temperature;
+        row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), value_of(key - 1));
+        double u = a.uniform_type == GWTF_UNIFORM_F64 ? static_cast<const double *>(a.u)[i] : double(static_cast<const float *>(a.u)[i]);
+        u = u >= 0.0 ? u : 0.0;
+        const Cut cut = {kNoneKey, 0, 1};
+        if (whole) {
+            row.sums(cut, u);
+        } else {
+            uint64_t *const sums = p.ws.sum + int64_t(slot) * R::kSegs;
+            const int each = (p.segs + kParts - 1) / kParts, end = (part + 1) * each < p.segs ? (part + 1) * each : p.segs;
+            for (int seg = part * each + wave; seg < end; seg += WAVES) {
+                double s = 0.0;
+                typename Vec8<T>::type raw[kOpenPer];
+#pragma unroll
+                for (int k = 0; k < kOpenPer; ++k) {
+                    const int64_t col = row.column(seg, k);
+                    raw[k] = load8_raw(row.x + col, a.vocab - col, T(-__builtin_inff()));
+                }
+#pragma unroll
+                for (int k = 0; k < kOpenPer; ++k) {
+                    float v[8];
+                    double w[8];
+                    widen<T>(raw[k], v);
+                    row.weights(v, row.zero, w);
+                    s += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+                }
+                s = wave_sum64(s);
+                if (lane == 0) __hip_atomic_store(sums + seg, __builtin_bit_cast(uint64_t, s), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            // sums and counter are words of agent scope; the waits put the sums in memory
+            // before the arrival is counted
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (threadIdx.x == 0)
+                sh.certain = __hip_atomic_fetch_add(p.ws.arrived + slot, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == uint32_t(kParts - 1);
+            __syncthreads();
+            const bool last = sh.certain;
+            __syncthreads();
+            if (!last) continue;
+            for (int seg = threadIdx.x; seg < p.segs; seg += WAVES * 64)
+                sh.sum[seg] = __builtin_bit_cast(double, __hip_atomic_load(sums + seg, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            if (threadIdx.x == 0) p.ws.arrived[slot] = 0;
+            __syncthreads();
+            if (wave == 0) row.pick(cut, u);
+            __syncthreads();
+        }
+        if (wave == 0) row.draw(cut, a.ids + i, a.logp ? a.logp + i : nullptr);
+        __syncthreads();
+    }
 }
 
 template <class T, int WAVES, int S>
@@ -1199,10 +1297,12 @@ hipError_t run(const gwtf_learn_sample_t &a, hipStream_t s)
 }
 
 template <class T, int WAVES>
-hipError_t run_open(const gwtf_learn_sample_t &a, hipStream_t s)
+hipError_t run_open(const gwtf_learn_sample_t &a, const RecheckWorkspace &ws, bool recheck, hipStream_t s)
 {
     SampleArgs p;
     p.a = a;
+    p.ws = ws;
+    if (!recheck) p.ws.key = nullptr;
     p.series = kSeries;
     p.per = kOpenPer;
     p.segs = int32_t((a.vocab + kOpenPer * kStepCols - 1) / (kOpenPer * kStepCols));
@@ -1214,17 +1314,21 @@ hipError_t run_open(const gwtf_learn_sample_t &a, hipStream_t s)
         const hipError_t e = launch(sample_open_kernel<T, WAVES>, n, WAVES * 64, s, p);
         if (e != hipSuccess) return e;
     }
-    return hipSuccess;
+    return recheck ? launch(sample_recheck_kernel<T, 8>, kRecheckGroups, 512, s, p) : hipSuccess;
 }
 
 template <class T>
-hipError_t by_width(const gwtf_learn_sample_t &a, hipStream_t s)
+hipError_t by_width(const gwtf_learn_sample_t &a, const RecheckWorkspace &ws, hipStream_t s)
 {
     const int64_t V = a.vocab;
     // 32-bit sums need a temperature whose quotients stay within 32 bits
     const bool open = !a.temperatures && !a.top_ks && !a.top_ps && !a.min_ps && a.top_k <= 0 && a.top_p >= 1.0 && a.min_p == 0.0 &&
                       a.temperature > 1e-30 && a.temperature < 1e30;
-    if (open && V <= kOpenMost) return V > 16384 ? (a.num_tokens <= 256 ? run_open<T, 16>(a, s) : run_open<T, 8>(a, s)) : run_open<T, 4>(a, s);
+    if (open && V <= kOpenMost) {
+        if (V <= 16384) return run_open<T, 4>(a, ws, false, s);
+        // Rows for all of the card: uncertain ones are shared out at the end.
+        return a.num_tokens <= 256 ? run_open<T, 16>(a, ws, false, s) : run_open<T, 8>(a, ws, a.num_tokens <= kRecheckRows, s);
+    }
     if (V <= 2048) return run<T, 4, 1>(a, s);
     if (V <= 8192) return run<T, 4, 4>(a, s);
     if (V <= 32768) return run<T, 16, 4>(a, s);
@@ -1236,12 +1340,12 @@ hipError_t by_width(const gwtf_learn_sample_t &a, hipStream_t s)
 
 } // namespace
 
-hipError_t launch_sample(const gwtf_learn_sample_t &a, hipStream_t s)
+hipError_t launch_sample(const gwtf_learn_sample_t &a, const LearnWorkspace &w, hipStream_t s)
 {
     switch (a.type) {
-    case GWTF_TYPE_F32: return by_width<float>(a, s);
-    case GWTF_TYPE_F16: return by_width<f16_t>(a, s);
-    default: return by_width<bf16_t>(a, s);
+    case GWTF_TYPE_F32: return by_width<float>(a, w.recheck, s);
+    case GWTF_TYPE_F16: return by_width<f16_t>(a, w.recheck, s);
+    default: return by_width<bf16_t>(a, w.recheck, s);
     }
 }
 

@@ -608,3 +608,49 @@ def test_same_bits_again(ops):
     group = ops.parameters(None, [torch.randn(1_000_003, device="cuda"), torch.randn(77, device="cuda")])
     n0 = ops.grad_norm(group)[0]
     assert all(torch.equal(n0, ops.grad_norm(group)[0]) for _ in range(3))
+
+
+def check_open(ops, x, u, temperature):
+    """Draws without filters of many rows against 64-bit sums in torch: the oracle's arithmetic, row by row too slow here."""
+    ids, logp, kept = ops.sample(x, u, temperature=temperature)
+    for i in range(0, x.shape[0], 64):
+        d = (x[i:i + 64].double() - x[i:i + 64].double().amax(1, keepdim=True)) / temperature
+        c = torch.cumsum(torch.exp(d), 1)
+        want = (c <= u[i:i + 64, None] * c[:, -1:]).sum(1)
+        assert torch.equal(ids[i:i + 64].long(), want)
+        lp = d.gather(1, want[:, None])[:, 0] - torch.log(c[:, -1])
+        assert ((logp[i:i + 64] - lp).abs() <= HALF["f32"] * lp.abs() + open_error(x.shape[1])).all()
+    assert (kept == x.shape[1]).all()
+    check_rows(ops, x[:3], u[:3], temperature=temperature)
+
+
+@pytest.mark.parametrize("n,v,dtype,std,shift,t", [(257, 16385, "bf16", 2.5, 0.0, 1.0), (700, 40000, "bf16", 0.01, 0.0, 1.0), (300, 17001, "f32", 1.0, 2e5, 1.0),
+                                                   (513, 20000, "f16", 4.0, 0.0, 0.25), (1000, 33000, "f32", 2.5, 0.0, 1.3), (4097, 16400, "bf16", 2.5, 0.0, 1.0),
+                                                   (600, 17000, "f32", 1.0, -3e5, 2.0), (256, 30000, "bf16", 1.0, 0.0, 1.0)])
+def test_sample_many_rows(ops, n, v, dtype, std, shift, t):
+    """Rows for all of the card; those that 32-bit sums leave open (all that are far from 0, more than are shared among them) are drawn by a second launch."""
+    x = logits(n, v, dtype, n, std=std).add_(shift)
+    check_open(ops, x, uniform(n, n), t)
+
+
+def test_sample_many_rows_again_and_captured():
+    """A call with many open rows leaves nothing behind for the next; replays give its results."""
+    side = torch.cuda.Stream()
+    x, u = logits(400, 17000, "f32", 41).add_(2e5), uniform(400, 41)
+    y = logits(400, 17000, "f32", 42)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), LearnOps(stream=side) as o:
+        first, second = o.sample(x, u), o.sample(y, u)
+        assert all(torch.equal(a, b) for a, b in zip(first, o.sample(x, u)))
+        out = tuple(torch.empty_like(t) for t in first)
+        graph = torch.cuda.CUDAGraph()
+        z = x.clone()
+        with torch.cuda.graph(graph, stream=side):
+            o.sample(z, u, out=out)
+        for source, want in ((x, first), (y, second), (x, first)):
+            z.copy_(source)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+            assert all(torch.equal(a, b) for a, b in zip(o.sample(source, u), want))
+        del graph
