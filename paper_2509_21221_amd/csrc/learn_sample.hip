@@ -843,7 +843,7 @@ struct SampleArgs {
     int64_t row0;
     int32_t per, segs, unit;
     Series series;
-    RecheckWorkspace ws; // of sample_open_kernel: where ws.key is not NULL uncertain rows are left to another launch
+    RecheckWorkspace ws;
 };
 
 template <class T, int WAVES, int S>
@@ -1057,7 +1057,8 @@ __device__ __forceinline__ bool draw_open(const R &row, double u, int32_t *id, f
     return found >= 0 && gap > 0x1.02p-24 * ((1.0 - v) * A * off_a + v * B * off_b) + 1e-13 * W;
 }
 
-template <class T, int WAVES>
+// LEAVE: uncertain rows are left to another launch.
+template <class T, int WAVES, bool LEAVE>
 __global__ __launch_bounds__(WAVES * 64) void sample_open_kernel(SampleArgs p)
 {
     using R = Row<T, WAVES, 0, 1>;
@@ -1153,7 +1154,7 @@ __global__ __launch_bounds__(WAVES * 64) void sample_open_kernel(SampleArgs p)
             a.ids[i] = -1;
             if (a.logp) a.logp[i] = wrong ? __builtin_nanf("") : -__builtin_inff();
             if (a.kept) a.kept[i] = 0;
-            if (p.ws.key) p.ws.key[i] = 0;
+            if (LEAVE) p.ws.key[i] = 0;
         }
         return;
     }
@@ -1172,14 +1173,15 @@ __global__ __launch_bounds__(WAVES * 64) void sample_open_kernel(SampleArgs p)
         const bool certain = draw_open(row, u, a.ids + i, a.logp ? a.logp + i : nullptr);
         if (row.lane == 0) {
             sh.certain = certain && fabs(highest) < kRange;
-            if (p.ws.key) p.ws.key[i] = sh.certain ? 0u : key;
+            if (LEAVE) p.ws.key[i] = sh.certain ? 0u : key;
         }
     }
-    if (p.ws.key) return;
-    __syncthreads();
-    if (sh.certain) return;
-    row.sums(cut, u);
-    if (row.wave == 0) row.draw(cut, a.ids + i, a.logp ? a.logp + i : nullptr);
+    if constexpr (!LEAVE) {
+        __syncthreads();
+        if (sh.certain) return;
+        row.sums(cut, u);
+        if (row.wave == 0) row.draw(cut, a.ids + i, a.logp ? a.logp + i : nullptr);
+    }
 }
 
 // The rows that sample_open_kernel has left, in 64 bits: each shared by kParts workgroups,
@@ -1198,8 +1200,12 @@ __global__ __launch_bounds__(WAVES * 64) void sample_recheck_kernel(SampleArgs p
     // the rows that are left, in their order
     constexpr int kEach = kRecheckRows / (WAVES * 64);
     const int r0 = threadIdx.x * kEach, N = int(a.num_tokens);
+    static_assert(kEach == 8, "two reads of four rows");
+    const uint4 k0 = reinterpret_cast<const uint4 *>(p.ws.key + r0)[0], k1 = reinterpret_cast<const uint4 *>(p.ws.key + r0)[1];
+    const uint32_t keys[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w}; // (of rows from N on, left by another call)
     uint32_t mine = 0;
-    for (int r = r0; r < r0 + kEach && r < N; ++r) mine += p.ws.key[r] != 0;
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) mine += r0 + q < N && keys[q] != 0;
     const uint32_t upto = scan_up(mine, lane);
     if (lane == 63) sh.wcount[wave] = upto;
     if (threadIdx.x < kTable) sh.table[threadIdx.x] = threadIdx.x ? exp2_series(double(threadIdx.x) / kTable) : 1.0;
@@ -1209,9 +1215,9 @@ __global__ __launch_bounds__(WAVES * 64) void sample_recheck_kernel(SampleArgs p
         at += w < wave ? sh.wcount[w] : 0u;
         left += sh.wcount[w];
     }
-    if (mine)
-        for (int r = r0; r < r0 + kEach && r < N; ++r)
-            if (p.ws.key[r] != 0) rows[at++] = uint16_t(r);
+#pragma unroll
+    for (int q = 0; q < kEach; ++q)
+        if (r0 + q < N && keys[q] != 0) rows[at++] = uint16_t(r0 + q);
     __syncthreads();
     // the first kRecheckSlots in parts, others whole
     const uint32_t shared = left < uint32_t(kRecheckSlots) ? left : uint32_t(kRecheckSlots), items = shared * kParts + (left - shared);
@@ -1233,14 +1239,20 @@ __global__ __launch_bounds__(WAVES * 64) void sample_recheck_kernel(SampleArgs p
         } else {
             uint64_t *const sums = p.ws.sum + int64_t(slot) * R::kSegs;
             const int each = (p.segs + kParts - 1) / kParts, end = (part + 1) * each < p.segs ? (part + 1) * each : p.segs;
-            for (int seg = part * each + wave; seg < end; seg += WAVES) {
-                double s = 0.0;
-                typename Vec8<T>::type raw[kOpenPer];
+            typename Vec8<T>::type raw[kOpenPer], next[kOpenPer];
+            auto fetch = [&](int seg) {
 #pragma unroll
                 for (int k = 0; k < kOpenPer; ++k) {
                     const int64_t col = row.column(seg, k);
-                    raw[k] = load8_raw(row.x + col, a.vocab - col, T(-__builtin_inff()));
+                    next[k] = load8_raw(row.x + col, seg < end ? a.vocab - col : 0, T(-__builtin_inff()));
                 }
+            };
+            fetch(part * each + wave);
+            for (int seg = part * each + wave; seg < end; seg += WAVES) {
+                double s = 0.0;
+#pragma unroll
+                for (int k = 0; k < kOpenPer; ++k) raw[k] = next[k];
+                fetch(seg + WAVES);
 #pragma unroll
                 for (int k = 0; k < kOpenPer; ++k) {
                     float v[8];
@@ -1296,13 +1308,12 @@ hipError_t run(const gwtf_learn_sample_t &a, hipStream_t s)
     return hipSuccess;
 }
 
-template <class T, int WAVES>
-hipError_t run_open(const gwtf_learn_sample_t &a, const RecheckWorkspace &ws, bool recheck, hipStream_t s)
+template <class T, int WAVES, bool LEAVE>
+hipError_t run_open(const gwtf_learn_sample_t &a, const RecheckWorkspace &ws, hipStream_t s)
 {
     SampleArgs p;
     p.a = a;
     p.ws = ws;
-    if (!recheck) p.ws.key = nullptr;
     p.series = kSeries;
     p.per = kOpenPer;
     p.segs = int32_t((a.vocab + kOpenPer * kStepCols - 1) / (kOpenPer * kStepCols));
@@ -1311,10 +1322,11 @@ hipError_t run_open(const gwtf_learn_sample_t &a, const RecheckWorkspace &ws, bo
     for (int64_t r = 0; r < a.num_tokens; r += slab) {
         p.row0 = r;
         const int64_t n = a.num_tokens - r < slab ? a.num_tokens - r : slab;
-        const hipError_t e = launch(sample_open_kernel<T, WAVES>, n, WAVES * 64, s, p);
+        const hipError_t e = launch(sample_open_kernel<T, WAVES, LEAVE>, n, WAVES * 64, s, p);
         if (e != hipSuccess) return e;
     }
-    return recheck ? launch(sample_recheck_kernel<T, 8>, kRecheckGroups, 512, s, p) : hipSuccess;
+    if constexpr (LEAVE) return launch(sample_recheck_kernel<T, 8>, kRecheckGroups, 512, s, p);
+    return hipSuccess;
 }
 
 template <class T>
@@ -1325,9 +1337,10 @@ hipError_t by_width(const gwtf_learn_sample_t &a, const RecheckWorkspace &ws, hi
     const bool open = !a.temperatures && !a.top_ks && !a.top_ps && !a.min_ps && a.top_k <= 0 && a.top_p >= 1.0 && a.min_p == 0.0 &&
                       a.temperature > 1e-30 && a.temperature < 1e30;
     if (open && V <= kOpenMost) {
-        if (V <= 16384) return run_open<T, 4>(a, ws, false, s);
-        // Rows for all of the card: uncertain ones are shared out at the end.
-        return a.num_tokens <= 256 ? run_open<T, 16>(a, ws, false, s) : run_open<T, 8>(a, ws, a.num_tokens <= kRecheckRows, s);
+        if (V <= 16384) return run_open<T, 4, false>(a, ws, s);
+        if (a.num_tokens <= 256) return run_open<T, 16, false>(a, ws, s);
+        // rows for all of the card: uncertain ones are shared out at the end
+        return a.num_tokens <= kRecheckRows ? run_open<T, 8, true>(a, ws, s) : run_open<T, 8, false>(a, ws, s);
     }
     if (V <= 2048) return run<T, 4, 1>(a, s);
     if (V <= 8192) return run<T, 4, 4>(a, s);
