@@ -77,10 +77,10 @@ def moments32(g, m, v, betas, factor=1.0):
     return m, v.astype(f) * f(betas[1]) + g * g * f(1 - betas[1])
 
 
-def draws(size, seed, site, step):
-    """16 random bits for each of a tensor's values."""
+def draws(size, seed, site, step, first=0):
+    """16 random bits for each of a tensor's values from number `first` on, a multiple of eight."""
     n = -(-size // 8)
-    i = np.arange(n, dtype=np.uint64)
+    i = np.arange(first // 8, first // 8 + n, dtype=np.uint64)
     counter = np.stack((i, np.full(n, site, np.uint64), np.full(n, step & 0xFFFFFFFF, np.uint64),
                         np.full(n, step >> 32, np.uint64)), -1)
     words = philox4x32(counter, (seed & 0xFFFFFFFF, seed >> 32))

@@ -18,6 +18,16 @@
 //
 // With top_k up to kFew the k-th largest of the eights' largest entries is a bound
 // that about k entries reach; they are ranked by comparison, and one wave does the rest.
+// With top_p alone w is added up in equal bins by distance from the largest entry, and the
+// entries of one bin are ranked.  Rows without a filter take one reading with 32-bit
+// sums (sample_open_kernel).
+//
+// Few rows are bound by what follows one another on a row's own compute unit: the
+// reading, 64-bit weights at some 20 instructions each, a dozen barriers (7 x
+// 131,072 bf16, top_k 50 with top_p and min_p 23 us; 64 x 32,000 f16, top_p 0.95 35; 255 x 50,001 f32,
+// each row its own settings 49; 1 x 32,001 f32 without a filter 8).  Many rows without
+// a filter: 1,024 x 131,072 bf16 59 us (268 MB, 4.5 TB/s; memory and vector issue alike, eight issue
+// slots an entry) and 24 for the rows that are left uncertain.
 #include "learn_internal.h"
 #include "stage_device.h"
 
@@ -178,7 +188,7 @@ struct Row {
     double c;  // kTable log2 e / T
     float zero;    // entries from here down have a w of 0 (2^-1000, but for the rounding of this bound: 2^-600 at most)
     typename Vec8<T>::type raw[S ? S : 1];
-    float largest[S ? S : 1]; // of each eight
+    float largest[S ? S : 1]; // of each eight; S = 0: of the lane's
 
     // first column of this lane's eight
     __device__ __forceinline__ int64_t column(int seg, int q) const { return (int64_t(seg) * per + q) * kStepCols + lane * kVec; }
@@ -701,13 +711,12 @@ struct Row {
     }
 
     // A key that at least `target` entries reach and not many more: the lower end of
-    // the bin of the target-th largest of the eights' largest.
+    // the bin of the target-th largest of the eights' largest (S = 0: of the lanes').
     __device__ __forceinline__ uint32_t bound_of(uint32_t target)
     {
-        if constexpr (S == 0) return kNoneKey + 1;
-        float mine = -__builtin_inff();
+        float mine = largest[0];
 #pragma unroll
-        for (int s = 0; s < S; ++s) mine = fmaxf(mine, largest[s]);
+        for (int s = 1; s < S; ++s) mine = fmaxf(mine, largest[s]);
         // no lane's largest is below lo, so that the bins are as narrow as can be
         uint32_t low = key_of(mine);
         low = low <= kNoneKey ? ~0u : low;
@@ -721,7 +730,7 @@ struct Row {
         int shift = kRes;
         while (((hi - lo) >> shift) >= uint32_t(kBins)) ++shift;
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
+        for (int s = 0; s < (S ? S : 1); ++s) {
             const uint32_t k = key_of(largest[s]);
             if (k >= lo && k > kNoneKey) atomicAdd(&sh.count[(k - lo) >> shift], 1u);
         }
@@ -887,6 +896,7 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
         },
         [](int) {});
     {
+        if constexpr (S == 0) row.largest[0] = most;
         const uint32_t key = wave_umax(key_of(most)), n = there, wrong = __ballot(bad) != 0;
         if (row.lane == 0) {
             sh.wmost[row.wave] = key;
