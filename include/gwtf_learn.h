@@ -82,8 +82,11 @@ const char *gwtf_learn_last_error(const gwtf_learn_t *h);
  * and of those before it, is above u times that of all:
  *   ids = its index, logp = ln of its share of the sum, kept = how many stay.
  * Sums, w and their products with u and p are held in 64 bits, so that a draw is
- * that of exact arithmetic unless u or p falls within some 1e-13 of a border; a w
- * below 2^-600 may count as 0.  u counts as within [0, 1)
+ * that of exact arithmetic unless u falls within some 1e-13 of a border, or p
+ * within some 1e-11; a w below 2^-600 may count as 0.  logp is rounded once from 64
+ * bits, but where nothing is filtered (the numbers top_k <= 0, top_p >= 1, min_p 0)
+ * it comes from a sum that is off by 2^-24 (2 ln 2 (log2 V + 5) + 12) of itself at most.
+ * u counts as within [0, 1)
  * (a NaN as 0).  An entry of -infinity is masked; a row of nothing else gives
  * ids -1, logp -infinity, kept 0.  A row with a NaN or +infinity, and one
  * whose settings are out of range (below), gives ids -1, logp NaN, kept 0.
@@ -126,10 +129,11 @@ typedef struct {
 } gwtf_learn_tensor_t;
 
 /* Makes a list of tensors, a HOST array, on the handle's GPU: a table of where
- * they lie, 80 bytes a tensor and 4 for each 2048 of its values, which the calls that are given the list
- * read.  All arrays have to stay where they are as long as the list is in use.  With
- * GWTF_STATE_NONE of a tensor size, grad_type and grad count alone.  At
- * most 2^42 values in all. */
+ * they lie, 80 bytes a tensor and 4 for each 2048 of its values, which the calls
+ * that are given the list read.  All arrays have to stay where they are as long
+ * as the list is in use, and none that a step writes may overlap another.  With
+ * GWTF_STATE_NONE of a tensor size, grad_type and grad count alone.  At most 2^42
+ * values in all.  Lists are made and destroyed outside of stream captures. */
 gwtf_status_t gwtf_learn_list_create(gwtf_learn_t *h, int64_t num_tensors, const gwtf_learn_tensor_t *tensors, int32_t form,
                                      gwtf_learn_list_t **out);
 

@@ -49,6 +49,9 @@ __device__ __forceinline__ float value_of(uint32_t k)
     return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
 }
 
+// The largest number below a key's (0 has two keys).
+__device__ __forceinline__ float below(uint32_t k) { return value_of(k - (k == 0x80000000u ? 2u : 1u)); }
+
 // 2^y, 0 <= y < 1, by the exponential's series, to about 1e-15.
 __device__ __forceinline__ double exp2_series(double y)
 {
@@ -926,7 +929,7 @@ __global__ __launch_bounds__(WAVES * 64) void sample_kernel(SampleArgs p)
     Cut cut = {kNoneKey, 0, F};
     bool summed = false;
     row.c = kTable * kLog2e64 / (T_ > 1e-300 ? T_ : 1e-300);
-    row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), value_of(key - 1));
+    row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), below(key));
     if (T_ == 0.0 || top_k == 1 || top_p == 0.0) {
         cut = {key, 1, 1};
     } else {
@@ -1168,7 +1171,7 @@ __global__ __launch_bounds__(WAVES * 64) void sample_open_kernel(SampleArgs p)
         }
         return;
     }
-    row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), value_of(key - 1));
+    row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), below(key));
     const Cut cut = {kNoneKey, 0, F};
     if (threadIdx.x == 0 && a.kept) a.kept[i] = int32_t(F);
     if (row.wave == 0) {
@@ -1240,7 +1243,7 @@ __global__ __launch_bounds__(WAVES * 64) void sample_recheck_kernel(SampleArgs p
         const uint32_t key = p.ws.key[i];
         row.top = value_of(key);
         row.c = kTable * kLog2e64 / a.temperature;
-        row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), value_of(key - 1));
+        row.zero = fminf(float(double(row.top) - kTable * 1000.0 / row.c), below(key));
         double u = a.uniform_type == GWTF_UNIFORM_F64 ? static_cast<const double *>(a.u)[i] : double(static_cast<const float *>(a.u)[i]);
         u = u >= 0.0 ? u : 0.0;
         const Cut cut = {kNoneKey, 0, 1};

@@ -128,7 +128,8 @@ class Parameters:
 
     The lists hold the memory that the tensors had when they were given, and
     keep it: gradients are written into the same tensors at every step
-    (accumulated, or copied), and a parameter that is to live elsewhere needs a new list."""
+    (accumulated, or copied), and a parameter that is to live elsewhere needs a new list.
+    Lists are made, and given up, outside of stream captures."""
 
     def __init__(self, owner, lists, form, array):
         self.list = None

@@ -654,3 +654,16 @@ def test_sample_many_rows_again_and_captured():
             assert all(torch.equal(a, b) for a, b in zip(out, want))
             assert all(torch.equal(a, b) for a, b in zip(o.sample(source, u), want))
         del graph
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t", [1e-300, 1e-45, 1e-20, 1e-3])
+def test_sample_largest_zero_and_small_temperatures(ops, dtype, t):
+    """Rows whose largest entry is 0, of either sign, at temperatures that leave it alone or nearly so."""
+    v = 3000
+    x = -logits(5, v, dtype, 50).abs() - 1e-3
+    x[0, 7], x[1, 8], x[1, 9] = 0.0, -0.0, 0.0
+    x[2] = 0.0
+    x[3, 100] = -1e-38
+    for kw in (dict(), dict(top_k=2), dict(top_p=0.5), dict(min_p=0.5), dict(top_k=2000, top_p=0.9)):
+        check_rows(ops, x, uniform(5, 51), temperature=t, **kw)
