@@ -1005,12 +1005,12 @@ __device__ __forceinline__ float min3(float a, float b, float c)
 // T), and the mean of -log2 w under the shares w / A is their entropy less log2 A, log2
 // V - log2 A at most.  So A is off by at most A 2^-24 (2 ln 2 (log2 V - log2 A + kAbove +
 // 1) + 12), B likewise, and near a border A = u W, B = (1 - u) W.
-// Otherwise (one row in fifteen of normal logits of deviation 2.5 and 131,072 columns),
+// Otherwise (one row in twenty of normal logits of deviation 2.5 and 131,072 columns),
 // and where the largest x c is beyond kRange, the sums are taken again in 64 bits.  r is
 // never below -kRange, so that entries further down, masks of -1e30 among them, add
 // nothing.
 constexpr float kRange = 0x1p17f;
-constexpr float kAbove = 4.f;
+constexpr float kAbove = 1.f;
 constexpr int kOpenPer = 2;                              // steps of a segment
 constexpr int64_t kOpenMost = 1024 * kOpenPer * kStepCols; // columns
 

@@ -47,9 +47,9 @@ def logits(n, v, dtype, seed, pad=0, offset=0, std=2.5):
 
 def open_error(v):
     """Where nothing is filtered logp's sum W is of 32-bit terms: of a term 2^y two roundings of y, the exponential's
-    2^-23, ten of additions, so that with |y| <= 5 + |log2 w| and the mean of |log2 w| <= log2 V - log2 W <= log2 V
-    the sum, and with it the logarithm, is off by 2^-24 (2 ln 2 (log2 V + 5) + 12) at most."""
-    return 2.0 ** -24 * (2 * math.log(2) * (math.log2(v) + 5) + 12)
+    2^-23, ten of additions, so that with |y| <= 2 + |log2 w| and the mean of |log2 w| <= log2 V - log2 W <= log2 V
+    the sum, and with it the logarithm, is off by 2^-24 (2 ln 2 (log2 V + 2) + 12) at most."""
+    return 2.0 ** -24 * (2 * math.log(2) * (math.log2(v) + 2) + 12)
 
 
 def check_rows(ops, x, u, **kw):
