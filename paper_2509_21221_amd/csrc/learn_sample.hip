@@ -85,36 +85,6 @@ struct Series {
 constexpr double kZ = kLn264 / kTable;
 constexpr Series kSeries = {kZ, kZ * kZ / 2, kZ * kZ * kZ / 6, kZ * kZ * kZ * kZ / 24, 0x1.8p52};
 
-// Sums over the wave, uniform, without a way through LDS.
-template <int n>
-__device__ __forceinline__ double row_ror64(double v)
-{
-    const uint64_t b = __builtin_bit_cast(uint64_t, v);
-    const uint32_t lo = uint32_t(row_ror<n>(int(uint32_t(b)))), hi = uint32_t(row_ror<n>(int(uint32_t(b >> 32))));
-    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
-}
-__device__ __forceinline__ double lane_value64(double v, int lane)
-{
-    const uint64_t b = __builtin_bit_cast(uint64_t, v);
-    const uint32_t lo = __builtin_amdgcn_readlane(uint32_t(b), lane), hi = __builtin_amdgcn_readlane(uint32_t(b >> 32), lane);
-    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
-}
-__device__ __forceinline__ double wave_sum64(double v)
-{
-    v += row_ror64<8>(v);
-    v += row_ror64<4>(v);
-    v += row_ror64<2>(v);
-    v += row_ror64<1>(v);
-    return (lane_value64(v, 0) + lane_value64(v, 16)) + (lane_value64(v, 32) + lane_value64(v, 48));
-}
-__device__ __forceinline__ uint32_t wave_add(uint32_t v)
-{
-    v += uint32_t(row_ror<8>(int(v)));
-    v += uint32_t(row_ror<4>(int(v)));
-    v += uint32_t(row_ror<2>(int(v)));
-    v += uint32_t(row_ror<1>(int(v)));
-    return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) + (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
-}
 __device__ __forceinline__ uint32_t scan_up(uint32_t v, int lane) // sums over lanes 0 .. lane
 {
 #pragma unroll

