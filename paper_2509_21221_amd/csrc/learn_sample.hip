@@ -185,7 +185,8 @@ struct Row {
         r = __builtin_bit_cast(typename Vec8<T>::type, w);
     }
     // f(eight's number s, first column, eight values) for every eight of this lane, done(segment) at a segment's
-    // end.  With `bound` eights are left out where all of a wave's are below.
+    // end.  With `bound` eights are left out where all of a wave's are below; at the first look (S = 0: with a
+    // bound of -infinity) none is, eights of nothing but NaN neither.
     template <class F, class D>
     __device__ __forceinline__ void scan(float bound, F f, D done)
     {
@@ -228,7 +229,7 @@ struct Row {
                     most = v[0];
 #pragma unroll
                     for (int i = 1; i < kVec; ++i) most = fmaxf(most, v[i]);
-                    if (__ballot(most >= bound)) f(0, col, v);
+                    if (__ballot(!(most < bound))) f(0, col, v); // (NaN is not below)
                     if (++q == per) {
                         done(seg);
                         q = 0;
