@@ -142,7 +142,7 @@ void gwtf_learn_list_destroy(gwtf_learn_list_t *list);
 
 /* norm = scale * sqrt(sum of the squares of all gradients) and
  * factor = scale * min(1, max_norm / norm), NaN where norm is not a finite
- * number: what the gradients are to be multiplied with, for gwtf_learn_adamw.
+ * number of 32 bits: what the gradients are to be multiplied with, for gwtf_learn_adamw.
  * Sums are held in 64 bits.  The list may have any form. */
 typedef struct {
     const gwtf_learn_list_t *list;

@@ -55,7 +55,7 @@ def sample_row(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
 
 def grad_norm(grads, max_norm=np.inf, scale=1.0):
     norm = scale * np.sqrt(sum(np.sum(np.asarray(g, np.float64) ** 2) for g in grads))
-    if not np.isfinite(norm):
+    if not norm < 2.0 ** 128 - 2.0 ** 103:  # infinite in 32 bits
         return norm, np.nan
     return norm, scale * (min(1.0, max_norm / norm) if norm > 0 else 1.0)
 

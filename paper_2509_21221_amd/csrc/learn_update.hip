@@ -80,8 +80,9 @@ __global__ __launch_bounds__(256) void norm_kernel(const LearnEntry *__restrict_
     if (threadIdx.x) return;
     *a.arrived = 0;
     const double n = a.scale * sqrt((red[0] + red[1]) + (red[2] + red[3]));
-    if (a.norm) *a.norm = float(n);
-    if (a.factor) *a.factor = n < __builtin_inf() ? float(n > a.max_norm ? a.scale * (a.max_norm / n) : a.scale) : __builtin_nanf("");
+    const float norm = float(n); // infinite where 32 bits do not hold it: no gradient is to be clipped by such
+    if (a.norm) *a.norm = norm;
+    if (a.factor) *a.factor = norm < __builtin_inff() ? float(n > a.max_norm ? a.scale * (a.max_norm / n) : a.scale) : __builtin_nanf("");
 }
 
 __global__ void norm_of_nothing_kernel(float scale, float *norm, float *factor)
