@@ -158,7 +158,7 @@ class LearnOps:
     tensors are returned unless ``out`` is given; autograd is not involved.  Work
     runs on ``stream`` (by default the current one when the object is made);
     called on another stream, an operator waits for that stream first and that
-    stream waits for it.  Calls that are captured into a graph need an object
+    stream waits for it; so do the states that ``parameters`` makes.  Calls that are captured into a graph need an object
     made with the capturing stream; step number and learning rate can be device
     tensors there, which a replay reads anew.
     """
@@ -302,6 +302,17 @@ class LearnOps:
         default.  With ``params`` None the list is for ``grad_norm`` alone."""
         if self.handle is None:
             raise RuntimeError("LearnOps: closed")
+        # states are made, and copies taken, in the order of the object's stream: after its pending steps and before the next
+        here = self.torch.cuda.current_stream(self.device)
+        if here.cuda_stream == self._raw:
+            return self._parameters(params, grads, bits, moments, scales, master, weight_decay, sites)
+        self.stream.wait_stream(here)
+        with self.torch.cuda.stream(self.stream):
+            made = self._parameters(params, grads, bits, moments, scales, master, weight_decay, sites)
+        here.wait_stream(self.stream)
+        return made
+
+    def _parameters(self, params, grads, bits, moments, scales, master, weight_decay, sites):
         torch, types = self.torch, tuple(self._types)
         f32 = torch.float32
         if params is None:
