@@ -159,8 +159,8 @@ gwtf_status_t gwtf_learn_grad_norm(gwtf_learn_t *h, const gwtf_learn_grad_norm_t
  *   p = p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay p)
  * where p is master, rounded to param too, or param itself where master is
  * NULL, and a denominator below 2^-126 counts as 2^-126 (with eps 0, values whose
- * gradients have all been 0 stay).  With a factor that is not a finite number
- * nothing is written.
+ * gradients have all been 0 stay).  With a factor, or a rate at lr_at, that is not a
+ * finite number, or a step number below 1 at step_at, nothing is written.
  *
  * GWTF_STATE_F8: m and v are values times the scale of their block, a power of
  * two that puts the block's largest magnitude into (224, 448] of m, (28672, 57344]

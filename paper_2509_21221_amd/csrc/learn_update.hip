@@ -195,10 +195,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a)
     const float factor = a.factor ? *a.factor : 1.f;
     if (!(__builtin_fabsf(factor) < __builtin_inff())) return;
     const float lr = a.lr_at ? *a.lr_at : a.lr;
+    if (!(__builtin_fabsf(lr) < __builtin_inff())) return;
     int64_t step = a.step;
     float unbias1 = a.unbias1, unbias2 = a.unbias2; // 1 / (1 - beta^step)
     if (a.step_at) {
         step = *a.step_at;
+        if (step < 1) return;
         unbias1 = float(-1.0 / expm1(double(step) * a.log_beta1));
         unbias2 = float(-1.0 / expm1(double(step) * a.log_beta2));
     }

@@ -396,8 +396,8 @@ class LearnOps:
     def adamw(self, group, lr, step, betas=(0.9, 0.999), eps: float = 1e-8, factor=None, seed: int = 0):
         """One AdamW step on all parameters of ``group``, in place.  ``lr`` and
         ``step`` (1 for the first) are numbers or device tensors of one (float32, int64);
-        ``factor``: ``grad_norm``'s, one that is not finite leaves everything
-        as it was; ``seed``: of 8-bit states' rounding."""
+        ``factor``: ``grad_norm``'s.  A factor or a device tensor's rate that is not finite, and
+        a device tensor's step below 1, leave everything as it was.  ``seed``: of 8-bit states' rounding."""
         table = self._group(group)
         if not 0 <= seed < 1 << 64:
             raise ValueError("seed must fit in 64 bits and be >= 0")
