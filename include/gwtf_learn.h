@@ -147,7 +147,7 @@ void gwtf_learn_list_destroy(gwtf_learn_list_t *list);
 typedef struct {
     const gwtf_learn_list_t *list;
     double max_norm; /* >= 0; +infinity: no bound */
-    double scale;    /* finite, >= 0 */
+    double scale;    /* finite in 32 bits, >= 0 */
     float *norm;     /* [1], or NULL */
     float *factor;   /* [1], or NULL */
 } gwtf_learn_grad_norm_t;
@@ -177,10 +177,10 @@ typedef struct {
     const gwtf_learn_list_t *list; /* of GWTF_STATE_F32 or GWTF_STATE_F8 */
     int64_t step;                  /* >= 1, number of this step */
     const int64_t *step_at;        /* [1], to be read in its place, or NULL */
-    double lr;                     /* finite */
+    double lr;                     /* finite in 32 bits */
     const float *lr_at;            /* [1], to be read in its place, or NULL */
     double beta1, beta2;           /* within [0, 1), in 32 bits too */
-    double eps;                    /* finite, >= 0 */
+    double eps;                    /* finite in 32 bits, >= 0 */
     uint64_t seed;                 /* with GWTF_STATE_F8 only */
     const float *factor;           /* [1], or NULL = 1 */
 } gwtf_learn_adamw_t;

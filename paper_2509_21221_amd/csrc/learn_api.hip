@@ -47,6 +47,9 @@ gwtf_status_t fail(gwtf_learn_t *h, gwtf_status_t code, const char *what, hipErr
     const hipError_t e = (expr);                                                        \
     return e == hipSuccess ? GWTF_OK : fail(h, GWTF_ERR_DEVICE, name " launch", e);
 
+// A number that a kernel takes in 32 bits: finite there too.
+bool finite32(double v) { return std::isfinite(v) && std::isfinite(float(v)); }
+
 constexpr int64_t kTensorSize = int64_t(1) << 35, kListSize = int64_t(1) << 42;
 
 // What is wrong with a tensor of a list.
@@ -198,7 +201,7 @@ extern "C" gwtf_status_t gwtf_learn_grad_norm(gwtf_learn_t *h, const gwtf_learn_
     LEARN_REQUIRE(a->list, "list is NULL")
     LEARN_REQUIRE(a->list->device == h->device, "the list is on another device")
     LEARN_REQUIRE(a->max_norm >= 0, "max_norm must be >= 0")
-    LEARN_REQUIRE(a->scale >= 0 && std::isfinite(a->scale), "scale must be finite and >= 0")
+    LEARN_REQUIRE(a->scale >= 0 && finite32(a->scale), "scale must be finite in 32 bits and >= 0")
     LEARN_CHECK(a->norm ? bad_vector(a->norm, 1, 4) : nullptr)
     LEARN_CHECK(a->factor ? bad_vector(a->factor, 1, 4) : nullptr)
     if (!a->norm && !a->factor) return GWTF_OK;
@@ -212,9 +215,9 @@ extern "C" gwtf_status_t gwtf_learn_adamw(gwtf_learn_t *h, const gwtf_learn_adam
     LEARN_REQUIRE(a->list->device == h->device, "the list is on another device")
     LEARN_REQUIRE(a->list->t.form != GWTF_STATE_NONE, "the list has gradients alone")
     LEARN_REQUIRE(a->step_at || a->step >= 1, "step below 1")
-    LEARN_REQUIRE(a->lr_at || std::isfinite(a->lr), "lr must be finite")
+    LEARN_REQUIRE(a->lr_at || finite32(a->lr), "lr must be finite in 32 bits")
     LEARN_REQUIRE(a->beta1 >= 0 && float(a->beta1) < 1 && a->beta2 >= 0 && float(a->beta2) < 1, "beta1 or beta2 outside [0, 1)")
-    LEARN_REQUIRE(a->eps >= 0 && std::isfinite(a->eps), "eps must be finite and >= 0")
+    LEARN_REQUIRE(a->eps >= 0 && finite32(a->eps), "eps must be finite in 32 bits and >= 0")
     LEARN_CHECK(a->step_at ? bad_vector(a->step_at, 1, 8) : nullptr)
     LEARN_CHECK(a->lr_at ? bad_vector(a->lr_at, 1, 4) : nullptr)
     LEARN_CHECK(a->factor ? bad_vector(a->factor, 1, 4) : nullptr)

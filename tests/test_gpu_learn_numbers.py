@@ -13,6 +13,7 @@ if have_gpu():
     import torch
 
     from paper_2509_21221_amd.learn import LearnOps
+    from paper_2509_21221_amd.mcf import GwtfError
 
 
 @pytest.mark.parametrize("bits,master", itertools.product((32, 8), (False, True)))
@@ -64,3 +65,22 @@ def test_captured_counter_that_moves_after_the_step():
             torch.cuda.synchronize()
             runs.append([t.clone().view(torch.uint8) for t in group.tensors])
     assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+def test_numbers_that_are_infinite_in_32_bits_are_refused(ops):  # noqa: F811
+    s = state([64], "bf16", "f32", 32, False, 24)
+    group = group_of(ops, s)
+    before = [t.clone().view(torch.uint8) for t in group.tensors]
+    most = 2.0 ** 128 - 2.0 ** 104
+    for kw, match in ((dict(lr=1e39), "lr"), (dict(lr=-1e39), "lr"), (dict(lr=2.0 ** 128), "lr"), (dict(eps=1e39), "eps"),
+                      (dict(eps=most * (1 + 2.0 ** -24)), "eps")):
+        with pytest.raises(GwtfError, match=match):
+            ops.adamw(group, **{**dict(lr=1e-3, step=1), **kw})
+    with pytest.raises(GwtfError, match="scale"):
+        ops.grad_norm(group, 1.0, scale=1e39)
+    with pytest.raises(GwtfError, match="weight_decay"):
+        group_of(ops, s, weight_decay=1e39)
+    assert all(torch.equal(a.view(torch.uint8), b) for a, b in zip(group.tensors, before))
+    ops.adamw(group, 1e-3, 1, eps=most)  # the largest number is one: a step of nothing but the decay
+    assert torch.equal(s["params"][0].view(torch.uint8), before[0])
+    ops.grad_norm(group, 1e300, scale=most)
