@@ -129,14 +129,19 @@ class Parameters:
     The lists hold the memory that the tensors had when they were given, and
     keep it: gradients are written into the same tensors at every step
     (accumulated, or copied), and a parameter that is to live elsewhere needs a new list.
-    Lists are made, and given up, outside of stream captures."""
+    Lists are made, and given up, outside of stream captures.
 
-    def __init__(self, owner, lists, form, array):
+    A step moves the versions of ``params`` and ``master``, so that a backward pass
+    of a graph that has kept the old values is refused, as after any change in place (a
+    replayed capture moves none: it is the graph's owner who orders it)."""
+
+    def __init__(self, owner, lists, form, array, versions=()):
         self.list = None
         self.owner = owner
         self.params, self.grads, self.m, self.v, self.m_scales, self.v_scales, self.master = lists
         self.form = form
         self.tensors = [t for one in lists if one for t in one]
+        self.versions = versions  # of what a step writes and a graph may have kept, tensors that carry them
         self.list = gwtf_learn_list_create(owner.handle, array, form)
 
     def __del__(self):
@@ -158,9 +163,9 @@ class LearnOps:
     tensors are returned unless ``out`` is given; autograd is not involved.  Work
     runs on ``stream`` (by default the current one when the object is made);
     called on another stream, an operator waits for that stream first and that
-    stream waits for it; so do the states that ``parameters`` makes.  Calls that are captured into a graph need an object
-    made with the capturing stream; step number and learning rate can be device
-    tensors there, which a replay reads anew.
+    stream waits for it; so do the states that ``parameters`` makes.  Calls that
+    are captured into a graph need an object made with the capturing stream; step
+    number and learning rate can be device tensors there, which a replay reads anew.
     """
 
     def __init__(self, device: int = 0, stream=None):
@@ -175,6 +180,7 @@ class LearnOps:
         self._types = {torch.float32: GWTF_TYPE_F32, torch.float16: GWTF_TYPE_F16, torch.bfloat16: GWTF_TYPE_BF16}
         self._uniforms = {torch.float32: GWTF_UNIFORM_F32, torch.float64: GWTF_UNIFORM_F64}
         self._current = torch._C._cuda_getCurrentRawStream  # the current stream without an object for it
+        self._written = torch.autograd.graph.increment_version
         self._f32 = torch.empty(0, dtype=torch.float32, device=self._dev)
         self._i32 = torch.empty(0, dtype=torch.int32, device=self._dev)
         lib = _library()
@@ -203,7 +209,11 @@ class LearnOps:
             return 0, v.data_ptr()
         return v, None
 
-    def _run(self, name, args, tensors):
+    def _given(self, out):
+        """Results that the caller gave have been written."""
+        self._written([t for t in out if t is not None and not t.is_inference()])
+
+    def _run(self, name, args, tensors, group=None):
         if self.handle is None:
             raise RuntimeError("LearnOps: closed")
         if self._current(self.device) == self._raw:
@@ -215,7 +225,7 @@ class LearnOps:
         self.stream.wait_stream(here)
         _check(self._calls[name](self.handle, args), self.handle)
         here.wait_stream(self.stream)
-        for t in tensors:
+        for t in (*tensors, *(group.tensors if group is not None else ())):
             if isinstance(t, self.torch.Tensor):
                 t.record_stream(self.stream)
 
@@ -246,7 +256,8 @@ class LearnOps:
         q, qs = self._setting(min_p, n, f32, "min_p")
         if not 0 <= k < 1 << 31:
             raise ValueError("top_k: outside [0, 2^31)")
-        if out is None:
+        given = out is not None
+        if not given:
             ids, logp, kept = out = self._i32.new_empty(n), self._f32.new_empty(n), self._i32.new_empty(n)
             to = ids.data_ptr(), logp.data_ptr(), kept.data_ptr()
         else:
@@ -256,6 +267,8 @@ class LearnOps:
         a = gwtf_learn_sample_t(n, v, self._types[logits.dtype], self._uniforms[u.dtype], k, t, p, q, ts, ks, ps, qs,
                                 logits.data_ptr(), stride, self._vec(u, n, u.dtype, "u"), *to)
         self._run("sample", a, (logits, u, temperature, top_k, top_p, min_p, ids, logp, kept))
+        if given:
+            self._given(out)
         return out
 
     # ---- update phase ----
@@ -323,7 +336,8 @@ class LearnOps:
             return Parameters(self, (None, grads, None, None, None, None, None), GWTF_STATE_NONE, array)
         if bits not in (8, 32):
             raise ValueError("bits: 8 or 32")
-        params = self._list(params, None, types, "params")
+        given = list(params)
+        params = self._list(given, None, types, "params")
         grads = self._list(grads, params, types, "grads")
         for i, (p, g) in enumerate(zip(params, grads)):
             if g.dtype not in (p.dtype, f32):
@@ -347,10 +361,14 @@ class LearnOps:
             if scales is None:
                 scales = [[torch.ones(b.shape, dtype=f32, device=self._dev) for b in blocks] for _ in kinds]
             ms, vs = (self._list(one, blocks, (f32,), name) for one, name in zip(scales, ("m_scale", "v_scale")))
+        # views of one tensor share its version
+        versions = {id(t if t._base is None else t._base): p for t, p in zip(given, params)}
         if master is True:
             master = [p.to(f32, copy=True) for p in params]
         elif master is not None and master is not False:
-            master = self._list(master, params, (f32,), "master")
+            given = list(master)
+            master = self._list(given, params, (f32,), "master")
+            versions.update({id(t if t._base is None else t._base): p for t, p in zip(given, master)})
         else:
             master = None
         n = len(params)
@@ -371,7 +389,8 @@ class LearnOps:
             if bits == 8:
                 a.m_scale, a.v_scale = ms[i].data_ptr(), vs[i].data_ptr()
             a.weight_decay, a.site = decay[i], sites[i]
-        return Parameters(self, (params, grads, m, v, ms, vs, master), GWTF_STATE_F8 if bits == 8 else GWTF_STATE_F32, array)
+        return Parameters(self, (params, grads, m, v, ms, vs, master), GWTF_STATE_F8 if bits == 8 else GWTF_STATE_F32, array,
+                          tuple(t for t in versions.values() if not t.is_inference()))
 
     def _group(self, group):
         if self.handle is None:
@@ -384,13 +403,16 @@ class LearnOps:
         """(norm, factor), float32 tensors of one: ``scale`` times the norm of
         all gradients of ``group``, and what they are to be multiplied with so
         that it is at most ``max_norm``; NaN where the norm is not finite."""
-        if out is None:
+        given = out is not None
+        if not given:
             out = self._f32.new_empty(1), self._f32.new_empty(1)
         norm, factor = out
         f32 = self.torch.float32
         a = gwtf_learn_grad_norm_t(self._group(group), max_norm, scale, None if norm is None else self._vec(norm, 1, f32, "norm"),
                                    None if factor is None else self._vec(factor, 1, f32, "factor"))
-        self._run("grad_norm", a, (*group.tensors, norm, factor) if self._current(self.device) != self._raw else ())
+        self._run("grad_norm", a, (norm, factor), group)
+        if given:
+            self._given(out)
         return out
 
     def adamw(self, group, lr, step, betas=(0.9, 0.999), eps: float = 1e-8, factor=None, seed: int = 0):
@@ -407,7 +429,8 @@ class LearnOps:
         step_, step_at = self._one(step, self.torch.int64, "step")
         a = gwtf_learn_adamw_t(table, step_, step_at, lr_, lr_at, betas[0], betas[1], eps, seed,
                                None if factor is None else self._one(factor, self.torch.float32, "factor")[1])
-        self._run("adamw", a, (*group.tensors, lr, step, factor) if self._current(self.device) != self._raw else ())
+        self._run("adamw", a, (lr, step, factor), group)
+        self._written(group.versions)
 
     def close(self):
         if self.handle is not None:
