@@ -170,7 +170,8 @@ gwtf_status_t gwtf_learn_grad_norm(gwtf_learn_t *h, const gwtf_learn_grad_norm_t
  * than half a step of 8 bits moves at all: with r = 16 bits of Philox4x32-10
  * under the key (low, high half of `seed`) and the counter (i / 8, site, low, high
  * half of step), word (i % 8) / 2, its low half for even i, for value i of a
- * tensor, the magnitude in steps of 8 bits plus (r + 0.5) 2^-16 is cut down to a
+ * tensor, the magnitude in steps of 8 bits plus (r + 0.5) 2^-16 (rounded to 32 bits
+ * where the magnitude is below the code's smallest normal number) is cut down to a
  * whole number.  A v above 0 is kept above 0, so that m / sqrt(v) stays bounded.
  * A NaN or infinity among a block's new values makes its scale NaN. */
 typedef struct {

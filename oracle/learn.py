@@ -89,7 +89,7 @@ def draws(size, seed, site, step, first=0):
 
 def narrow(x, r, kind):
     """(values in units of the scale, scales) that 8 bits hold of x: the magnitude in steps, and a remainder of
-    (r + 1/2) 2^-16 steps, cut down to whole steps."""
+    (r + 1/2) 2^-16 steps, cut down to whole steps; the sum is one of 32 bits where steps are the smallest."""
     x = np.asarray(x, np.float64)
     scales = np.empty(-(-len(x) // BLOCK), np.float32)
     out = np.empty(len(x))
@@ -104,7 +104,9 @@ def narrow(x, r, kind):
             e += 1
         a = np.abs(y) * 2.0 ** -e
         step = np.maximum(2.0 ** (np.floor(np.log2(np.maximum(a, 1e-300))) - _MANTISSA[kind]), _LEAST[kind])
-        q = np.floor(a / step + (r[b * BLOCK:(b + 1) * BLOCK] + 0.5) / 65536) * step
+        total = a / step + (r[b * BLOCK:(b + 1) * BLOCK] + 0.5) / 65536
+        normal = _LEAST[kind] * 2.0 ** _MANTISSA[kind]
+        q = np.floor(np.where(a < normal, total.astype(np.float32), total)) * step
         if kind == "e5m2":
             q[(a > 0) & (q == 0)] = _LEAST[kind]
         scales[b], out[b * BLOCK:(b + 1) * BLOCK] = 2.0 ** e, np.where(y < 0, -q, q)
