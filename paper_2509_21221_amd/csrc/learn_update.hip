@@ -168,7 +168,7 @@ __device__ __forceinline__ u32x2 narrow_f8(const float x[8], const uint32_t r[8]
         const float a = __builtin_fabsf(x[i]) * up;
         const uint32_t large = ((__float_as_uint(a) + (r[i] << (CUT - 16)) + (1u << (CUT - 17))) >> CUT) - BIAS;
         uint32_t small = uint32_t(a * UNIT + (float(r[i]) + 0.5f) * 0x1p-16f);
-        if (E5M2 && a > 0.f && small == 0) small = 1;
+        if (E5M2 && x[i] > 0.f && small == 0) small = 1; // (its magnitude under the scale may be 0 in 32 bits)
         uint32_t c = a >= NORMAL ? large : small;
         if (!E5M2) c |= (__float_as_uint(x[i]) >> 24) & (c ? 0x80u : 0u);
         w[i / 4] |= c << (8 * (i & 3));

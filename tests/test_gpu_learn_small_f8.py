@@ -47,3 +47,15 @@ def test_second_moment(ops):  # noqa: F811
     g = np.sqrt(x.astype(np.float64)).astype(np.float32)
     g[::128] = 224.0
     check(ops, g, g * g, r, "v", "e5m2")
+
+
+def test_second_moment_far_below_its_block_stays_above_0(ops):  # noqa: F811
+    """Values that the block's scale takes below the least number of 32 bits, beside 0."""
+    g = np.zeros(N, np.float32)
+    g[::128], g[1::128], g[2::128], g[3::128] = 1e18, 1e-6, 1e-18, 2.0 ** -74  # of 2^-148 the square is one step of 32 bits
+    group = ops.parameters([torch.zeros(N, device="cuda")], [torch.from_numpy(g).cuda()], bits=8, sites=[SITE])
+    ops.adamw(group, 0.0, STEP, betas=(0.0, 0.0), seed=SEED)
+    v = group.v[0].float().view(-1, 128)
+    assert (v[:, 0] > 28672).all() and (v[:, 1:4] == 2.0 ** -16).all() and (v[:, 4:] == 0).all()
+    q, z = O.narrow(g * g, O.draws(N, SEED, SITE, STEP), "e5m2")
+    assert np.array_equal(group.v_scales[0].cpu().numpy(), z) and np.array_equal(group.v[0].double().cpu().numpy(), q)
