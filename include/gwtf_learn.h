@@ -82,8 +82,9 @@ const char *gwtf_learn_last_error(const gwtf_learn_t *h);
  * and of those before it, is above u times that of all:
  *   ids = its index, logp = ln of its share of the sum, kept = how many stay.
  * Sums, w and their products with u and p are held in 64 bits, so that a draw is
- * that of exact arithmetic unless u falls within some 1e-13 of a border, or p
- * within some 1e-11 (V 2^-61 where that is more); a w below 2^-600 may count as 0.  logp is rounded once from 64
+ * that of exact arithmetic unless u falls within some 1e-13 of a border, p
+ * within some 1e-11 (V 2^-61 where that is more), or q, below 1, within 1e-13 of itself of
+ * a w; a w below 2^-600 may count as 0.  logp is rounded once from 64
  * bits, but where nothing is filtered (the numbers top_k <= 0, top_p >= 1, min_p 0)
  * it comes from a sum that is off by 2^-24 (2 ln 2 (log2 V + 2) + 12) of itself at most.
  * u counts as within [0, 1)

@@ -879,6 +879,11 @@ struct Row {
             n_p += in && at < target ? 1u : 0u;
             n_q += in && w[q] >= min_p ? 1u : 0u;
         }
+        if (min_p == 1.0) { // a w just below 1 may be 1 in 64 bits
+            n_q = 0;
+#pragma unroll
+            for (int q = 0; q < kEach; ++q) n_q += j0 + q < K && uint32_t(e[q] >> 32) == key_of(top) ? 1u : 0u;
+        }
         n_p = top_p < 1.0 ? wave_add(n_p) + 1u : K;
         n_q = wave_add(n_q);
         uint32_t n = n_p < n_q ? n_p : n_q;
