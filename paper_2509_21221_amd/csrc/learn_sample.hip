@@ -450,24 +450,25 @@ struct Row {
     }
 
     // The bin of an entry by its distance from the largest: kBins - 1 at the top, 0 at
-    // kSpan bits of w and further down.  Temperatures whose quotients leave 32 bits tell
-    // entries apart that are next to 0 or not at all: there the distance is taken 2^100 times, where it
-    // stays within 32 bits.
+    // kSpan bits of w and further down.  The smallest temperatures tell entries apart that are next to
+    // 0 or not at all: there the distance is taken 2^100 times.  The largest tell entries apart whose
+    // distance 32 bits do not hold: there a quarter of it is taken.
     static constexpr int kSpan = 48;
     struct Distance {
-        float far, from, scale; // far: 1 or 2^100
+        float far, near, from, scale; // far: 1, 2^100 or 2^-2, near: its reciprocal
     };
     __device__ __forceinline__ Distance distance() const
     {
         const double scale = c * (double(kBins) / (kTable * kSpan));
-        const float far = scale > 1e38 && fabsf(top) < 0x1p20f ? 0x1p100f : 1.f;
-        return {far, top * far, float(fmin(scale / double(far), 0x1p127))};
+        const bool cold = scale > 1e38 && fabsf(top) < 0x1p20f, hot = scale < 1e-30;
+        const float far = cold ? 0x1p100f : hot ? 0.25f : 1.f, near = cold ? 0x1p-100f : hot ? 4.f : 1.f;
+        return {far, near, top * far, float(fmin(scale * double(near), 0x1p127))};
     }
     static __device__ __forceinline__ uint32_t bin_of(float v, const Distance &d)
     {
         return uint32_t(kBins - 1) - uint32_t(fminf(fmaf(v, -d.far, d.from) * d.scale, float(kBins - 1)));
     }
-    // No w of a bin passes 2^-shift, and but for bin 0 none is half of that.
+    // No w of a bin passes 2^-shift (but by some 1e-5 of it), and but for bin 0 none is much below half of that.
     static __device__ __forceinline__ uint32_t shift_of(uint32_t bin) { return (kBins - 1 - bin) * uint32_t(kSpan / 16) / uint32_t(kBins / 16); }
 
     // The cut after the least number of entries whose sum of w reaches the target, or (whole_row) top_p
@@ -531,7 +532,7 @@ struct Row {
         const uint32_t bin = kBins - 1 - first, L = uniform(sh.bin.count), above = uniform(sh.bin.above);
         const double above_mass = uniform(sh.bin.above_mass);
         // nothing of the bin is below this
-        const float low = bin ? top - (float(kBins - bin) * 1.0001f + 1.f) / dist.scale / dist.far : -__builtin_inff();
+        const float low = bin ? top - (float(kBins - bin) * 1.0001f + 1.f) / dist.scale * dist.near : -__builtin_inff();
         const float bound = fmaxf(low, value_of(kNoneKey + 1));
         if (L > uint32_t(kList)) {
             // the bin's keys, no entry of another bin among them

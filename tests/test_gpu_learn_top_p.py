@@ -128,3 +128,18 @@ def test_all_equal(ops):  # noqa: F811
             got = ops.sample(x, u, top_p=p)
             check_kept(x, u, got, top_p=p)
             assert (got[2] == int(np.ceil(v * p))).all()  # v p is far from a whole number, or is one
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t", [1e30, 1e36, 2e37, 1e38, 1e39, 1e45, 1e300])
+def test_distances_beyond_32_bits(ops, dtype, t):  # noqa: F811
+    """Entries whose distance from the largest 32 bits do not hold, at temperatures that weigh them."""
+    rng = np.random.default_rng(11)
+    v = 5000
+    x = np.stack((np.where(rng.random(v) < 0.3, 3e38, -3e38), rng.uniform(-3.3e38, 3.3e38, v), np.where(np.arange(v) == 9, 3.3e38, -3.3e38),
+                  np.where(rng.random(v) < 0.5, 1.0, -3.3e38)))
+    x = dev(x.astype(np.float32), DT[dtype])
+    x[1, 100:200] = float("-inf")
+    u = uniform(4, 12)
+    for kw in (dict(top_p=0.5), dict(top_p=0.9), dict(top_p=1 - 1e-9), dict(top_p=0.7, top_k=1000), dict(top_p=0.7, top_k=4500)):
+        check_kept(x, u, ops.sample(x, u, temperature=t, **kw), temperature=t, **kw)
