@@ -361,16 +361,17 @@ class LearnOps:
             if scales is None:
                 scales = [[torch.ones(b.shape, dtype=f32, device=self._dev) for b in blocks] for _ in kinds]
             ms, vs = (self._list(one, blocks, (f32,), name) for one, name in zip(scales, ("m_scale", "v_scale")))
-        # views of one tensor share its version
-        versions = {id(t if t._base is None else t._base): p for t, p in zip(given, params)}
         if master is True:
             master = [p.to(f32, copy=True) for p in params]
+            given += master
         elif master is not None and master is not False:
-            given = list(master)
-            master = self._list(given, params, (f32,), "master")
-            versions.update({id(t if t._base is None else t._base): p for t, p in zip(given, master)})
+            copies = list(master)
+            master = self._list(copies, params, (f32,), "master")
+            given += copies
         else:
             master = None
+        # of what a step writes; views of one tensor share its version
+        versions = {id(t if t._base is None else t._base): w for t, w in zip(given, [*params, *(master or ())])}
         n = len(params)
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
         sites = list(range(n)) if sites is None else list(sites)

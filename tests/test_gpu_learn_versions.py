@@ -73,3 +73,16 @@ def test_inference_tensors(ops):  # noqa: F811
     ops.adamw(group, 1e-2, 2)
     ops.sample(x, u, out=out)
     assert p.is_inference() and (p < 0.99).all()
+
+
+def test_versions_of_copies_that_the_list_makes(ops):  # noqa: F811
+    p, g = torch.ones(9, device="cuda").bfloat16(), torch.ones(9, device="cuda")
+    group = ops.parameters([p], [g], master=True)
+    scale = torch.ones(9, device="cuda", requires_grad=True)
+    kept = (scale * group.master[0]).sum()
+    ops.adamw(group, 1e-2, 1)
+    with pytest.raises(RuntimeError, match="inplace"):
+        kept.backward()
+    empty = ops.parameters([], [])
+    ops.adamw(empty, 1e-2, 1)
+    assert empty.versions == ()
