@@ -2,12 +2,14 @@
 import pytest
 
 from tests.gpu_util import have_gpu
-from tests.test_gpu_learn import DT, ops, uniform  # noqa: F401
+from tests.test_gpu_learn import ops, uniform  # noqa: F401
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not have_gpu(), reason="no GPU")]
 
 if have_gpu():
     import torch
+
+    from tests.test_gpu_learn import DT
 
 
 @pytest.mark.parametrize("dtype,v", [("f32", 3000), ("bf16", 300), ("f32", 70000), ("bf16", 40000)])
