@@ -13,19 +13,20 @@
 // index.  A cut by number or by sum is found by counting keys in equal bins
 // between two bounds (and adding up w, as whole numbers, so that the order of the
 // additions does not matter), and again within the bin that the cut falls into,
-// until a bin is one key.  Whole numbers of one unit would lose what is far below the largest, so
-// sums of many entries are first taken in bins by distance from it, each in a unit of its own.  The draw needs no order: sums of what stays over
-// segments of the row, then a prefix within the segment that u falls into.
+// until a bin is one key.  Whole numbers of one unit would lose what is far below the
+// largest, so sums of many entries are first taken in bins by distance from it, each in a
+// unit of its own.  The draw needs no order: sums of what stays over segments of the row,
+// then a prefix within the segment that u falls into.
 //
 // With top_k up to kFew the k-th largest of the eights' largest entries is a bound
 // that about k entries reach; they are ranked by comparison, and one wave does the rest.
-// With top_p the entries of one such bin are ranked.  Rows without a filter take one reading with 32-bit
-// sums (sample_open_kernel).
+// With top_p the entries of one such bin are ranked.  Rows without a filter take one
+// reading with 32-bit sums (sample_open_kernel).
 //
 // Few rows are bound by what follows one another on a row's own compute unit: the
 // reading, 64-bit weights at some 20 instructions each, a dozen barriers (7 x
 // 131,072 bf16, top_k 50 with top_p and min_p 23 us; 64 x 32,000 f16, top_p 0.95 35; 255 x 50,001 f32,
-// each row its own settings 49; 1 x 32,001 f32 without a filter 8).  Many rows without
+// each row its own settings 51; 1 x 32,001 f32 without a filter 8).  Many rows without
 // a filter: 1,024 x 131,072 bf16 59 us (268 MB, 4.5 TB/s; memory and vector issue alike, eight issue
 // slots an entry) and 24 for the rows that are left uncertain.
 #include "learn_internal.h"
@@ -120,7 +121,7 @@ struct Cut {
 
 constexpr int kBins = 2048;
 constexpr int kAhead = 4;  // steps that a wave has in flight
-constexpr int kFew = 256;  // top_k up to which the entries are ranked
+constexpr int kFew = 256;  // top_k up to which the entries are ranked (64 x 131,072 bf16, 256 40 us; 300, searched by key, 49)
 constexpr int kList = 512; // entries that can be ranked
 constexpr int kBySearch = 4096; // top_k up to which its entries' sum is searched by key alone
 
@@ -1436,6 +1437,20 @@ hipError_t run_open(const gwtf_learn_sample_t &a, const RecheckWorkspace &ws, hi
     return hipSuccess;
 }
 
+// How many waves take a row, and how many eights a lane keeps.  Few waves leave room for other rows on a
+// compute unit, many end one row sooner; this way and the other (us, bf16 if nothing else is said):
+//   no filter, 4 waves to 16,384 columns: 1,024 rows of 4,096 13.0, of 16,384 21.5 (16 waves 18.4, 24.3; 64 rows
+//     10.4 and 9.3); beyond, 64 rows of 32,768 15.4, 1,024 29.6 (4 waves 19.4, 34.5)
+//   no filter, 16 waves for no more rows than the card has compute units: 64 rows of 20,000 15.3, 256 16.3 (8 waves
+//     16.8, 18.0); from there on 8: 512 rows 21.0, 1,024 26.2 (26.8, 39.8).  At 131,072 columns 8 waves and
+//     the second launch would be ahead for few rows too: 64 rows 43, with them 27
+//   filters, 4 waves of one eight to 2,048: 1,024 rows of 1,000 with top_p 20.5 (of four eights 32.9)
+//   4 waves to 8,192: 1,024 rows of 4,096 with top_p 39, with top_k 50 22 (16 waves 73, 46; 64 rows of 8,192 with top_p
+//     24 and 22)
+//   16 waves beyond: 64 rows of 16,384 with top_p 27, 1,024 100 (4 waves of eight eights 36, 75)
+//   16 eights in registers to 131,072 of 16 bits: 64 rows with top_p 105, of 152,064, read at every look, 132
+constexpr int64_t kFewRows = 256;
+
 template <class T>
 hipError_t by_width(const gwtf_learn_sample_t &a, const RecheckWorkspace &ws, hipStream_t s)
 {
@@ -1445,7 +1460,7 @@ hipError_t by_width(const gwtf_learn_sample_t &a, const RecheckWorkspace &ws, hi
                       a.temperature > 1e-30 && a.temperature < 1e30;
     if (open && V <= kOpenMost) {
         if (V <= 16384) return run_open<T, 4, false>(a, ws, s);
-        if (a.num_tokens <= 256) return run_open<T, 16, false>(a, ws, s);
+        if (a.num_tokens <= kFewRows) return run_open<T, 16, false>(a, ws, s);
         // rows for all of the card: uncertain ones are shared out at the end
         return a.num_tokens <= kRecheckRows ? run_open<T, 8, true>(a, ws, s) : run_open<T, 8, false>(a, ws, s);
     }

@@ -10,8 +10,8 @@
 // kernel's arguments, 50 a launch, 70).
 //
 // Bound by memory: 38 million bf16 weights with 32-bit copies, states and gradients 208 us
-// (1.13 GB, 5.5 TB/s), 201 million with 8-bit states 393 us (2.04 GB, 5.2 TB/s), where vector
-// issue takes as long: 82 instructions a value, 27 of them the generator's, which
+// (1.13 GB, 5.5 TB/s), 201 million with 8-bit states 397 us (2.04 GB, 5.1 TB/s), where vector
+// issue takes as long: 84 instructions a value, 27 of them the generator's, which
 // serves m and v with the same 16 bits.  With divisions and exact roots in place of the
 // hardware's 542 us.  The norm of 201 million bf16 70 us (5.8 TB/s).
 #include "learn_internal.h"

@@ -128,7 +128,8 @@ class Parameters:
 
     The lists hold the memory that the tensors had when they were given, and
     keep it: gradients are written into the same tensors at every step
-    (accumulated, or copied), and a parameter that is to live elsewhere needs a new list.
+    (accumulated after ``zero_grad(set_to_none=False)``, or copied; tensors that
+    torch makes anew are not seen), and a parameter that is to live elsewhere needs a new list.
     Lists are made, and given up, outside of stream captures.
 
     A step moves the versions of ``params`` and ``master``, so that a backward pass
